@@ -413,6 +413,167 @@ maxdnn_status maxdnn_conv_bprop_filter(const maxdnn_conv_desc* desc, maxdnn_kern
                                        void* workspace, size_t workspace_bytes,
                                        void* cuda_stream);
 
+/*
+ * ======================================================================================
+ * Training and serving in 8 bits: matrix product, packing, layer norm, activation
+ * ======================================================================================
+ *
+ * The linear layers between and behind convolutions (a 1x1 convolution is one), with operands
+ * and kept activations in 8-bit floating point.  Matrices here are ROW-MAJOR, rows = tokens
+ * (positions of all images or sequences), columns = channels, with a row pitch in elements
+ * (ld*).  Conventions of the entry points above hold: device pointers aligned to 16 bytes
+ * (scales, statistics and weight vectors: to their element), no overlap between inputs and
+ * outputs, work enqueued on cuda_stream, errors as return codes, nothing allocated after the
+ * device's first call (make that outside stream capture).  A matrix of no rows is valid:
+ * nothing is launched, except that sums over no rows are written as zeros.
+ *
+ * The packed format.  Values are E4M3 (largest 448) or E5M2 (largest 57344), in blocks of up
+ * to 128 values, which end early at the matrix's end.  A block's scale is a power of two, kept
+ * as an E8M0 byte (exponent + 127; what the value stands for is q 2^E): with m the largest
+ * finite magnitude in the block, E is the least integer with m <= 2^E (largest), clamped to
+ * [-126, 127]; 0 for a block of zeros.  q is x 2^-E rounded to nearest, ties to even: one
+ * rounding, the same whoever computes it.  NaN stay NaN; infinities become NaN (E4M3) or stay
+ * (E5M2), and neither touches the scale of its neighbours.
+ *   MAXDNN_BLOCK_ROW   1 x 128:   scales [ceil(cols/128)][rows]
+ *   MAXDNN_BLOCK_COL   128 x 1:   scales [ceil(rows/128)][cols]
+ *   MAXDNN_BLOCK_TILE  128 x 128: scales [ceil(rows/128)][ceil(cols/128)]
+ * A packed matrix's row pitch is a multiple of 16 bytes where the library writes it or
+ * multiplies it (NOT_SUPPORTED otherwise).
+ */
+typedef enum maxdnn_dtype {
+  MAXDNN_F32 = 0,
+  MAXDNN_BF16 = 1,
+  MAXDNN_F16 = 2,
+  MAXDNN_E4M3 = 3,
+  MAXDNN_E5M2 = 4,
+  MAXDNN_E8M0 = 5   /* scales only */
+} maxdnn_dtype;
+
+typedef enum maxdnn_block {
+  MAXDNN_BLOCK_ROW = 0,
+  MAXDNN_BLOCK_COL = 1,
+  MAXDNN_BLOCK_TILE = 2
+} maxdnn_block;
+
+/*
+ * Packing.  x is a wide matrix (x_type F32, BF16, F16), or a packed one (x_type E4M3 / E5M2 with
+ * x_scale, its ROW-block scales): an activation kept for the backward pass in row blocks, the
+ * forward product's operand, is packed again in column blocks for the weight gradient.  Any
+ * of the three forms may be asked for in one call (q_* with s_*; null: not wanted); x is read once.
+ * ldq is the pitch of every q_*.
+ */
+typedef struct maxdnn_quant8_desc {
+  int32_t rows, cols;
+  int64_t ldx, ldq;
+  int32_t x_type, q_type;
+} maxdnn_quant8_desc;
+
+maxdnn_status maxdnn_quant8(const maxdnn_quant8_desc* desc, const void* x, const void* x_scale,
+                            void* q_row, void* s_row, void* q_col, void* s_col, void* q_tile,
+                            void* s_tile, void* cuda_stream);
+/* The values that a packed matrix stands for, in x_type (wide). */
+maxdnn_status maxdnn_dequant8(const maxdnn_quant8_desc* desc, maxdnn_block block, const void* q,
+                              const void* s, void* x, void* cuda_stream);
+
+/*
+ * Matrix product of two packed matrices, 32-bit sums:
+ *
+ *   C[m, n] = sum_k (a[m, k] sa) (b[n, k] sb)
+ *
+ * Each operand is given as it is stored.  MAXDNN_MAJOR_K: rows are m (n), columns the reduction
+ * k, blocks ROW or TILE.  MAXDNN_MAJOR_MN: rows are the reduction k, columns m (n), blocks COL or
+ * TILE.  (Blocks lie along the reduction, so that a scale can be applied to the sum over one.)
+ * With X [T][I] and W [O][I], Y = X W^T:
+ *   Y  (T x O):  A = X, MAJOR_K, ROW;     B = W, MAJOR_K, TILE
+ *   dX (T x I):  A = dY, MAJOR_K, ROW;    B = W, MAJOR_MN, TILE   (the same packed weights)
+ *   dW (O x I):  A = dY, MAJOR_MN, COL;   B = X, MAJOR_MN, COL
+ * a_type / b_type: E4M3 or E5M2, independently.  Scales: E8M0 bytes or fp32 numbers (weights that
+ * were packed elsewhere; the product of two scales must be a finite fp32 number).  C: F32, BF16
+ * or F16, row-major with pitch ldc, overwritten.  K = 0 writes zeros.
+ * The sum over a block of 128 is taken by the tensor core, scaled, and added in fp32 with one
+ * rounding per block; results do not change from run to run.
+ * NOT_SUPPORTED: lda or ldb not a multiple of 16, a size above 2^30.
+ */
+typedef enum maxdnn_major { MAXDNN_MAJOR_K = 0, MAXDNN_MAJOR_MN = 1 } maxdnn_major;
+
+typedef struct maxdnn_gemm8_desc {
+  int32_t M, N, K;
+  int64_t lda, ldb, ldc;
+  int32_t a_type, b_type, c_type;
+  int32_t a_major, b_major;
+  int32_t a_block, b_block;
+  int32_t a_scale_type, b_scale_type;   /* MAXDNN_E8M0 or MAXDNN_F32 */
+} maxdnn_gemm8_desc;
+
+maxdnn_status maxdnn_gemm8(const maxdnn_gemm8_desc* desc, const void* a, const void* a_scale,
+                           const void* b, const void* b_scale, void* c, void* cuda_stream);
+
+/*
+ * Layer norm over the columns (population variance):
+ *
+ *   mean = sum x / cols,  rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps)
+ *   y = (x - mean) rstd gamma + beta
+ *
+ * gamma / beta: [cols] in w_type (F32, BF16, F16), null for 1 / 0.  Forward, any of the results
+ * may be null: y (y_type = x_type, pitch ldy), mean and rstd (fp32 [rows], what the backward pass
+ * reads), (q, s): y packed in row blocks, the next product's operand, and (c, sc): x packed in
+ * row blocks, which the backward pass takes in place of x (both q_type, pitch ldq; y is packed
+ * from its 32-bit value).  NOT_SUPPORTED: x_type other than y_type (forward; backward unless x
+ * is packed).
+ */
+typedef struct maxdnn_layer_norm_desc {
+  int32_t rows, cols;
+  int64_t ldx, ldy, ldq;      /* pitch of x; of y, dy and dx; of q and c */
+  int32_t x_type, y_type, w_type, q_type;
+  float eps;
+} maxdnn_layer_norm_desc;
+
+maxdnn_status maxdnn_layer_norm_fprop(const maxdnn_layer_norm_desc* desc, const void* x,
+                                      const void* gamma, const void* beta, void* y, float* mean,
+                                      float* rstd, void* q, void* s, void* c, void* sc,
+                                      void* cuda_stream);
+/* dx (y_type), dgamma and dbeta (fp32 [cols], null: not wanted), with xh = (x - mean) rstd:
+ *   dx = rstd (g - mean(g) - xh mean(g xh)),  g = gamma dy
+ *   dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy
+ * x: wide (x_type = y_type), or packed in row blocks (x_type E4M3 / E5M2, x_scale).  The sums over rows
+ * go through the workspace and are added in a fixed order. */
+maxdnn_status maxdnn_layer_norm_bprop_workspace(const maxdnn_layer_norm_desc* desc, size_t* bytes);
+maxdnn_status maxdnn_layer_norm_bprop(const maxdnn_layer_norm_desc* desc, const void* dy,
+                                      const void* x, const void* x_scale, const void* gamma,
+                                      const float* mean, const float* rstd, void* dx, float* dgamma,
+                                      float* dbeta, void* workspace, size_t workspace_bytes,
+                                      void* cuda_stream);
+
+/*
+ * Activation of a feed-forward layer, gated (a = f(g) u; h is [rows][2 cols], g in the first half
+ * of a row, u in the second) or plain (a = f(g); h is [rows][cols]):
+ *   SILU g / (1 + exp(-g));  GELU g P(g), P the normal distribution function;
+ *   GELU_TANH g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2
+ * Forward: a (x_type, pitch lda; may be null), (q, s): a packed in row blocks, the next product's
+ * operand (may be null, not both), and (c, sc): h packed for the backward pass (may be null),
+ * each half in row blocks of its own (u's blocks start at its first column): c [rows] with pitch
+ * ldc, sc [2 ceil(cols/128)][rows], the first half's blocks first.
+ * Backward: dh from da and h, where h is wide (h_type = x_type, pitch ldh) or packed
+ * (h_type E4M3 / E5M2, pitch ldc, h_scale):  dg = da u f'(g),  du = da f(g).
+ */
+typedef enum maxdnn_act {
+  MAXDNN_ACT_SILU = 0,
+  MAXDNN_ACT_GELU = 1,
+  MAXDNN_ACT_GELU_TANH = 2
+} maxdnn_act;
+
+typedef struct maxdnn_act8_desc {
+  int32_t rows, cols;               /* of a */
+  int64_t ldh, lda, ldq, ldc;       /* pitch of h and dh; of a and da; of q; of packed h */
+  int32_t x_type, h_type, q_type;
+  int32_t act, gated;
+} maxdnn_act8_desc;
+
+maxdnn_status maxdnn_act8_fprop(const maxdnn_act8_desc* desc, const void* h, void* a, void* q, void* s,
+                                void* c, void* sc, void* cuda_stream);
+maxdnn_status maxdnn_act8_bprop(const maxdnn_act8_desc* desc, const void* da, const void* h,
+                                const void* h_scale, void* dh, void* cuda_stream);
+
 /* Synchronises `cuda_stream`, then reads and clears the current device's
  * status word.  MAXDNN_OK, MAXDNN_DEVICE_TIMEOUT (a bounded wait inside some
  * kernel launched since the last query ran out; that kernel's output is not
@@ -442,7 +603,9 @@ maxdnn_status maxdnn_last_kernel_clock(uint32_t* sm_cycles, uint32_t* nanosecond
  * what the tile's ring would hold), FFMA_STREAMK (0: never split tail tiles along K; 2: always, whatever
  * the model says), UMMA_KC, UMMA_PAIR (1 two-SM / -1 one-SM tiles), UMMA_MERGE, UMMA_STAGE_KB, UMMA_COLS, WGRAD_SPLITS, WGRAD_PAIR, SM_COUNT (SM
  * count for host-only workspace queries), X3_CHUNK_ROWS, DEBUG_STATUS, KERNEL_CLOCK (see
- * maxdnn_last_kernel_clock), RAGGED_PADDED (see maxdnn_conv_fprop_ragged), and
+ * maxdnn_last_kernel_clock), RAGGED_PADDED (see maxdnn_conv_fprop_ragged), GEMM8_COLS,
+ * GEMM8_SPLIT, GEMM8_SWAP (pin maxdnn_gemm8's tile columns 16/32/64/128/256, the CTAs that share
+ * a tile's reduction 1/2/4/8, and whether the roles of A and B are exchanged), and
  * TEST_MISSING_ARRIVAL (test hook: CTA 0's "full" barriers expect an arrival that
  * never comes, so a bounded wait runs out).  The environment variable MAXDNN_<name>
  * gives an option its initial value; the environment is read once, at the first use of

@@ -8,5 +8,7 @@ raises — there is no CPU fallback.
 from . import workloads  # noqa: F401
 from .binding import *  # noqa: F401,F403
 from .binding import __all__ as _binding_all
+from .train8 import *  # noqa: F401,F403
+from .train8 import __all__ as _train8_all
 
-__all__ = ["workloads"] + list(_binding_all)
+__all__ = ["workloads"] + list(_binding_all) + list(_train8_all)

@@ -49,6 +49,9 @@ EXPORTED_SYMBOLS = [
     "maxdnn_last_device_status_noalloc", "maxdnn_set_option", "maxdnn_unset_option",
     "maxdnn_get_option", "maxdnn_reset_options", "maxdnn_last_kernel_clock",
     "maxdnn_conv_plan_items",
+    "maxdnn_quant8", "maxdnn_dequant8", "maxdnn_gemm8", "maxdnn_layer_norm_fprop",
+    "maxdnn_layer_norm_bprop_workspace", "maxdnn_layer_norm_bprop", "maxdnn_act8_fprop",
+    "maxdnn_act8_bprop",
 ]
 
 

@@ -1,0 +1,177 @@
+// Gated (or plain) activation of a feed-forward layer that works with packed activations.
+//
+//   a = f(g) u   (plain: a = f(g));   dg = da u f'(g),  du = da f(g)
+//
+// h holds g in columns [0, C) and u in [C, 2C).  Forward, a is packed as the next product's
+// operand and g, u are packed as what the backward pass will read; backward, g and u come from
+// there (or from h itself).  f: SiLU g s(g); GELU g P(g), P the normal distribution; GELU with
+// the tanh approximation.
+//
+// A CTA takes 128 columns x 64 rows: 16 lanes cover a row block, thread t has eight columns of
+// the rows t/16 + 16 k, so 4 (plain) or 8 (gated) loads of 16 bytes are in flight per thread.
+#pragma once
+#include "fp8_util.cuh"
+
+namespace maxdnn {
+
+constexpr int kActThreads = 256;
+constexpr int kActRows = 64;
+
+struct Act8Args {
+  const void* h;               // wide, or packed (bprop)
+  const uint8_t* h_scale;
+  void* a;                     // fprop, may be null
+  uint8_t *q, *s;              // packed a, may be null
+  uint8_t *c, *sc;             // packed h, may be null
+  const void* da;
+  void* dh;
+  int64_t ldh, lda, ldq, ldc;
+  int32_t rows, cols, col_blocks;
+  int32_t vec_h, vec_u, vec_a, vec_c, vec_cu, vec_dh, vec_du;
+};
+
+// f and, where asked for, f'.
+template <int ACT, bool GRAD>
+__device__ __forceinline__ void activation(float g, float* f, float* df) {
+  if constexpr (ACT == MAXDNN_ACT_SILU) {
+    const float s = 1.f / (1.f + expf(-g));
+    *f = g * s;
+    if (GRAD) *df = s * fmaf(g, 1.f - s, 1.f);
+  } else if constexpr (ACT == MAXDNN_ACT_GELU) {
+    const float p = 0.5f * (1.f + erff(g * 0.70710678118654752f));
+    *f = g * p;
+    if (GRAD) *df = fmaf(g * 0.39894228040143268f, expf(-0.5f * g * g), p);
+  } else {
+    const float k = 0.79788456080286536f;                    // sqrt(2 / pi)
+    const float t = tanhf(k * fmaf(0.044715f * g * g, g, g));
+    const float p = 0.5f * (1.f + t);
+    *f = g * p;
+    if (GRAD) *df = fmaf(0.5f * g * (1.f - t * t), k * fmaf(0.134145f, fminf(g * g, 1e8f), 1.f), p);   // no 0 x inf
+  }
+}
+
+// Packs eight values of a row block; returns the scale byte.
+template <int QT>
+__device__ __forceinline__ uint32_t pack_row8(const float (&v)[8], uint8_t* p, int n, bool vec, bool live) {
+  float m = max_over_block_lanes(max8(v));
+  const bool fix = isinf(m);
+  if (__any_sync(0xFFFFFFFFu, fix)) m = max_over_block_lanes(finite_max8(v));
+  const uint32_t byte = scale_byte<QT>(m);
+  if (live) store_bytes8(p, pack8<QT>(v, inv_scale_of(byte), fix), n, vec);
+  return byte;
+}
+
+template <int XT, int QT, int ACT, bool GATED>
+__global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_constant__ Act8Args args) {
+  typedef typename ElemOf<XT>::T T;
+  __shared__ uint8_t bytes[3][kActRows];
+  const int t = threadIdx.x;
+  const int cb = blockIdx.x % args.col_blocks;
+  const int rb = blockIdx.x / args.col_blocks;
+  const int r0 = rb * kActRows, c0 = cb * kBlock8 + 8 * (t & 15);
+  const int n = min(max(args.cols - c0, 0), 8);
+  const T* h = static_cast<const T*>(args.h);
+  Raw8<XT> rg[4], ru[GATED ? 4 : 1];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = r0 + (t >> 4) + 16 * k;
+    const int nr = r < args.rows ? n : 0;
+    rg[k] = load_raw8<XT>(h + (int64_t)r * args.ldh + c0, nr, args.vec_h != 0);
+    if constexpr (GATED) ru[k] = load_raw8<XT>(h + (int64_t)r * args.ldh + args.cols + c0, nr, args.vec_u != 0);
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = r0 + (t >> 4) + 16 * k;
+    const bool live = r < args.rows && n > 0;
+    float g[8], u[8], a[8];
+    to_float8<XT>(rg[k], g);
+    if constexpr (GATED) to_float8<XT>(ru[k], u);
+    if (args.c) {
+      uint8_t* c = args.c + (int64_t)r * args.ldc + c0;
+      uint32_t b = pack_row8<QT>(g, c, n, args.vec_c != 0, live);
+      if ((t & 15) == 0) bytes[1][(t >> 4) + 16 * k] = (uint8_t)b;
+      if constexpr (GATED) {
+        b = pack_row8<QT>(u, c + args.cols, n, args.vec_cu != 0, live);
+        if ((t & 15) == 0) bytes[2][(t >> 4) + 16 * k] = (uint8_t)b;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float f, unused;
+      activation<ACT, false>(g[i], &f, &unused);
+      a[i] = GATED ? f * u[i] : f;
+    }
+    if (args.a && live)
+      store_float8<XT>(static_cast<T*>(args.a) + (int64_t)r * args.lda + c0, a, n, args.vec_a != 0);
+    if (args.q) {
+      const uint32_t b = pack_row8<QT>(a, args.q + (int64_t)r * args.ldq + c0, n, true, live);
+      if ((t & 15) == 0) bytes[0][(t >> 4) + 16 * k] = (uint8_t)b;
+    }
+  }
+  __syncthreads();
+  // scales of this CTA's blocks: rows are next to each other
+  const int row = t & (kActRows - 1), which = t / kActRows;
+  if (r0 + row >= args.rows) return;
+  const int64_t at = (int64_t)cb * args.rows + r0 + row;
+  if (which == 0 && args.q) args.s[at] = bytes[0][row];
+  if (which == 1 && args.c) args.sc[at] = bytes[1][row];
+  if (GATED && which == 2 && args.c) args.sc[(int64_t)args.col_blocks * args.rows + at] = bytes[2][row];
+}
+
+// HT: the type of h (wide, or packed); XT: of da and dh.
+template <int HT, int XT, int ACT, bool GATED>
+__global__ void __launch_bounds__(kActThreads) act8_bprop_kernel(const __grid_constant__ Act8Args args) {
+  typedef typename ElemOf<HT>::T TH;
+  typedef typename ElemOf<XT>::T T;
+  const int t = threadIdx.x;
+  const int cb = blockIdx.x % args.col_blocks;
+  const int rb = blockIdx.x / args.col_blocks;
+  const int r0 = rb * kActRows + (t >> 4), c0 = cb * kBlock8 + 8 * (t & 15);
+  const int n = min(max(args.cols - c0, 0), 8);
+  if (n == 0) return;
+  const TH* h = static_cast<const TH*>(args.h);
+  const int64_t ldh = is_fp8(HT) ? args.ldc : args.ldh;
+  Raw8<HT> rg[4], ru[GATED ? 4 : 1];
+  Raw8<XT> rd[4];
+  float sg[4], su[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = r0 + 16 * k;
+    const int nr = r < args.rows ? n : 0;
+    rg[k] = load_raw8<HT>(h + (int64_t)r * ldh + c0, nr, args.vec_h != 0);
+    if constexpr (GATED) ru[k] = load_raw8<HT>(h + (int64_t)r * ldh + args.cols + c0, nr, args.vec_u != 0);
+    rd[k] = load_raw8<XT>(static_cast<const T*>(args.da) + (int64_t)r * args.lda + c0, nr, args.vec_a != 0);
+    sg[k] = su[k] = 1.f;
+    if (is_fp8(HT) && nr > 0) {
+      sg[k] = e8m0_value(args.h_scale[(int64_t)cb * args.rows + r]);
+      if constexpr (GATED) su[k] = e8m0_value(args.h_scale[(int64_t)(args.col_blocks + cb) * args.rows + r]);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = r0 + 16 * k;
+    if (r >= args.rows) break;
+    float g[8], u[8], d[8], dg[8], du[8];
+    to_float8<HT>(rg[k], g);
+    if constexpr (GATED) to_float8<HT>(ru[k], u);
+    to_float8<XT>(rd[k], d);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (is_fp8(HT)) g[i] *= sg[k];
+      if constexpr (is_fp8(HT) && GATED) u[i] *= su[k];
+      float f, df;
+      activation<ACT, true>(g[i], &f, &df);
+      if constexpr (GATED) {
+        dg[i] = d[i] * u[i] * df;
+        du[i] = d[i] * f;
+      } else {
+        dg[i] = d[i] * df;
+      }
+    }
+    T* dh = static_cast<T*>(args.dh) + (int64_t)r * args.ldh + c0;
+    store_float8<XT>(dh, dg, n, args.vec_dh != 0);
+    if constexpr (GATED) store_float8<XT>(dh + args.cols, du, n, args.vec_du != 0);
+  }
+}
+
+}  // namespace maxdnn

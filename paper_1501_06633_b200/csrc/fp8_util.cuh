@@ -1,0 +1,255 @@
+// Element types of the 8-bit training operators: conversions between fp32 and the storage types,
+// loads and stores of eight neighbouring values, and the scale of a block.
+//
+// Format.  A block of up to 128 values has one scale 2^E, kept as the byte E + 127 (E8M0).  With
+// m the largest finite magnitude of the block and V = 1.75 2^8 (E4M3) or 1.75 2^15 (E5M2) the
+// largest number of the type, E is the least integer with m <= V 2^E: the exponent of m less 8
+// (15), plus one if m's mantissa is above 1.75.  It is clamped to [-126, 127], so that 2^E and
+// 2^-E are normal numbers, and is 0 for a block of zeros.  Multiplying by a power of two is
+// exact: a value is rounded once, to the 8-bit type, and the result does not depend on who
+// computes it.  Infinities and NaN do not enter m; they are stored as NaN (E4M3, which has no
+// infinity) or as themselves (E5M2).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/maxdnn.h"
+
+namespace maxdnn {
+
+constexpr int kBlock8 = 128;       // values along a block
+constexpr int kLanesPerBlock = 16; // lanes of eight values that cover a block
+
+template <int DT> struct ElemOf;
+template <> struct ElemOf<MAXDNN_F32> { typedef float T; };
+template <> struct ElemOf<MAXDNN_BF16> { typedef __nv_bfloat16 T; };
+template <> struct ElemOf<MAXDNN_F16> { typedef __half T; };
+template <> struct ElemOf<MAXDNN_E4M3> { typedef uint8_t T; };
+template <> struct ElemOf<MAXDNN_E5M2> { typedef uint8_t T; };
+
+__host__ __device__ constexpr int elem_bytes(int dt) {
+  return dt == MAXDNN_F32 ? 4 : (dt == MAXDNN_BF16 || dt == MAXDNN_F16) ? 2 : 1;
+}
+__host__ __device__ constexpr bool is_fp8(int dt) { return dt == MAXDNN_E4M3 || dt == MAXDNN_E5M2; }
+__host__ __device__ constexpr bool is_wide(int dt) {
+  return dt == MAXDNN_F32 || dt == MAXDNN_BF16 || dt == MAXDNN_F16;
+}
+
+// ---- two 8-bit values <-> fp32 (low byte first) ----
+template <int QT>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint16_t r;
+  if constexpr (QT == MAXDNN_E4M3)
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  else
+    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <int QT>
+__device__ __forceinline__ float2 unpack2(uint32_t two) {
+  uint32_t h;
+  const uint16_t t = (uint16_t)two;
+  if constexpr (QT == MAXDNN_E4M3)
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(t));
+  else
+    asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(h) : "h"(t));
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+// Eight values in 8 bytes.  FIX: infinities become NaN (E4M3) or infinity (E5M2), where the
+// conversion above would give the largest number; needed only where a block holds one.
+template <int QT>
+__device__ __forceinline__ uint2 pack8(const float (&v)[8], float inv, bool fix) {
+  uint32_t w[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t a = pack2<QT>(v[4 * h] * inv, v[4 * h + 1] * inv);
+    const uint32_t b = pack2<QT>(v[4 * h + 2] * inv, v[4 * h + 3] * inv);
+    w[h] = a | (b << 16);
+  }
+  if (fix) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (isinf(v[i])) {
+        const uint32_t code = (v[i] < 0 ? 0x80u : 0u) | (QT == MAXDNN_E4M3 ? 0x7Fu : 0x7Cu);
+        const int sh = 8 * (i & 3);
+        w[i >> 2] = (w[i >> 2] & ~(0xFFu << sh)) | (code << sh);
+      }
+    }
+  }
+  return make_uint2(w[0], w[1]);
+}
+
+// ---- scales ----
+// The biased exponent byte for a largest magnitude `m` (finite, not negative).
+template <int QT>
+__device__ __forceinline__ uint32_t scale_byte(float m) {
+  constexpr int kTop = QT == MAXDNN_E4M3 ? 8 : 15;
+  const uint32_t b = __float_as_uint(m);
+  // adding 0x1FFFFF carries into the exponent exactly where the mantissa is above 1.75
+  const int e = (int)((b + 0x1FFFFFu) >> 23) - kTop;
+  return b == 0 ? 127u : (uint32_t)max(e, 1);
+}
+// 2^E and 2^-E of a byte in [1, 253].
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+__device__ __forceinline__ float inv_scale_of(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+// Any E8M0 byte: 0 is 2^-127, 255 is NaN.
+__device__ __forceinline__ float e8m0_value(uint32_t byte) {
+  return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7FC00000u : byte << 23);
+}
+
+__device__ __forceinline__ float max_over_block_lanes(float m) {
+#pragma unroll
+  for (int d = kLanesPerBlock / 2; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+  return m;
+}
+
+// Largest magnitude of eight values; NaN do not count, infinities do (see finite_max8).
+__device__ __forceinline__ float max8(const float (&v)[8]) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[i]));
+  return m;
+}
+__device__ __forceinline__ float finite_max8(const float (&v)[8]) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, isinf(v[i]) ? 0.f : fabsf(v[i]));
+  return m;
+}
+
+// ---- eight neighbouring values as they lie in memory ----
+template <int DT> struct Raw8;
+template <> struct Raw8<MAXDNN_F32> { uint4 a, b; };
+template <> struct Raw8<MAXDNN_BF16> { uint4 a; };
+template <> struct Raw8<MAXDNN_F16> { uint4 a; };
+template <> struct Raw8<MAXDNN_E4M3> { uint2 a; };
+template <> struct Raw8<MAXDNN_E5M2> { uint2 a; };
+
+// Loads `n` (0..8) values at `p`; the rest are zeros.  vec: p is aligned for the wide load.
+template <int DT>
+__device__ __forceinline__ Raw8<DT> load_raw8(const typename ElemOf<DT>::T* p, int n, bool vec) {
+  typedef typename ElemOf<DT>::T T;
+  Raw8<DT> r;
+  if (n == 8 && vec) {
+    if constexpr (DT == MAXDNN_F32) {
+      r.a = __ldg(reinterpret_cast<const uint4*>(p));
+      r.b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
+    } else if constexpr (is_fp8(DT)) {
+      r.a = __ldg(reinterpret_cast<const uint2*>(p));
+    } else {
+      r.a = __ldg(reinterpret_cast<const uint4*>(p));
+    }
+  } else {
+    uint32_t w[8 * sizeof(T) / 4];
+#pragma unroll
+    for (int i = 0; i < (int)(8 * sizeof(T) / 4); ++i) w[i] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i < n) {
+        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(p[i]);
+        else if constexpr (sizeof(T) == 2)
+          w[i >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
+        else w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+      }
+    }
+    if constexpr (DT == MAXDNN_F32) {
+      r.a = make_uint4(w[0], w[1], w[2], w[3]);
+      r.b = make_uint4(w[4], w[5], w[6], w[7]);
+    } else if constexpr (is_fp8(DT)) {
+      r.a = make_uint2(w[0], w[1]);
+    } else {
+      r.a = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  return r;
+}
+
+template <int DT>
+__device__ __forceinline__ void to_float8(const Raw8<DT>& r, float (&v)[8]) {
+  if constexpr (DT == MAXDNN_F32) {
+    v[0] = __uint_as_float(r.a.x); v[1] = __uint_as_float(r.a.y);
+    v[2] = __uint_as_float(r.a.z); v[3] = __uint_as_float(r.a.w);
+    v[4] = __uint_as_float(r.b.x); v[5] = __uint_as_float(r.b.y);
+    v[6] = __uint_as_float(r.b.z); v[7] = __uint_as_float(r.b.w);
+  } else if constexpr (DT == MAXDNN_BF16) {
+    const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  } else if constexpr (DT == MAXDNN_F16) {
+    const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      v[2 * i] = f.x;
+      v[2 * i + 1] = f.y;
+    }
+  } else {
+    const uint32_t w[2] = {r.a.x, r.a.y};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = unpack2<DT>(w[i >> 1] >> (16 * (i & 1)));
+      v[2 * i] = f.x;
+      v[2 * i + 1] = f.y;
+    }
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ typename ElemOf<DT>::T from_float(float v) {
+  if constexpr (DT == MAXDNN_F32) return v;
+  else if constexpr (DT == MAXDNN_BF16) return __float2bfloat16_rn(v);
+  else return __float2half_rn(v);
+}
+
+template <int DT>
+__device__ __forceinline__ void store_float8(typename ElemOf<DT>::T* p, const float (&v)[8], int n, bool vec) {
+  static_assert(!is_fp8(DT), "8-bit values are stored by store_bytes8");
+  if (n == 8 && vec) {
+    if constexpr (DT == MAXDNN_F32) {
+      reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+      reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (DT == MAXDNN_BF16) {
+          const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+          w[i] = *reinterpret_cast<const uint32_t*>(&t);
+        } else {
+          const __half2 t = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+          w[i] = *reinterpret_cast<const uint32_t*>(&t);
+        }
+      }
+      *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = from_float<DT>(v[i]);
+  }
+}
+
+__device__ __forceinline__ void store_bytes8(uint8_t* p, uint2 w, int n, bool vec) {
+  if (n == 8 && vec) {
+    *reinterpret_cast<uint2*>(p) = w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+  }
+}
+
+// A weight of run-time type (read once per kernel, not per row).
+__device__ __forceinline__ float load_weight(const void* p, int64_t i, int type) {
+  if (type == MAXDNN_F32) return static_cast<const float*>(p)[i];
+  if (type == MAXDNN_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+  return __half2float(static_cast<const __half*>(p)[i]);
+}
+
+}  // namespace maxdnn

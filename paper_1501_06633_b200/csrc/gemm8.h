@@ -1,0 +1,28 @@
+// Host-side planning of the 8-bit matrix product: argument checks and the choice of tile, operand
+// roles and split.  Plain C++, no CUDA calls.
+#pragma once
+#include <stdint.h>
+
+#include "../../include/maxdnn.h"
+
+namespace maxdnn {
+
+constexpr int kGemm8TileM = 128;     // rows of a tile (TMEM lanes)
+constexpr int kGemm8BlockK = 128;    // reduction steps per stage: one scale block
+constexpr int kGemm8MaxSplit = 8;    // CTAs of a cluster that share one tile's reduction
+
+struct Gemm8Plan {
+  int32_t swap;        // 1: the kernel's rows are the columns of C (few rows of C)
+  int32_t tile_n;      // columns of a tile: 16, 32, 64, 128 or 256
+  int32_t split;       // CTAs that share a tile's reduction: 1, 2, 4 or 8
+  int32_t m_tiles, n_tiles, k_blocks;
+  int32_t stages;
+  int32_t b_stage_bytes;
+  int32_t grid;
+  int32_t smem_bytes;
+};
+
+maxdnn_status check_gemm8(const maxdnn_gemm8_desc* d);
+maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* plan);
+
+}  // namespace maxdnn

@@ -10,6 +10,7 @@
 #include "bprop.cuh"
 #include "ffma_conv.cuh"
 #include "plan.h"
+#include "runtime.h"
 #include "umma_conv.cuh"
 #include "wgrad_umma.cuh"
 
@@ -1359,6 +1360,29 @@ maxdnn_status read_and_clear_status(DeviceState* ds, cudaStream_t stream) {
 }
 
 }  // namespace
+
+// ---- what other translation units use (see runtime.h) ----
+maxdnn_status runtime_device(RuntimeDevice* out) {
+  DeviceState* ds = nullptr;
+  const maxdnn_status st = device_state(&ds);
+  if (st != MAXDNN_OK) return st;
+  if (!ds->sm100) return MAXDNN_NOT_SUPPORTED;
+  out->state = ds;
+  out->index = (int)(ds - g_dev);
+  out->sm_count = ds->sm_count;
+  return MAXDNN_OK;
+}
+
+WaitCtx runtime_wait_ctx(const RuntimeDevice& dev) { return next_wait_ctx(static_cast<DeviceState*>(dev.state)); }
+
+maxdnn_status runtime_encode(CUtensorMap* m, CUtensorMapDataType dt, int rank, const void* base,
+                             const uint64_t* dims, const uint64_t* strides, const uint32_t* box,
+                             CUtensorMapSwizzle swz) {
+  return encode_map(m, dt, rank, base, dims, strides, box, swz);
+}
+
+void runtime_count_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
+
 }  // namespace maxdnn
 
 using namespace maxdnn;

@@ -87,7 +87,7 @@ __device__ __forceinline__ void record_give_up(const WaitCtx& wc, uint32_t code)
   atomicExch(wc.status + 1, wc.epoch);
 }
 
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, const WaitCtx& wc,
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, const WaitCtx& wc,
                                             uint32_t code) {
   const uint64_t t0 = globaltimer_ns();
   for (;;) {
@@ -109,7 +109,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const W
 
 // Exit-path wait after another wait ran out: copies already issued land within
 // microseconds; give their barrier one millisecond, then move on without a code.
-__device__ __noinline__ void mbar_wait_grace(uint32_t bar, uint32_t parity) {
+static __device__ __noinline__ void mbar_wait_grace(uint32_t bar, uint32_t parity) {
   const uint64_t t0 = globaltimer_ns();
   while (!mbar_try_wait(bar, parity))
     if (globaltimer_ns() - t0 > 1000000ull) break;
@@ -122,7 +122,7 @@ __device__ __noinline__ void mbar_wait_grace(uint32_t bar, uint32_t parity) {
 // Producer-side wait: sleeps between polls, so that a warp waiting for a ring slot
 // does not take issue slots from the arithmetic warps of its scheduler.  Same 2 s
 // budget as mbar_wait.
-__device__ __noinline__ bool mbar_wait_sleep_slow(uint32_t bar, uint32_t parity, const WaitCtx& wc,
+static __device__ __noinline__ bool mbar_wait_sleep_slow(uint32_t bar, uint32_t parity, const WaitCtx& wc,
                                                   uint32_t code) {
   const uint64_t t0 = globaltimer_ns();
   for (;;) {

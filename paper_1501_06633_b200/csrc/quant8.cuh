@@ -1,0 +1,199 @@
+// Packing of matrices into 8 bits with a scale for each block (rows, columns, tiles), from any
+// wide type or from another packed matrix, and unpacking.
+//
+// One CTA takes a 128 x 128 tile of the matrix, which is whole blocks of every kind, so that one
+// reading serves every packed form that is asked for.  Thread t holds eight neighbouring columns
+// (8 (t mod 16)) of the eight rows t/16 + 16 k, as they lie in memory: 16 lanes cover a row
+// block, and eight loads of 16 bytes are in flight in each thread.  Row maxima are shuffles over
+// those 16 lanes; column maxima are a maximum over the thread's rows, a shuffle between the two
+// halves of the warp and one pass through shared memory.
+#pragma once
+#include "fp8_util.cuh"
+
+namespace maxdnn {
+
+constexpr int kQuantThreads = 256;
+
+struct Quant8Args {
+  const void* x;
+  const uint8_t* x_scale;      // packed x: its row scales
+  uint8_t *q_row, *s_row, *q_col, *s_col, *q_tile, *s_tile;   // null: not asked for
+  int64_t ldx, ldq;
+  int32_t rows, cols;
+  int32_t col_blocks;          // blocks of 128 columns
+  int32_t vec_x;               // rows of x allow the wide load
+};
+
+template <int XT, int QT>
+__global__ void __launch_bounds__(kQuantThreads) quant8_kernel(const __grid_constant__ Quant8Args args) {
+  typedef typename ElemOf<XT>::T T;
+  __shared__ float col_part[kQuantThreads / 32][kBlock8];   // per warp: maxima of its rows
+  __shared__ float col_inv[kBlock8];
+  __shared__ uint8_t row_byte[kBlock8];
+  __shared__ float warp_max[kQuantThreads / 32];
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int cb = blockIdx.x % args.col_blocks;
+  const int rb = blockIdx.x / args.col_blocks;
+  const int r0 = rb * kBlock8, c0 = cb * kBlock8 + 8 * (t & 15);
+  const int n = min(max(args.cols - c0, 0), 8);
+  const int rg = t >> 4;
+  const T* x = static_cast<const T*>(args.x);
+  Raw8<XT> raw[8];
+  float xs[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = r0 + rg + 16 * k;
+    raw[k] = load_raw8<XT>(x + (int64_t)r * args.ldx + c0, r < args.rows ? n : 0, args.vec_x != 0);
+    if constexpr (is_fp8(XT))
+      xs[k] = r < args.rows ? e8m0_value(args.x_scale[(int64_t)cb * args.rows + r]) : 0.f;
+  }
+  // the eight values of one of the thread's rows
+  auto values = [&](int k, float (&v)[8]) {
+    to_float8<XT>(raw[k], v);
+    if constexpr (is_fp8(XT)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= xs[k];
+    }
+  };
+  float row_max[8], col_max[8];
+  bool inf = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) col_max[i] = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    float v[8];
+    values(k, v);
+    row_max[k] = max8(v);
+    inf |= isinf(row_max[k]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) col_max[i] = fmaxf(col_max[i], fabsf(v[i]));
+  }
+  const bool fix = __syncthreads_or(inf) != 0;   // rare: a tile that holds an infinity
+  if (fix) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) col_max[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      float v[8];
+      values(k, v);
+      row_max[k] = finite_max8(v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) col_max[i] = fmaxf(col_max[i], isinf(v[i]) ? 0.f : fabsf(v[i]));
+    }
+  }
+
+  auto store = [&](uint8_t* q, int k, float inv_row, const float* inv_col) {
+    const int r = r0 + rg + 16 * k;
+    if (r >= args.rows) return;
+    float v[8];
+    values(k, v);
+    if (inv_col) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = isinf(v[i]) ? v[i] : v[i] * inv_col[i];
+    }
+    store_bytes8(q + (int64_t)r * args.ldq + c0, pack8<QT>(v, inv_row, fix), n, true);
+  };
+
+  if (args.q_row) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t b = scale_byte<QT>(max_over_block_lanes(row_max[k]));
+      if ((t & 15) == 0) row_byte[rg + 16 * k] = (uint8_t)b;
+      store(args.q_row, k, inv_scale_of(b), nullptr);
+    }
+  }
+  if (args.q_col || args.q_tile) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) col_max[i] = fmaxf(col_max[i], __shfl_xor_sync(0xFFFFFFFFu, col_max[i], 16));
+    if (lane < 16) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) col_part[warp][8 * lane + i] = col_max[i];
+    }
+  }
+  __syncthreads();
+  if (args.q_row && t < kBlock8 && r0 + t < args.rows)
+    args.s_row[(int64_t)cb * args.rows + r0 + t] = row_byte[t];
+  if (!args.q_col && !args.q_tile) return;
+  if (t < kBlock8) {
+    float m = 0.f;
+#pragma unroll
+    for (int w = 0; w < kQuantThreads / 32; ++w) m = fmaxf(m, col_part[w][t]);
+    const uint32_t b = scale_byte<QT>(m);
+    col_inv[t] = inv_scale_of(b);
+    if (args.q_col && cb * kBlock8 + t < args.cols)
+      args.s_col[(int64_t)rb * args.cols + cb * kBlock8 + t] = (uint8_t)b;
+    m = max_over_block_lanes(m);
+    m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+    if (lane == 0) warp_max[warp] = m;
+  }
+  __syncthreads();
+  if (args.q_col) {
+    float inv[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) inv[i] = col_inv[8 * (t & 15) + i];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) store(args.q_col, k, 1.f, inv);
+  }
+  if (args.q_tile) {
+    const uint32_t b = scale_byte<QT>(fmaxf(fmaxf(warp_max[0], warp_max[1]), fmaxf(warp_max[2], warp_max[3])));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) store(args.q_tile, k, inv_scale_of(b), nullptr);
+    if (t == 0) args.s_tile[(int64_t)rb * args.col_blocks + cb] = (uint8_t)b;
+  }
+}
+
+struct Dequant8Args {
+  const uint8_t *q, *s;
+  void* x;
+  int64_t ldx, ldq;
+  int32_t rows, cols;
+  int32_t col_blocks;
+  int32_t block;               // maxdnn_block
+  int32_t vec_x, vec_q;
+};
+
+// The same tile and the same eight columns x eight rows in each thread.
+template <int XT, int QT>
+__global__ void __launch_bounds__(kQuantThreads) dequant8_kernel(const __grid_constant__ Dequant8Args args) {
+  typedef typename ElemOf<XT>::T T;
+  const int t = threadIdx.x;
+  const int cb = blockIdx.x % args.col_blocks;
+  const int rb = blockIdx.x / args.col_blocks;
+  const int r0 = rb * kBlock8 + (t >> 4), c0 = cb * kBlock8 + 8 * (t & 15);
+  const int n = min(max(args.cols - c0, 0), 8);
+  if (n == 0) return;
+  Raw8<QT> raw[8];
+  uint32_t byte[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = r0 + 16 * k;
+    raw[k] = load_raw8<QT>(args.q + (int64_t)r * args.ldq + c0, r < args.rows ? n : 0, args.vec_q != 0);
+    byte[k] = 127;
+    if (args.block == MAXDNN_BLOCK_ROW && r < args.rows) byte[k] = args.s[(int64_t)cb * args.rows + r];
+  }
+  float s[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s[i] = 1.f;
+  if (args.block == MAXDNN_BLOCK_COL) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) s[i] = e8m0_value(args.s[(int64_t)rb * args.cols + c0 + i]);
+  } else if (args.block == MAXDNN_BLOCK_TILE) {
+    const float one = e8m0_value(args.s[(int64_t)rb * args.col_blocks + cb]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = one;
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = r0 + 16 * k;
+    if (r >= args.rows) break;
+    float v[8];
+    to_float8<QT>(raw[k], v);
+    const float m = e8m0_value(byte[k]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = args.block == MAXDNN_BLOCK_ROW ? v[i] * m : v[i] * s[i];
+    store_float8<XT>(static_cast<T*>(args.x) + (int64_t)r * args.ldx + c0, v, n, args.vec_x != 0);
+  }
+}
+
+}  // namespace maxdnn

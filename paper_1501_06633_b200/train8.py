@@ -1,0 +1,305 @@
+"""ctypes binding of the 8-bit training operators of ``libmaxdnn.so``: same names as
+``include/maxdnn.h``, argument marshalling only.  Tensors are torch CUDA tensors; matrices may be
+views with a row pitch (``stride(0)``) that matches the descriptor.  8-bit values are
+``torch.float8_e4m3fn`` / ``torch.float8_e5m2``, scales ``torch.float8_e8m0fnu`` (or ``uint8`` bytes)."""
+from __future__ import annotations
+
+import ctypes
+
+from .binding import OK, MaxdnnError, load_library
+
+__all__ = [
+    "DTYPE_F32", "DTYPE_BF16", "DTYPE_F16", "DTYPE_E4M3", "DTYPE_E5M2", "DTYPE_E8M0",
+    "BLOCK_ROW", "BLOCK_COL", "BLOCK_TILE", "MAJOR_K", "MAJOR_MN",
+    "ACT_SILU", "ACT_GELU", "ACT_GELU_TANH",
+    "Quant8Desc", "Gemm8Desc", "LayerNormDesc", "Act8Desc",
+    "quant8", "dequant8", "gemm8", "layer_norm_fprop", "layer_norm_bprop_workspace",
+    "layer_norm_bprop", "act8_fprop", "act8_bprop", "empty_packed", "empty_scales",
+]
+
+DTYPE_F32, DTYPE_BF16, DTYPE_F16, DTYPE_E4M3, DTYPE_E5M2, DTYPE_E8M0 = range(6)
+BLOCK_ROW, BLOCK_COL, BLOCK_TILE = range(3)
+MAJOR_K, MAJOR_MN = range(2)
+ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(3)
+
+_vp = ctypes.c_void_p
+torch = None      # imported with the library, at the first call
+_TYPES = ()       # the tensor types of each DTYPE_* code
+
+
+def _round16(n):
+    return -(-int(n) // 16) * 16
+
+
+def _or(value, default):
+    return int(default if value is None else value)
+
+
+class Quant8Desc(ctypes.Structure):
+    """maxdnn_quant8_desc."""
+
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("ldx", ctypes.c_int64),
+                ("ldq", ctypes.c_int64), ("x_type", ctypes.c_int32), ("q_type", ctypes.c_int32)]
+
+    @classmethod
+    def make(cls, rows, cols, x_type=DTYPE_BF16, q_type=DTYPE_E4M3, ldx=None, ldq=None) -> "Quant8Desc":
+        return cls(int(rows), int(cols), _or(ldx, cols), _or(ldq, _round16(cols)), int(x_type), int(q_type))
+
+
+class Gemm8Desc(ctypes.Structure):
+    """maxdnn_gemm8_desc."""
+
+    _fields_ = [(n, ctypes.c_int32) for n in ("M", "N", "K")] + \
+               [(n, ctypes.c_int64) for n in ("lda", "ldb", "ldc")] + \
+               [(n, ctypes.c_int32) for n in ("a_type", "b_type", "c_type", "a_major", "b_major", "a_block",
+                                              "b_block", "a_scale_type", "b_scale_type")]
+
+    @classmethod
+    def make(cls, M, N, K, a_type=DTYPE_E4M3, b_type=DTYPE_E4M3, c_type=DTYPE_BF16, a_major=MAJOR_K,
+             b_major=MAJOR_K, a_block=None, b_block=BLOCK_TILE, a_scale_type=DTYPE_E8M0,
+             b_scale_type=DTYPE_E8M0, lda=None, ldb=None, ldc=None) -> "Gemm8Desc":
+        if a_block is None:
+            a_block = BLOCK_ROW if a_major == MAJOR_K else BLOCK_COL
+        return cls(int(M), int(N), int(K), _or(lda, _round16(K if a_major == MAJOR_K else M)),
+                   _or(ldb, _round16(K if b_major == MAJOR_K else N)), _or(ldc, N), int(a_type), int(b_type),
+                   int(c_type), int(a_major), int(b_major), int(a_block), int(b_block), int(a_scale_type),
+                   int(b_scale_type))
+
+
+class LayerNormDesc(ctypes.Structure):
+    """maxdnn_layer_norm_desc."""
+
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("ldx", ctypes.c_int64),
+                ("ldy", ctypes.c_int64), ("ldq", ctypes.c_int64), ("x_type", ctypes.c_int32),
+                ("y_type", ctypes.c_int32), ("w_type", ctypes.c_int32), ("q_type", ctypes.c_int32),
+                ("eps", ctypes.c_float)]
+
+    @classmethod
+    def make(cls, rows, cols, eps=1e-5, x_type=DTYPE_BF16, y_type=None, w_type=DTYPE_F32, q_type=DTYPE_E4M3,
+             ldx=None, ldy=None, ldq=None) -> "LayerNormDesc":
+        return cls(int(rows), int(cols), _or(ldx, cols), _or(ldy, cols), _or(ldq, _round16(cols)), int(x_type),
+                   _or(y_type, x_type), int(w_type), int(q_type), float(eps))
+
+
+class Act8Desc(ctypes.Structure):
+    """maxdnn_act8_desc."""
+
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64) for n in ("ldh", "lda", "ldq", "ldc")] + \
+               [(n, ctypes.c_int32) for n in ("x_type", "h_type", "q_type", "act", "gated")]
+
+    @classmethod
+    def make(cls, rows, cols, act=ACT_SILU, gated=True, x_type=DTYPE_BF16, h_type=None, q_type=DTYPE_E4M3,
+             ldh=None, lda=None, ldq=None, ldc=None) -> "Act8Desc":
+        wide = int(cols) * (2 if gated else 1)
+        return cls(int(rows), int(cols), _or(ldh, wide), _or(lda, cols), _or(ldq, _round16(cols)),
+                   _or(ldc, _round16(wide)), int(x_type), _or(h_type, x_type), int(q_type), int(act),
+                   1 if gated else 0)
+
+
+_lib = None
+
+
+def _library():
+    global _lib, torch, _TYPES
+    if _lib is None:
+        lib = load_library()
+        import torch
+        _TYPES = ((torch.float32,), (torch.bfloat16,), (torch.float16,),
+                  (torch.float8_e4m3fn, torch.uint8), (torch.float8_e5m2, torch.uint8),
+                  (torch.float8_e8m0fnu, torch.uint8))
+        P, sz = ctypes.POINTER, ctypes.c_size_t
+        for name, args in (
+                ("maxdnn_quant8", [P(Quant8Desc)] + [_vp] * 9),
+                ("maxdnn_dequant8", [P(Quant8Desc), ctypes.c_int] + [_vp] * 4),
+                ("maxdnn_gemm8", [P(Gemm8Desc)] + [_vp] * 6),
+                ("maxdnn_layer_norm_fprop", [P(LayerNormDesc)] + [_vp] * 11),
+                ("maxdnn_layer_norm_bprop_workspace", [P(LayerNormDesc), P(sz)]),
+                ("maxdnn_layer_norm_bprop", [P(LayerNormDesc)] + [_vp] * 10 + [sz, _vp]),
+                ("maxdnn_act8_fprop", [P(Act8Desc)] + [_vp] * 7),
+                ("maxdnn_act8_bprop", [P(Act8Desc)] + [_vp] * 5)):
+            fn = getattr(lib, name)
+            fn.restype, fn.argtypes = ctypes.c_int, args
+        _lib = lib
+    return _lib
+
+
+def _raise(status, where):
+    if status != OK:
+        raise MaxdnnError(status, where)
+
+
+def _mat(t, dtype, rows, cols, ld, what, optional=False):
+    """Address of a [rows][cols] matrix with row pitch ld: a 2-d view with these strides, or any
+    contiguous tensor of rows x cols elements where ld = cols."""
+    if t is None:
+        if optional:
+            return None
+        raise TypeError("%s must be a CUDA tensor" % what)
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise TypeError("%s must be a CUDA tensor" % what)
+    if not 0 <= dtype < len(_TYPES) or t.dtype not in _TYPES[dtype]:
+        raise TypeError("%s has dtype %s, which is not what the descriptor says" % (what, t.dtype))
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is not on the current device" % what)
+    if t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols:
+        if rows and ((cols > 1 and t.stride(1) != 1) or (rows > 1 and cols and t.stride(0) != ld)):
+            raise ValueError("%s has strides %s, expected (%d, 1)" % (what, tuple(t.stride()), ld))
+    elif t.numel() != rows * cols or not t.is_contiguous() or (ld != cols and rows > 1):
+        raise ValueError("%s has shape %s, expected (%d, %d) with row pitch %d" % (what, tuple(t.shape), rows, cols, ld))
+    return t.data_ptr()
+
+
+def _vec(t, dtypes, n, what, optional=False):
+    if t is None and optional:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous()):
+        raise TypeError("%s must be a contiguous CUDA tensor" % what)
+    if t.dtype not in dtypes:
+        raise TypeError("%s has dtype %s, which is not what the descriptor says" % (what, t.dtype))
+    if t.numel() != n:
+        raise ValueError("%s has %d elements, expected %d" % (what, t.numel(), n))
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is not on the current device" % what)
+    return t.data_ptr()
+
+
+def _blocks(n):
+    return -(-n // 128)
+
+
+def _n_scales(block, rows, cols):
+    return (_blocks(cols) * rows, _blocks(rows) * cols, _blocks(rows) * _blocks(cols))[block]
+
+
+def _scales(t, n, what, kind=DTYPE_E8M0, optional=False):
+    return _vec(t, _TYPES[kind], n, what, optional)
+
+
+def _stream(stream):
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def _pair(pair, dtype, rows, cols, ld, n_scales, what):
+    """(values, scales) of a packed result that may not be wanted."""
+    if pair is None:
+        return None, None
+    q, s = pair
+    return _mat(q, dtype, rows, cols, ld, what), _scales(s, n_scales, "scales of " + what)
+
+
+def empty_packed(rows, cols, dtype=DTYPE_E4M3, device="cuda"):
+    """An 8-bit matrix whose rows start at multiples of 16 bytes, as a [rows][cols] view."""
+    _library()
+    wide = torch.empty(rows, _round16(cols), dtype=torch.uint8, device=device)
+    return wide.view(_TYPES[dtype][0])[:, :cols]
+
+
+def empty_scales(block, rows, cols, device="cuda"):
+    """Scales of a packed [rows][cols] matrix in their layout for `block`."""
+    _library()
+    shape = ((_blocks(cols), rows), (_blocks(rows), cols), (_blocks(rows), _blocks(cols)))[block]
+    return torch.empty(shape, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu)
+
+
+def quant8(desc: Quant8Desc, x, row=None, col=None, tile=None, x_scale=None, stream=None) -> None:
+    """maxdnn_quant8: packs x into the forms asked for; row, col, tile: (values, scales)."""
+    lib = _library()
+    r, c = desc.rows, desc.cols
+    px = _mat(x, desc.x_type, r, c, desc.ldx, "x")
+    ps = _scales(x_scale, _n_scales(BLOCK_ROW, r, c), "x_scale", optional=desc.x_type < DTYPE_E4M3)
+    out = []
+    for block, pair, what in ((BLOCK_ROW, row, "row"), (BLOCK_COL, col, "col"), (BLOCK_TILE, tile, "tile")):
+        out += _pair(pair, desc.q_type, r, c, desc.ldq, _n_scales(block, r, c), what)
+    _raise(lib.maxdnn_quant8(ctypes.byref(desc), px, ps, *out, _stream(stream)), "maxdnn_quant8")
+
+
+def dequant8(desc: Quant8Desc, q, s, x, block=BLOCK_ROW, stream=None) -> None:
+    """maxdnn_dequant8: the values that a packed matrix stands for."""
+    lib = _library()
+    r, c = desc.rows, desc.cols
+    _raise(lib.maxdnn_dequant8(
+        ctypes.byref(desc), block, _mat(q, desc.q_type, r, c, desc.ldq, "q"),
+        _scales(s, _n_scales(block, r, c) if 0 <= block <= 2 else -1, "s"),
+        _mat(x, desc.x_type, r, c, desc.ldx, "x"), _stream(stream)), "maxdnn_dequant8")
+
+
+def _operand(t, s, dtype, major, block, scale_type, mn, k, ld, what):
+    rows, cols = (mn, k) if major == MAJOR_K else (k, mn)
+    p = _mat(t, dtype, rows, cols, ld, what)
+    n = _n_scales(block, rows, cols) if 0 <= block <= 2 else -1
+    return p, _vec(s, _TYPES[scale_type], n, "scales of " + what)
+
+
+def gemm8(desc: Gemm8Desc, a, a_scale, b, b_scale, c, stream=None) -> None:
+    """maxdnn_gemm8: C[m, n] = sum_k a[m, k] b[n, k] of packed matrices."""
+    lib = _library()
+    M, N, K = desc.M, desc.N, desc.K
+    pa, psa = _operand(a, a_scale, desc.a_type, desc.a_major, desc.a_block, desc.a_scale_type, M, K, desc.lda, "a")
+    pb, psb = _operand(b, b_scale, desc.b_type, desc.b_major, desc.b_block, desc.b_scale_type, N, K, desc.ldb, "b")
+    pc = _mat(c, desc.c_type, M, N, desc.ldc, "c")
+    _raise(lib.maxdnn_gemm8(ctypes.byref(desc), pa, psa, pb, psb, pc, _stream(stream)), "maxdnn_gemm8")
+
+
+def layer_norm_fprop(desc: LayerNormDesc, x, gamma=None, beta=None, y=None, mean=None, rstd=None, packed=None,
+                     checkpoint=None, stream=None) -> None:
+    """maxdnn_layer_norm_fprop; packed: (q, s) of y, checkpoint: (c, sc) of x."""
+    lib = _library()
+    r, c = desc.rows, desc.cols
+    f32, w, n = _TYPES[DTYPE_F32], _TYPES[desc.w_type], _n_scales(BLOCK_ROW, r, c)
+    q, s = _pair(packed, desc.q_type, r, c, desc.ldq, n, "packed")
+    k, sk = _pair(checkpoint, desc.q_type, r, c, desc.ldq, n, "checkpoint")
+    _raise(lib.maxdnn_layer_norm_fprop(
+        ctypes.byref(desc), _mat(x, desc.x_type, r, c, desc.ldx, "x"), _vec(gamma, w, c, "gamma", True),
+        _vec(beta, w, c, "beta", True), _mat(y, desc.y_type, r, c, desc.ldy, "y", True),
+        _vec(mean, f32, r, "mean", True), _vec(rstd, f32, r, "rstd", True), q, s, k, sk, _stream(stream)),
+        "maxdnn_layer_norm_fprop")
+
+
+def layer_norm_bprop_workspace(desc: LayerNormDesc) -> int:
+    """Bytes of device scratch maxdnn_layer_norm_bprop needs for dgamma and dbeta."""
+    n = ctypes.c_size_t()
+    _raise(_library().maxdnn_layer_norm_bprop_workspace(ctypes.byref(desc), ctypes.byref(n)),
+           "maxdnn_layer_norm_bprop_workspace")
+    return int(n.value)
+
+
+def layer_norm_bprop(desc: LayerNormDesc, dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, workspace=None,
+                     x_scale=None, stream=None) -> None:
+    """maxdnn_layer_norm_bprop; x: wide, or the checkpoint with its x_scale."""
+    lib = _library()
+    r, c, f32 = desc.rows, desc.cols, _TYPES[DTYPE_F32]
+    if workspace is not None and not (workspace.is_cuda and workspace.is_contiguous()):
+        raise TypeError("workspace must be a contiguous CUDA tensor")
+    _raise(lib.maxdnn_layer_norm_bprop(
+        ctypes.byref(desc), _mat(dy, desc.y_type, r, c, desc.ldy, "dy"), _mat(x, desc.x_type, r, c, desc.ldx, "x"),
+        _scales(x_scale, _n_scales(BLOCK_ROW, r, c), "x_scale", optional=desc.x_type < DTYPE_E4M3),
+        _vec(gamma, _TYPES[desc.w_type], c, "gamma", True), _vec(mean, f32, r, "mean"), _vec(rstd, f32, r, "rstd"),
+        _mat(dx, desc.y_type, r, c, desc.ldy, "dx"), _vec(dgamma, f32, c, "dgamma", True),
+        _vec(dbeta, f32, c, "dbeta", True), None if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)),
+        "maxdnn_layer_norm_bprop")
+
+
+def act8_fprop(desc: Act8Desc, h, a=None, packed=None, checkpoint=None, stream=None) -> None:
+    """maxdnn_act8_fprop; packed: (q, s) of the result, checkpoint: (c, sc) of h."""
+    lib = _library()
+    r, c, many = desc.rows, desc.cols, 1 + desc.gated
+    n = _n_scales(BLOCK_ROW, r, c)
+    q, s = _pair(packed, desc.q_type, r, c, desc.ldq, n, "packed")
+    k, sk = _pair(checkpoint, desc.q_type, r, many * c, desc.ldc, many * n, "checkpoint")
+    _raise(lib.maxdnn_act8_fprop(
+        ctypes.byref(desc), _mat(h, desc.x_type, r, many * c, desc.ldh, "h"),
+        _mat(a, desc.x_type, r, c, desc.lda, "a", True), q, s, k, sk, _stream(stream)), "maxdnn_act8_fprop")
+
+
+def act8_bprop(desc: Act8Desc, da, h, dh, h_scale=None, stream=None) -> None:
+    """maxdnn_act8_bprop; h: wide, or the checkpoint with its h_scale."""
+    lib = _library()
+    r, c, many = desc.rows, desc.cols, 1 + desc.gated
+    packed = desc.h_type >= DTYPE_E4M3
+    _raise(lib.maxdnn_act8_bprop(
+        ctypes.byref(desc), _mat(da, desc.x_type, r, c, desc.lda, "da"),
+        _mat(h, desc.h_type, r, many * c, desc.ldc if packed else desc.ldh, "h"),
+        _scales(h_scale, many * _n_scales(BLOCK_ROW, r, c), "h_scale", optional=not packed),
+        _mat(dh, desc.x_type, r, many * c, desc.ldh, "dh"), _stream(stream)), "maxdnn_act8_bprop")
