@@ -604,8 +604,9 @@ maxdnn_status maxdnn_last_kernel_clock(uint32_t* sm_cycles, uint32_t* nanosecond
  * the model says), UMMA_KC, UMMA_PAIR (1 two-SM / -1 one-SM tiles), UMMA_MERGE, UMMA_STAGE_KB, UMMA_COLS, WGRAD_SPLITS, WGRAD_PAIR, SM_COUNT (SM
  * count for host-only workspace queries), X3_CHUNK_ROWS, DEBUG_STATUS, KERNEL_CLOCK (see
  * maxdnn_last_kernel_clock), RAGGED_PADDED (see maxdnn_conv_fprop_ragged), GEMM8_COLS,
- * GEMM8_SPLIT, GEMM8_SWAP (pin maxdnn_gemm8's tile columns 16/32/64/128/256, the CTAs that share
- * a tile's reduction 1/2/4/8, and whether the roles of A and B are exchanged), and
+ * GEMM8_SPLIT, GEMM8_SWAP, GEMM8_PAIR (pin maxdnn_gemm8's tile columns 16/32/64/128/192/224/256,
+ * the CTAs that share a tile's reduction 1/2/4/8, whether the roles of A and B are exchanged, and
+ * 1 two-SM / -1 one-SM tiles; NOT_SUPPORTED where no kernel has that combination), and
  * TEST_MISSING_ARRIVAL (test hook: CTA 0's "full" barriers expect an arrival that
  * never comes, so a bounded wait runs out).  The environment variable MAXDNN_<name>
  * gives an option its initial value; the environment is read once, at the first use of

@@ -85,19 +85,19 @@ __device__ __forceinline__ float gemm8_scale(const Gemm8Scale& s, int i, int kb)
                     : e8m0_value(__ldg(static_cast<const uint8_t*>(s.p) + at));
 }
 
-__device__ __forceinline__ void gemm8_store1(const Gemm8Args& args, int64_t at, float v) {
-  if (args.c_type == MAXDNN_F32) static_cast<float*>(args.c)[at] = v;
-  else if (args.c_type == MAXDNN_BF16) static_cast<__nv_bfloat16*>(args.c)[at] = __float2bfloat16_rn(v);
-  else static_cast<__half*>(args.c)[at] = __float2half_rn(v);
+__device__ __forceinline__ void gemm8_store1(void* c, int c_type, int64_t at, float v) {
+  if (c_type == MAXDNN_F32) static_cast<float*>(c)[at] = v;
+  else if (c_type == MAXDNN_BF16) static_cast<__nv_bfloat16*>(c)[at] = __float2bfloat16_rn(v);
+  else static_cast<__half*>(c)[at] = __float2half_rn(v);
 }
 
 // The tile (row tile, column tile) of index t: tiles that run at the same time share operand
 // rows and columns (groups of eight row tiles, walked column by column).
-__device__ __forceinline__ void gemm8_tile(const Gemm8Args& args, int t, int* mt, int* nt) {
-  const int per_group = 8 * args.n_tiles;
+__device__ __forceinline__ void gemm8_tile(int m_tiles, int n_tiles, int t, int* mt, int* nt) {
+  const int per_group = 8 * n_tiles;
   const int group = t / per_group;
   const int first = group * 8;
-  const int height = min(8, args.m_tiles - first);
+  const int height = min(8, m_tiles - first);
   const int in = t - group * per_group;
   *mt = first + in % height;
   *nt = in / height;
@@ -172,7 +172,7 @@ gemm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     bool ok = true;
     for (int tile = unit; tile < n_tiles && ok; tile += n_units) {
       int mt, nt;
-      gemm8_tile(args, tile, &mt, &nt);
+      gemm8_tile(args.m_tiles, args.n_tiles, tile, &mt, &nt);
       const int m0 = mt * kGemm8TileM, n0 = nt * NT;
       for (int kb = kb0; kb < kb1; ++kb) {
         if (!mbar_wait(empty_bar + 8u * stage, phase ^ 1u, args.wc, kDevTimeoutEmpty)) {
@@ -252,7 +252,7 @@ gemm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     bool ok = true;
     for (int tile = unit; tile < n_tiles && ok; tile += n_units) {
       int mt, nt;
-      gemm8_tile(args, tile, &mt, &nt);
+      gemm8_tile(args.m_tiles, args.n_tiles, tile, &mt, &nt);
       const int m = mt * kGemm8TileM + q * 32 + lane;
       const int n0 = nt * NT + part * CW;
       float tot[CW];
@@ -323,7 +323,7 @@ gemm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
           } else {
 #pragma unroll
             for (int i = 0; i < CW; ++i)
-              if (n0 + i < args.N) gemm8_store1(args, at + (int64_t)(n0 + i) * args.c_col, tot[i]);
+              if (n0 + i < args.N) gemm8_store1(args.c, args.c_type, at + (int64_t)(n0 + i) * args.c_col, tot[i]);
           }
         }
       } else {
@@ -344,7 +344,7 @@ gemm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     cluster_wait();
     const int cols = NT / split;
     int mt, nt;
-    gemm8_tile(args, unit, &mt, &nt);
+    gemm8_tile(args.m_tiles, args.n_tiles, unit, &mt, &nt);
     constexpr int kThreads = gemm8_threads(NT);
     for (int e = threadIdx.x; e < cols * kGemm8TileM; e += kThreads) {
       const int row = e & (kGemm8TileM - 1), col = rank * cols + (e >> 7);
@@ -352,7 +352,7 @@ gemm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
       float v = 0.f;
       for (int r = 0; r < split; ++r) v += ld_cluster_f32(map_to_cta(off, (uint32_t)r));
       const int m = mt * kGemm8TileM + row, n = nt * NT + col;
-      if (m < args.M && n < args.N) gemm8_store1(args, (int64_t)m * args.c_row + (int64_t)n * args.c_col, v);
+      if (m < args.M && n < args.N) gemm8_store1(args.c, args.c_type, (int64_t)m * args.c_row + (int64_t)n * args.c_col, v);
     }
     cluster_arrive();
     cluster_wait();

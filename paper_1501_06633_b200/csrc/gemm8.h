@@ -12,8 +12,12 @@ constexpr int kGemm8BlockK = 128;    // reduction steps per stage: one scale blo
 constexpr int kGemm8MaxSplit = 8;    // CTAs of a cluster that share one tile's reduction
 
 struct Gemm8Plan {
+  int32_t mx;          // 1: the tensor core applies the scales (both operands' are E8M0 bytes)
+  int32_t pair;        // 1: tiles of 256 rows on two SMs
   int32_t swap;        // 1: the kernel's rows are the columns of C (few rows of C)
-  int32_t tile_n;      // columns of a tile: 16, 32, 64, 128 or 256
+  int32_t tile_n;      // columns of a tile
+  int32_t chunk;       // mx: blocks of the reduction per accumulator
+  int32_t bulk_c;      // mx: C is stored by bulk tensor copies
   int32_t split;       // CTAs that share a tile's reduction: 1, 2, 4 or 8
   int32_t m_tiles, n_tiles, k_blocks;
   int32_t stages;

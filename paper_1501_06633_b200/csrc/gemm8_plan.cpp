@@ -38,50 +38,76 @@ maxdnn_status check_gemm8(const maxdnn_gemm8_desc* d) {
   return MAXDNN_OK;
 }
 
+// One candidate of the search below.
+struct Shape { int mx, pair, nt; };
+
 maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* plan) {
-  static const int kTileN[5] = {16, 32, 64, 128, 256};
+  static const Shape kShapes[] = {{1, 0, 16}, {1, 0, 32}, {1, 0, 64}, {1, 0, 128},
+                                  {1, 1, 128}, {1, 1, 192}, {1, 1, 224}, {1, 1, 256},
+                                  {0, 0, 16}, {0, 0, 32}, {0, 0, 64}, {0, 0, 128}, {0, 0, 256}};
   static const int kSplit[4] = {1, 2, 4, 8};
   const int k_blocks = (d.K + kGemm8BlockK - 1) / kGemm8BlockK;
+  const int mx = d.a_scale_type == MAXDNN_E8M0 && d.b_scale_type == MAXDNN_E8M0;
+  const int c_bytes = d.c_type == MAXDNN_F32 ? 4 : 2;
   double best = 0;
   bool found = false;
   for (int swap = 0; swap < 2; ++swap) {
     if (option_is_set(OPT_GEMM8_SWAP) && option(OPT_GEMM8_SWAP) != swap) continue;
     const int64_t M = swap ? d.N : d.M, N = swap ? d.M : d.N;
     const int b_major = swap ? d.a_major : d.b_major;
-    for (int nt : kTileN) {
-      if (option_is_set(OPT_GEMM8_COLS) && option(OPT_GEMM8_COLS) != nt) continue;
-      const int64_t m_tiles = (M + kGemm8TileM - 1) / kGemm8TileM, n_tiles = (N + nt - 1) / nt;
+    for (const Shape& s : kShapes) {
+      if (s.mx != mx) continue;
+      if (option_is_set(OPT_GEMM8_COLS) && option(OPT_GEMM8_COLS) != s.nt) continue;
+      if (option_is_set(OPT_GEMM8_PAIR) && (option(OPT_GEMM8_PAIR) > 0) != (s.pair != 0)) continue;
+      const int tile_m = s.pair ? 2 * kGemm8TileM : kGemm8TileM, rows_b = s.pair ? s.nt / 2 : s.nt;
+      const int64_t m_tiles = (M + tile_m - 1) / tile_m, n_tiles = (N + s.nt - 1) / s.nt;
       const int64_t tiles = m_tiles * n_tiles;
-      const int b_stage = b_major == MAXDNN_MAJOR_MN ? std::max(nt, 128) * 128 : nt * 128;
-      // clocks of one block: MMAs, reading and adding the product, filling the stage
-      const double mma = 2.0 * nt, add = 100.0 + 1.2 * nt, fill = (16384 + b_stage) / 48.0;
-      const double per_block = std::max(mma, std::max(add, fill));
+      const int b_stage = b_major == MAXDNN_MAJOR_MN ? std::max(rows_b, 128) * 128 : rows_b * 128;
+      const int slots = s.pair ? sm_count / 2 : sm_count;        // tiles that run side by side
+      // an fp32 result is added up from accumulators of four blocks (gemm8_mx.cuh)
+      const int chunk = mx ? (d.c_type == MAXDNN_F32 ? 4 : std::max(k_blocks, 1)) : 1;
+      // clocks of one block: its MMAs, filling its stage, reading and adding the product
+      const double mma = 2.0 * s.nt, fill = (16384 + b_stage) / 56.0, add = mx ? 0.0 : 100.0 + 4.0 * s.nt;
+      double per_block = std::max(mma, std::max(add, fill)) + 20.0;
+      if (mx && s.nt > 224) per_block += 500.0 / chunk;          // its one accumulator is emptied in between
       for (int split : kSplit) {
         if (option_is_set(OPT_GEMM8_SPLIT) && option(OPT_GEMM8_SPLIT) != split) continue;
-        if (split > k_blocks) continue;
+        if (split > k_blocks || (split > 1 && s.pair)) continue;
         if (split > 1 && tiles * split > 2 * sm_count && !option_is_set(OPT_GEMM8_SPLIT)) continue;
-        const int64_t units = split == 1 ? std::min<int64_t>(tiles, sm_count) : tiles;
-        const int64_t waves = split == 1 ? (tiles + sm_count - 1) / sm_count : (tiles * split + sm_count - 1) / sm_count;
+        const int64_t units = split == 1 ? std::min<int64_t>(tiles, slots) : tiles;
+        const int64_t waves = (tiles * split + slots - 1) / slots;
         const int64_t blocks = (k_blocks + split - 1) / split;
-        const double t = (double)waves * ((double)blocks * per_block + 1500.0) + (split > 1 ? 1500.0 + 4.0 * nt : 0.0);
+        const double t = (double)waves * ((double)blocks * per_block + 800.0) + 1500.0 + (split > 1 ? 1500.0 + 4.0 * s.nt : 0.0);
         if (found && t >= best) continue;
         found = true;
         best = t;
+        plan->mx = mx;
+        plan->pair = s.pair;
         plan->swap = swap;
-        plan->tile_n = nt;
+        plan->tile_n = s.nt;
+        plan->chunk = chunk;
         plan->split = split;
         plan->m_tiles = (int32_t)m_tiles;
         plan->n_tiles = (int32_t)n_tiles;
         plan->k_blocks = k_blocks;
         plan->b_stage_bytes = b_stage;
-        plan->grid = (int32_t)(units * split);
+        plan->grid = (int32_t)(units * (s.pair ? 2 : split));
+        // bulk copies of 32 rows x 32 columns: rows of C contiguous, starting and ending at
+        // multiples of 16 bytes (a copy that is cut at the tensor's edge writes whole 16 bytes)
+        plan->bulk_c = mx && !swap && split == 1 && s.nt >= 32 && (d.ldc * c_bytes) % 16 == 0 &&
+                       ((int64_t)d.N * c_bytes) % 16 == 0;
       }
     }
   }
   if (!found) return MAXDNN_NOT_SUPPORTED;
   if ((int64_t)plan->m_tiles * plan->n_tiles > (1 << 30)) return MAXDNN_NOT_SUPPORTED;
-  const int warps = 4 * (plan->tile_n < 64 ? 1 : plan->tile_n / 64), cw = std::min(plan->tile_n, 64);
-  const int fixed = 1024 + 64 + warps * 2 * cw * 4;
+  int fixed = 1024 + 128;
+  if (plan->mx) {
+    fixed += (plan->bulk_c ? 8 * 4096 : 0) + 2 * 128 * (4 + 4 * ((plan->tile_n + 127) / 128));
+  } else {
+    const int warps = 4 * (plan->tile_n < 64 ? 1 : plan->tile_n / 64), cw = std::min(plan->tile_n, 64);
+    fixed += warps * 2 * cw * 4;
+  }
   const int per_stage = 16384 + plan->b_stage_bytes + 16;
   plan->stages = std::min(12, (232448 - fixed) / per_stage);
   plan->smem_bytes = fixed + plan->stages * per_stage;

@@ -20,7 +20,7 @@ enum OptionId : int {
   OPT_FFMA_TILE_M = 0, OPT_FFMA_COLS, OPT_FFMA_KH, OPT_FFMA_KC, OPT_FFMA_STREAMK,
   OPT_UMMA_KC, OPT_UMMA_PAIR, OPT_UMMA_MERGE, OPT_UMMA_STAGE_KB, OPT_UMMA_COLS,
   OPT_WGRAD_SPLITS, OPT_WGRAD_PAIR, OPT_SM_COUNT, OPT_X3_CHUNK_ROWS, OPT_DEBUG_STATUS,
-  OPT_KERNEL_CLOCK, OPT_RAGGED_PADDED, OPT_GEMM8_COLS, OPT_GEMM8_SPLIT, OPT_GEMM8_SWAP,
+  OPT_KERNEL_CLOCK, OPT_RAGGED_PADDED, OPT_GEMM8_COLS, OPT_GEMM8_SPLIT, OPT_GEMM8_SWAP, OPT_GEMM8_PAIR,
   OPT_TEST_MISSING_ARRIVAL, OPT_COUNT
 };
 bool option_is_set(OptionId id);

@@ -24,6 +24,7 @@ ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(3)
 
 _vp = ctypes.c_void_p
 torch = None      # imported with the library, at the first call
+_current_device = _current_raw_stream = None
 _TYPES = ()       # the tensor types of each DTYPE_* code
 
 
@@ -100,11 +101,21 @@ class Act8Desc(ctypes.Structure):
 _lib = None
 
 
+def _raw_stream(device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
 def _library():
-    global _lib, torch, _TYPES
+    global _lib, torch, _TYPES, _current_device, _current_raw_stream
     if _lib is None:
         lib = load_library()
         import torch
+        # what torch.cuda.current_device() and current_stream().cuda_stream return, without the
+        # objects around them: a small layer's call is bound by the host
+        _current_device, _current_raw_stream = torch.cuda.current_device, _raw_stream
+        if hasattr(torch._C, "_cuda_getDevice") and hasattr(torch._C, "_cuda_getCurrentRawStream"):
+            torch.cuda.init()
+            _current_device, _current_raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
         _TYPES = ((torch.float32,), (torch.bfloat16,), (torch.float16,),
                   (torch.float8_e4m3fn, torch.uint8), (torch.float8_e5m2, torch.uint8),
                   (torch.float8_e8m0fnu, torch.uint8))
@@ -129,19 +140,18 @@ def _raise(status, where):
         raise MaxdnnError(status, where)
 
 
-def _mat(t, dtype, rows, cols, ld, what, optional=False):
+def _mat(t, dtype, rows, cols, ld, what):
     """Address of a [rows][cols] matrix with row pitch ld: a 2-d view with these strides, or any
     contiguous tensor of rows x cols elements where ld = cols."""
-    if t is None:
-        if optional:
-            return None
-        raise TypeError("%s must be a CUDA tensor" % what)
-    if not (isinstance(t, torch.Tensor) and t.is_cuda):
-        raise TypeError("%s must be a CUDA tensor" % what)
+    try:
+        if (t.shape == (rows, cols) and t.stride() == (ld, 1) and t.dtype in _TYPES[dtype]
+                and t.get_device() == _current_device()):
+            return t.data_ptr()
+    except (AttributeError, IndexError):
+        pass
+    _on_device(t, what)
     if not 0 <= dtype < len(_TYPES) or t.dtype not in _TYPES[dtype]:
         raise TypeError("%s has dtype %s, which is not what the descriptor says" % (what, t.dtype))
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError("%s is not on the current device" % what)
     if t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols:
         if rows and ((cols > 1 and t.stride(1) != 1) or (rows > 1 and cols and t.stride(0) != ld)):
             raise ValueError("%s has strides %s, expected (%d, 1)" % (what, tuple(t.stride()), ld))
@@ -150,17 +160,20 @@ def _mat(t, dtype, rows, cols, ld, what, optional=False):
     return t.data_ptr()
 
 
-def _vec(t, dtypes, n, what, optional=False):
-    if t is None and optional:
-        return None
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous()):
-        raise TypeError("%s must be a contiguous CUDA tensor" % what)
+def _on_device(t, what):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise TypeError("%s must be a CUDA tensor" % what)
+    if t.get_device() != _current_device():
+        raise ValueError("%s is not on the current device" % what)
+
+
+def _vec(t, dtypes, n, what):
+    """Address of a contiguous tensor of n elements."""
+    _on_device(t, what)
     if t.dtype not in dtypes:
         raise TypeError("%s has dtype %s, which is not what the descriptor says" % (what, t.dtype))
-    if t.numel() != n:
-        raise ValueError("%s has %d elements, expected %d" % (what, t.numel(), n))
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError("%s is not on the current device" % what)
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s has shape %s, expected %d contiguous elements" % (what, tuple(t.shape), n))
     return t.data_ptr()
 
 
@@ -172,12 +185,12 @@ def _n_scales(block, rows, cols):
     return (_blocks(cols) * rows, _blocks(rows) * cols, _blocks(rows) * _blocks(cols))[block]
 
 
-def _scales(t, n, what, kind=DTYPE_E8M0, optional=False):
-    return _vec(t, _TYPES[kind], n, what, optional)
+def _scales(t, n, what):
+    return _vec(t, _TYPES[DTYPE_E8M0], n, what)
 
 
 def _stream(stream):
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+    return _current_raw_stream(_current_device()) if stream is None else stream.cuda_stream
 
 
 def _pair(pair, dtype, rows, cols, ld, n_scales, what):
@@ -207,7 +220,7 @@ def quant8(desc: Quant8Desc, x, row=None, col=None, tile=None, x_scale=None, str
     lib = _library()
     r, c = desc.rows, desc.cols
     px = _mat(x, desc.x_type, r, c, desc.ldx, "x")
-    ps = _scales(x_scale, _n_scales(BLOCK_ROW, r, c), "x_scale", optional=desc.x_type < DTYPE_E4M3)
+    ps = None if desc.x_type < DTYPE_E4M3 else _scales(x_scale, _n_scales(BLOCK_ROW, r, c), "x_scale")
     out = []
     for block, pair, what in ((BLOCK_ROW, row, "row"), (BLOCK_COL, col, "col"), (BLOCK_TILE, tile, "tile")):
         out += _pair(pair, desc.q_type, r, c, desc.ldq, _n_scales(block, r, c), what)
@@ -250,9 +263,9 @@ def layer_norm_fprop(desc: LayerNormDesc, x, gamma=None, beta=None, y=None, mean
     q, s = _pair(packed, desc.q_type, r, c, desc.ldq, n, "packed")
     k, sk = _pair(checkpoint, desc.q_type, r, c, desc.ldq, n, "checkpoint")
     _raise(lib.maxdnn_layer_norm_fprop(
-        ctypes.byref(desc), _mat(x, desc.x_type, r, c, desc.ldx, "x"), _vec(gamma, w, c, "gamma", True),
-        _vec(beta, w, c, "beta", True), _mat(y, desc.y_type, r, c, desc.ldy, "y", True),
-        _vec(mean, f32, r, "mean", True), _vec(rstd, f32, r, "rstd", True), q, s, k, sk, _stream(stream)),
+        ctypes.byref(desc), _mat(x, desc.x_type, r, c, desc.ldx, "x"), None if gamma is None else _vec(gamma, w, c, "gamma"),
+        None if beta is None else _vec(beta, w, c, "beta"), None if y is None else _mat(y, desc.y_type, r, c, desc.ldy, "y"),
+        None if mean is None else _vec(mean, f32, r, "mean"), None if rstd is None else _vec(rstd, f32, r, "rstd"), q, s, k, sk, _stream(stream)),
         "maxdnn_layer_norm_fprop")
 
 
@@ -269,14 +282,16 @@ def layer_norm_bprop(desc: LayerNormDesc, dy, x, gamma, mean, rstd, dx, dgamma=N
     """maxdnn_layer_norm_bprop; x: wide, or the checkpoint with its x_scale."""
     lib = _library()
     r, c, f32 = desc.rows, desc.cols, _TYPES[DTYPE_F32]
-    if workspace is not None and not (workspace.is_cuda and workspace.is_contiguous()):
-        raise TypeError("workspace must be a contiguous CUDA tensor")
+    if workspace is not None:
+        _on_device(workspace, "workspace")
+        if not workspace.is_contiguous():
+            raise TypeError("workspace must be a contiguous CUDA tensor")
     _raise(lib.maxdnn_layer_norm_bprop(
         ctypes.byref(desc), _mat(dy, desc.y_type, r, c, desc.ldy, "dy"), _mat(x, desc.x_type, r, c, desc.ldx, "x"),
-        _scales(x_scale, _n_scales(BLOCK_ROW, r, c), "x_scale", optional=desc.x_type < DTYPE_E4M3),
-        _vec(gamma, _TYPES[desc.w_type], c, "gamma", True), _vec(mean, f32, r, "mean"), _vec(rstd, f32, r, "rstd"),
-        _mat(dx, desc.y_type, r, c, desc.ldy, "dx"), _vec(dgamma, f32, c, "dgamma", True),
-        _vec(dbeta, f32, c, "dbeta", True), None if workspace is None else workspace.data_ptr(),
+        None if desc.x_type < DTYPE_E4M3 else _scales(x_scale, _n_scales(BLOCK_ROW, r, c), "x_scale"),
+        None if gamma is None else _vec(gamma, _TYPES[desc.w_type], c, "gamma"), _vec(mean, f32, r, "mean"), _vec(rstd, f32, r, "rstd"),
+        _mat(dx, desc.y_type, r, c, desc.ldy, "dx"), None if dgamma is None else _vec(dgamma, f32, c, "dgamma"),
+        None if dbeta is None else _vec(dbeta, f32, c, "dbeta"), None if workspace is None else workspace.data_ptr(),
         0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)),
         "maxdnn_layer_norm_bprop")
 
@@ -290,7 +305,7 @@ def act8_fprop(desc: Act8Desc, h, a=None, packed=None, checkpoint=None, stream=N
     k, sk = _pair(checkpoint, desc.q_type, r, many * c, desc.ldc, many * n, "checkpoint")
     _raise(lib.maxdnn_act8_fprop(
         ctypes.byref(desc), _mat(h, desc.x_type, r, many * c, desc.ldh, "h"),
-        _mat(a, desc.x_type, r, c, desc.lda, "a", True), q, s, k, sk, _stream(stream)), "maxdnn_act8_fprop")
+        None if a is None else _mat(a, desc.x_type, r, c, desc.lda, "a"), q, s, k, sk, _stream(stream)), "maxdnn_act8_fprop")
 
 
 def act8_bprop(desc: Act8Desc, da, h, dh, h_scale=None, stream=None) -> None:
@@ -301,5 +316,5 @@ def act8_bprop(desc: Act8Desc, da, h, dh, h_scale=None, stream=None) -> None:
     _raise(lib.maxdnn_act8_bprop(
         ctypes.byref(desc), _mat(da, desc.x_type, r, c, desc.lda, "da"),
         _mat(h, desc.h_type, r, many * c, desc.ldc if packed else desc.ldh, "h"),
-        _scales(h_scale, many * _n_scales(BLOCK_ROW, r, c), "h_scale", optional=not packed),
+        _scales(h_scale, many * _n_scales(BLOCK_ROW, r, c), "h_scale") if packed else None,
         _mat(dh, desc.x_type, r, many * c, desc.ldh, "dh"), _stream(stream)), "maxdnn_act8_bprop")

@@ -38,8 +38,10 @@ def down(t):
 
 
 def packed_up(q, s, kind):
-    """A packed operand from values and scale bytes (pitch: the next multiple of 16)."""
-    t = mx.empty_packed(q.shape[0], q.shape[1], PACKED[kind][0])
+    """A packed operand from values and scale bytes (pitch: the next multiple of 16; its gaps hold
+    NaN, which nothing may read)."""
+    wide = torch.full((q.shape[0], -(-q.shape[1] // 16) * 16), 0x7F, dtype=torch.uint8, device="cuda")
+    t = wide.view(PACKED[kind][1])[:, :q.shape[1]]
     bits = torch.from_numpy(q.astype(np.float32)).to(PACKED[kind][1]).view(torch.uint8)
     t.view(torch.uint8)[:] = bits.cuda()
     return t, torch.from_numpy(s).cuda().view(torch.float8_e8m0fnu)
@@ -219,11 +221,33 @@ def test_gemm_sizes_and_majors(way, M, N, K):
 @pytest.mark.parametrize("split", [1, 2, 8])
 @pytest.mark.parametrize("swap", [0, 1])
 @pytest.mark.parametrize("way", ["fprop", "wgrad"])
-def test_gemm_every_plan(cols, split, swap, way):
+def test_gemm_every_plan_with_fp32_scales(cols, split, swap, way):
     mx.set_option("GEMM8_COLS", cols)
     mx.set_option("GEMM8_SPLIT", split)
     mx.set_option("GEMM8_SWAP", swap)
-    run_gemm(150, 330, 1100, *WAYS[way], ct="bf16", seed=cols + split)
+    run_gemm(150, 330, 1100, *WAYS[way], ct="bf16", seed=cols + split, f32_scales="ab")
+
+
+@pytest.mark.parametrize("pair,cols,split", [(-1, c, s) for c in (16, 32, 64, 128) for s in (1, 2, 4, 8)] +
+                         [(1, c, 1) for c in (128, 192, 224, 256)])
+@pytest.mark.parametrize("swap", [0, 1])
+@pytest.mark.parametrize("way", ["fprop", "dgrad", "wgrad"])
+@pytest.mark.parametrize("ct,ldc", [("bf16", 336), ("f32", 336), ("f16", 331)])
+def test_gemm_every_plan(pair, cols, split, swap, way, ct, ldc):
+    mx.set_option("GEMM8_PAIR", pair)
+    mx.set_option("GEMM8_COLS", cols)
+    mx.set_option("GEMM8_SPLIT", split)
+    mx.set_option("GEMM8_SWAP", swap)
+    run_gemm(150, 330, 1100, *WAYS[way], ct=ct, ldc=ldc, seed=cols + split)
+
+
+@pytest.mark.parametrize("pair,cols", [(-1, 128), (1, 128), (1, 192), (1, 224), (1, 256)])
+def test_gemm_many_tiles_and_chunks(pair, cols):
+    """More tiles than SMs, several accumulator chunks: every buffer and barrier goes around."""
+    mx.set_option("GEMM8_PAIR", pair)
+    mx.set_option("GEMM8_COLS", cols)
+    run_gemm(2300, 5000, 1700, *WAYS["fprop"], seed=cols)
+    run_gemm(2300, 5000, 700, *WAYS["wgrad"], ct="bf16", seed=cols)
 
 
 @pytest.mark.parametrize("at,bt", [("e4m3", "e5m2"), ("e5m2", "e4m3"), ("e5m2", "e5m2")])
