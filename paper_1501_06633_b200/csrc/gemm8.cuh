@@ -32,6 +32,7 @@ struct Gemm8Scale {
   int32_t shift;       // 0: one per row; 7: one per 128 rows
   int32_t is_float;    // 0: E8M0 bytes
   int32_t count;       // rows
+  int32_t words;       // bytes of four neighbouring rows can be read as a word
 };
 
 struct Gemm8Args {

@@ -32,13 +32,14 @@ namespace maxdnn {
 
 constexpr int kMxThreads = 384;
 constexpr int kMxEpiWarps = 8;
+constexpr int kMxScaleBufs = 4;      // scale groups (four blocks each) between the gathering warp and the MMAs
 
 __host__ __device__ constexpr int mx_buffers(int nt) { return nt <= 224 ? 2 : 1; }
 __host__ __device__ constexpr int mx_units(int nt) { return (nt + 63) / 64; }           // 32 columns each, per warp
 __host__ __device__ constexpr int mx_sf_cols(int nt) { return 4 + 4 * ((nt + 127) / 128); }
 __host__ __device__ constexpr int mx_sf_bytes(int nt) { return 128 * mx_sf_cols(nt); }
 __host__ __device__ constexpr int mx_tmem_cols(int nt) {
-  const int need = mx_buffers(nt) * nt + 2 * mx_sf_cols(nt);
+  const int need = mx_buffers(nt) * nt + kMxScaleBufs * mx_sf_cols(nt);
   return need <= 64 ? 64 : need <= 128 ? 128 : need <= 256 ? 256 : 512;
 }
 
@@ -103,13 +104,44 @@ __device__ __forceinline__ void tma_store_2d_hint(const CUtensorMap* m, uint32_t
       : "memory");
 }
 
-// The scale bytes of row i in blocks kb .. kb + 3 (clamped to the last block), as one word.
-__device__ __forceinline__ uint32_t mx_scale_word(const Gemm8Scale& s, int i, int kb, int last) {
-  const uint8_t* p = static_cast<const uint8_t*>(s.p) + (int64_t)(min(i, s.count - 1) >> s.shift) * s.step;
-  uint32_t w = 0;
+// The scale bytes of rows row0 + 4 lane .. + 3 in each of the blocks kb .. kb + 3 (clamped to the
+// last row and block): one word per block.
+__device__ __forceinline__ void mx_load_scales(const Gemm8Scale& s, int row0, int lane, int kb, int last,
+                                               uint32_t (&raw)[4]) {
+  const uint8_t* p = static_cast<const uint8_t*>(s.p);
+  const int r = row0 + 4 * lane;
+  if (s.shift) {    // row0 is a multiple of 16: the four rows have one scale
+    p += (int64_t)(min(r, s.count - 1) >> s.shift) * s.step;
 #pragma unroll
-  for (int b = 0; b < 4; ++b) w |= (uint32_t)__ldg(p + (int64_t)min(kb + b, last) * s.kstep) << (8 * b);
-  return w;
+    for (int b = 0; b < 4; ++b) raw[b] = 0x01010101u * __ldg(p + (int64_t)min(kb + b, last) * s.kstep);
+  } else {
+    if (s.words && r + 3 < s.count) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        raw[b] = __ldg(reinterpret_cast<const uint32_t*>(p + (int64_t)min(kb + b, last) * s.kstep + r));
+    } else {
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const uint8_t* q = p + (int64_t)min(kb + b, last) * s.kstep;
+        raw[b] = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[b] |= (uint32_t)__ldg(q + min(r + i, s.count - 1)) << (8 * i);
+      }
+    }
+  }
+}
+
+// Those bytes as the tensor-memory copy wants them: row r's four block bytes in word r / 32 of the
+// 16-byte line r mod 32.
+__device__ __forceinline__ void mx_store_scales(uint8_t* dst, int lane, const uint32_t (&raw)[4]) {
+  // transpose of 4 x 4 bytes
+  const uint32_t a = __byte_perm(raw[0], raw[1], 0x5140), b = __byte_perm(raw[0], raw[1], 0x7362);
+  const uint32_t c = __byte_perm(raw[2], raw[3], 0x5140), d = __byte_perm(raw[2], raw[3], 0x7362);
+  const uint32_t w[4] = {__byte_perm(a, c, 0x5410), __byte_perm(a, c, 0x7632), __byte_perm(b, d, 0x5410),
+                         __byte_perm(b, d, 0x7632)};
+  uint8_t* p = dst + ((4 * lane) & 31) * 16 + (lane >> 3) * 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(p + 16 * i) = w[i];
 }
 
 template <int NT, bool PAIR>
@@ -129,13 +161,14 @@ gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   const int stages = args.stages;
   const uint32_t b_off = (uint32_t)stages * kAStage;
   const uint32_t st_off = b_off + (uint32_t)stages * (uint32_t)args.b_stage_bytes;
-  const uint32_t sf_off = st_off + (args.bulk_c ? kMxEpiWarps * (uint32_t)kStageTileBytes : 0u);
-  const uint32_t bar_off = sf_off + 2u * kSfBytes;
+  const uint32_t stg_bytes = args.c_type == MAXDNN_F32 ? 4096u : 2048u;   // 32 rows x 32 columns
+  const uint32_t sf_off = st_off + (args.bulk_c ? kMxEpiWarps * stg_bytes : 0u);
+  const uint32_t bar_off = sf_off + kMxScaleBufs * kSfBytes;
   const uint32_t full_bar = base + bar_off;
   const uint32_t empty_bar = full_bar + 8u * stages;
-  const uint32_t sff_bar = empty_bar + 8u * stages;    // 2: scales of a group are in shared memory
-  const uint32_t sfe_bar = sff_bar + 16u;              // 2: and no longer needed
-  const uint32_t accf_bar = sfe_bar + 16u;             // 2
+  const uint32_t sff_bar = empty_bar + 8u * stages;    // scales of a group are in shared memory
+  const uint32_t sfe_bar = sff_bar + 8u * kMxScaleBufs;    // and no longer needed
+  const uint32_t accf_bar = sfe_bar + 8u * kMxScaleBufs;   // 2
   const uint32_t acce_bar = accf_bar + 16u;            // 2
   const uint32_t done_bar = acce_bar + 16u;
   const uint32_t tmem_slot = done_bar + 8u;
@@ -158,9 +191,11 @@ gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       mbar_init(full_bar + 8u * s, 2 + extra);          // the (leader's) two copy warps
       mbar_init(empty_bar + 8u * s, 1);
     }
-    for (int a = 0; a < 2; ++a) {
+    for (int a = 0; a < kMxScaleBufs; ++a) {
       mbar_init(sff_bar + 8u * a, PAIR ? 2 : 1);
       mbar_init(sfe_bar + 8u * a, 1);
+    }
+    for (int a = 0; a < 2; ++a) {
       mbar_init(accf_bar + 8u * a, 1);
       mbar_init(acce_bar + 8u * a, kMxEpiWarps * (PAIR ? 2 : 1));
     }
@@ -231,41 +266,55 @@ gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     }
   } else if (warp == 2) {
     // ------------------------------------------------------------ scales
+    // Three groups' loads are in flight: a group's MMAs last about as long as one load.
+    constexpr int kSides = kSfCols / 4;          // 128 rows of A, then of B's columns
     const uint32_t report = PAIR ? map_to_cta(sff_bar, 0) : sff_bar;
-    uint32_t group = 0;
-    bool ok = true;
-    for (int tile = unit; tile < n_tiles && ok; tile += n_units) {
-      int mt, nt;
-      gemm8_tile(args.m_tiles, args.n_tiles, tile, &mt, &nt);
-      const int m0 = mt * tile_m + (PAIR ? rank * kGemm8TileM : 0), n0 = nt * NT;
-      for (int kb = kb0; kb < kb1; kb += 4, ++group) {
-        uint32_t w[kSfCols];
-        if (args.sa.shift) {
-          w[0] = mx_scale_word(args.sa, m0, kb, kb1 - 1);
-          w[1] = w[2] = w[3] = w[0];
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) w[j] = mx_scale_word(args.sa, m0 + 32 * j + lane, kb, kb1 - 1);
-        }
-#pragma unroll
-        for (int j = 0; j < kSfCols - 4; ++j)
-          w[4 + j] = 32 * j < NT ? mx_scale_word(args.sb, n0 + 32 * j + lane, kb, kb1 - 1) : 0u;
-        const uint32_t buf = group & 1u;
-        if (!mbar_wait(sfe_bar + 8u * buf, ((group >> 1) & 1u) ^ 1u, args.wc, kDevTimeoutEmpty)) {
-          ok = false;
-          break;
-        }
-        uint8_t* dst = base_ptr + sf_off + buf * kSfBytes + lane * 16;
-#pragma unroll
-        for (int j = 0; j < kSfCols; j += 4)
-          *reinterpret_cast<uint4*>(dst + j * 128) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-          if constexpr (PAIR) mbar_arrive_cluster(report + 8u * buf);
-          else mbar_arrive(report + 8u * buf);
-        }
+    uint32_t raw[3][kSides][4];
+    int tile = unit, kb = kb0, m0 = 0, n0 = 0;   // the next group to load
+    auto load = [&](uint32_t (&r)[kSides][4]) {
+      if (tile >= n_tiles) return;
+      if (kb == kb0) {
+        int mt, nt;
+        gemm8_tile(args.m_tiles, args.n_tiles, tile, &mt, &nt);
+        m0 = mt * tile_m + (PAIR ? rank * kGemm8TileM : 0);
+        n0 = nt * NT;
       }
+      mx_load_scales(args.sa, m0, lane, kb, kb1 - 1, r[0]);
+#pragma unroll
+      for (int j = 1; j < kSides; ++j) mx_load_scales(args.sb, n0 + 128 * (j - 1), lane, kb, kb1 - 1, r[j]);
+      kb += 4;
+      if (kb >= kb1) { kb = kb0; tile += n_units; }
+    };
+    uint32_t group = 0;
+    const int my_tiles = unit < n_tiles ? (n_tiles - unit + n_units - 1) / n_units : 0;
+    const uint32_t groups = (uint32_t)my_tiles * (uint32_t)((kb1 - kb0 + 3) / 4);
+    bool ok = true;
+    auto pass_on = [&](uint32_t (&r)[kSides][4]) {
+      if (!ok || group >= groups) return;
+      const uint32_t buf = group % kMxScaleBufs;
+      if (!mbar_wait(sfe_bar + 8u * buf, ((group / kMxScaleBufs) & 1u) ^ 1u, args.wc, kDevTimeoutEmpty)) {
+        ok = false;
+        return;
+      }
+#pragma unroll
+      for (int j = 0; j < kSides; ++j)
+        mx_store_scales(base_ptr + sf_off + buf * kSfBytes + 512 * j, lane, r[j]);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        if constexpr (PAIR) mbar_arrive_cluster(report + 8u * buf);
+        else mbar_arrive(report + 8u * buf);
+      }
+      ++group;
+      load(r);
+    };
+    load(raw[0]);
+    load(raw[1]);
+    load(raw[2]);
+    while (ok && group < groups) {
+      pass_on(raw[0]);
+      pass_on(raw[1]);
+      pass_on(raw[2]);
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMAs (the leader's, for both CTAs)
@@ -290,7 +339,7 @@ gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             }
           }
           if (in_group == 0) {
-            if (!mbar_wait(sff_bar + 8u * (group & 1u), (group >> 1) & 1u, args.wc, kDevTimeoutFull)) {
+            if (!mbar_wait(sff_bar + 8u * (group % kMxScaleBufs), (group / kMxScaleBufs) & 1u, args.wc, kDevTimeoutFull)) {
               ok = false;
               break;
             }
@@ -301,10 +350,10 @@ gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
           }
           tcgen05_fence_after();
           const bool last = kb == kb1 - 1;
-          const uint32_t sf = tmem_base + kBuf * NT + (group & 1u) * kSfCols;
+          const uint32_t sf = tmem_base + kBuf * NT + (group % kMxScaleBufs) * kSfCols;
           if (elect_one()) {
             if (in_group == 0) {
-              const uint32_t src = base + sf_off + (group & 1u) * kSfBytes;
+              const uint32_t src = base + sf_off + (group % kMxScaleBufs) * kSfBytes;
 #pragma unroll
               for (int j = 0; j < kSfCols; j += 4) tcgen05_copy_scales<PAIR>(sf + j, src + j * 128);
             }
@@ -321,8 +370,8 @@ gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             if constexpr (PAIR) tcgen05_commit_pair(empty_bar + 8u * stage);
             else tcgen05_commit(empty_bar + 8u * stage);
             if (in_group == 3 || last) {
-              if constexpr (PAIR) tcgen05_commit_pair(sfe_bar + 8u * (group & 1u));
-              else tcgen05_commit(sfe_bar + 8u * (group & 1u));
+              if constexpr (PAIR) tcgen05_commit_pair(sfe_bar + 8u * (group % kMxScaleBufs));
+              else tcgen05_commit(sfe_bar + 8u * (group % kMxScaleBufs));
             }
             if (in_chunk == chunk - 1 || last) {
               if constexpr (PAIR) tcgen05_commit_pair(accf_bar + 8u * (acc_n % kBuf));
@@ -348,8 +397,8 @@ gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const int ew = warp - 4;
     const int u0 = (ew >> 2) * kUnits;        // its first unit of 32 columns
     const uint32_t release = PAIR ? map_to_cta(acce_bar, 0) : acce_bar;
-    const uint32_t stg = base + st_off + (uint32_t)ew * kStageTileBytes;
-    uint8_t* stg_ptr = base_ptr + st_off + (size_t)ew * kStageTileBytes;
+    const uint32_t stg = base + st_off + (uint32_t)ew * stg_bytes;
+    uint8_t* stg_ptr = base_ptr + st_off + (size_t)ew * stg_bytes;
     const uint64_t policy = l2_policy_evict_first();
     const int blocks = kb1 - kb0, chunks = (blocks + args.chunk - 1) / args.chunk;
     uint32_t acc_n = 0;

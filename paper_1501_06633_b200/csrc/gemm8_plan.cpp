@@ -101,9 +101,9 @@ maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* pl
   }
   if (!found) return MAXDNN_NOT_SUPPORTED;
   if ((int64_t)plan->m_tiles * plan->n_tiles > (1 << 30)) return MAXDNN_NOT_SUPPORTED;
-  int fixed = 1024 + 128;
+  int fixed = 1024 + 160;
   if (plan->mx) {
-    fixed += (plan->bulk_c ? 8 * 4096 : 0) + 2 * 128 * (4 + 4 * ((plan->tile_n + 127) / 128));
+    fixed += (plan->bulk_c ? 8 * 32 * 32 * c_bytes : 0) + 4 * 128 * (4 + 4 * ((plan->tile_n + 127) / 128));
   } else {
     const int warps = 4 * (plan->tile_n < 64 ? 1 : plan->tile_n / 64), cw = std::min(plan->tile_n, 64);
     fixed += warps * 2 * cw * 4;

@@ -416,6 +416,7 @@ Gemm8Scale scale_of_operand(const Operand& o, int32_t K) {
     s.shift = 0;
     s.step = 1;
     s.kstep = o.mn;
+    s.words = (reinterpret_cast<uintptr_t>(o.s) & 3u) == 0 && o.mn % 4 == 0;
   }
   return s;
 }
