@@ -64,8 +64,8 @@ maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* pl
       const int64_t tiles = m_tiles * n_tiles;
       const int b_stage = b_major == MAXDNN_MAJOR_MN ? std::max(rows_b, 128) * 128 : rows_b * 128;
       const int slots = s.pair ? sm_count / 2 : sm_count;        // tiles that run side by side
-      // an fp32 result is added up from accumulators of four blocks (gemm8_mx.cuh)
-      const int chunk = mx ? (d.c_type == MAXDNN_F32 ? 4 : std::max(k_blocks, 1)) : 1;
+      // an fp32 result is added up from accumulators of sixteen blocks (gemm8_mx.cuh)
+      const int chunk = mx ? (d.c_type == MAXDNN_F32 ? 16 : std::max(k_blocks, 1)) : 1;
       // clocks of one block: its MMAs, filling its stage, reading and adding the product
       const double mma = 2.0 * s.nt, fill = (16384 + b_stage) / 56.0, add = mx ? 0.0 : 100.0 + 4.0 * s.nt;
       double per_block = std::max(mma, std::max(add, fill)) + 20.0;
@@ -101,9 +101,9 @@ maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* pl
   }
   if (!found) return MAXDNN_NOT_SUPPORTED;
   if ((int64_t)plan->m_tiles * plan->n_tiles > (1 << 30)) return MAXDNN_NOT_SUPPORTED;
-  int fixed = 1024 + 160;
+  int fixed = 1024 + 192;
   if (plan->mx) {
-    fixed += (plan->bulk_c ? 8 * 32 * 32 * c_bytes : 0) + 4 * 128 * (4 + 4 * ((plan->tile_n + 127) / 128));
+    fixed += (plan->bulk_c ? 8 * 32 * 32 * c_bytes : 0) + 8 * 128 * (4 + 4 * ((plan->tile_n + 127) / 128));
   } else {
     const int warps = 4 * (plan->tile_n < 64 ? 1 : plan->tile_n / 64), cw = std::min(plan->tile_n, 64);
     fixed += warps * 2 * cw * 4;
