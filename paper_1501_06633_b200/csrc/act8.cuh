@@ -27,7 +27,8 @@ struct Act8Args {
   void* dh;
   int64_t ldh, lda, ldq, ldc;
   int32_t rows, cols, col_blocks;
-  int32_t vec_h, vec_u, vec_a, vec_c, vec_cu, vec_dh, vec_du;
+  int32_t vec_h, vec_u, vec_a, vec_cu, vec_dh, vec_du;
+  int32_t e5m2;                // the packed results'
 };
 
 // f and, where asked for, f'.
@@ -51,17 +52,17 @@ __device__ __forceinline__ void activation(float g, float* f, float* df) {
 }
 
 // Packs eight values of a row block; returns the scale byte.
-template <int QT>
-__device__ __forceinline__ uint32_t pack_row8(const float (&v)[8], uint8_t* p, int n, bool vec, bool live) {
+template <bool EDGE>
+__device__ __forceinline__ uint32_t pack_row8(const float (&v)[8], bool e5m2, uint8_t* p, int n, bool vec, bool live) {
   float m = max_over_block_lanes(max8(v));
   const bool fix = isinf(m);
   if (__any_sync(0xFFFFFFFFu, fix)) m = max_over_block_lanes(finite_max8(v));
-  const uint32_t byte = scale_byte<QT>(m);
-  if (live) store_bytes8(p, pack8<QT>(v, inv_scale_of(byte), fix), n, vec);
+  const uint32_t byte = scale_byte_of(m, e5m2);
+  if (live) store_bytes8<EDGE>(p, pack8_as(v, inv_scale_of(byte), fix, e5m2), n, vec);
   return byte;
 }
 
-template <int XT, int QT, int ACT, bool GATED>
+template <int XT, int ACT, bool GATED, bool EDGE>
 __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_constant__ Act8Args args) {
   typedef typename ElemOf<XT>::T T;
   __shared__ uint8_t bytes[3][kActRows];
@@ -76,8 +77,8 @@ __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_co
   for (int k = 0; k < 4; ++k) {
     const int r = r0 + (t >> 4) + 16 * k;
     const int nr = r < args.rows ? n : 0;
-    rg[k] = load_raw8<XT>(h + (int64_t)r * args.ldh + c0, nr, args.vec_h != 0);
-    if constexpr (GATED) ru[k] = load_raw8<XT>(h + (int64_t)r * args.ldh + args.cols + c0, nr, args.vec_u != 0);
+    rg[k] = load_raw8<XT, EDGE>(h + (int64_t)r * args.ldh + c0, nr, args.vec_h != 0);
+    if constexpr (GATED) ru[k] = load_raw8<XT, EDGE>(h + (int64_t)r * args.ldh + args.cols + c0, nr, args.vec_u != 0);
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -88,10 +89,10 @@ __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_co
     if constexpr (GATED) to_float8<XT>(ru[k], u);
     if (args.c) {
       uint8_t* c = args.c + (int64_t)r * args.ldc + c0;
-      uint32_t b = pack_row8<QT>(g, c, n, args.vec_c != 0, live);
+      uint32_t b = pack_row8<EDGE>(g, args.e5m2 != 0, c, n, true, live);
       if ((t & 15) == 0) bytes[1][(t >> 4) + 16 * k] = (uint8_t)b;
       if constexpr (GATED) {
-        b = pack_row8<QT>(u, c + args.cols, n, args.vec_cu != 0, live);
+        b = pack_row8<EDGE>(u, args.e5m2 != 0, c + args.cols, n, args.vec_cu != 0, live);
         if ((t & 15) == 0) bytes[2][(t >> 4) + 16 * k] = (uint8_t)b;
       }
     }
@@ -102,9 +103,9 @@ __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_co
       a[i] = GATED ? f * u[i] : f;
     }
     if (args.a && live)
-      store_float8<XT>(static_cast<T*>(args.a) + (int64_t)r * args.lda + c0, a, n, args.vec_a != 0);
+      store_float8<XT, EDGE>(static_cast<T*>(args.a) + (int64_t)r * args.lda + c0, a, n, args.vec_a != 0);
     if (args.q) {
-      const uint32_t b = pack_row8<QT>(a, args.q + (int64_t)r * args.ldq + c0, n, true, live);
+      const uint32_t b = pack_row8<EDGE>(a, args.e5m2 != 0, args.q + (int64_t)r * args.ldq + c0, n, true, live);
       if ((t & 15) == 0) bytes[0][(t >> 4) + 16 * k] = (uint8_t)b;
     }
   }
@@ -119,7 +120,7 @@ __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_co
 }
 
 // HT: the type of h (wide, or packed); XT: of da and dh.
-template <int HT, int XT, int ACT, bool GATED>
+template <int HT, int XT, int ACT, bool GATED, bool EDGE>
 __global__ void __launch_bounds__(kActThreads) act8_bprop_kernel(const __grid_constant__ Act8Args args) {
   typedef typename ElemOf<HT>::T TH;
   typedef typename ElemOf<XT>::T T;
@@ -138,9 +139,9 @@ __global__ void __launch_bounds__(kActThreads) act8_bprop_kernel(const __grid_co
   for (int k = 0; k < 4; ++k) {
     const int r = r0 + 16 * k;
     const int nr = r < args.rows ? n : 0;
-    rg[k] = load_raw8<HT>(h + (int64_t)r * ldh + c0, nr, args.vec_h != 0);
-    if constexpr (GATED) ru[k] = load_raw8<HT>(h + (int64_t)r * ldh + args.cols + c0, nr, args.vec_u != 0);
-    rd[k] = load_raw8<XT>(static_cast<const T*>(args.da) + (int64_t)r * args.lda + c0, nr, args.vec_a != 0);
+    rg[k] = load_raw8<HT, EDGE>(h + (int64_t)r * ldh + c0, nr, args.vec_h != 0);
+    if constexpr (GATED) ru[k] = load_raw8<HT, EDGE>(h + (int64_t)r * ldh + args.cols + c0, nr, args.vec_u != 0);
+    rd[k] = load_raw8<XT, EDGE>(static_cast<const T*>(args.da) + (int64_t)r * args.lda + c0, nr, args.vec_a != 0);
     sg[k] = su[k] = 1.f;
     if (is_fp8(HT) && nr > 0) {
       sg[k] = e8m0_value(args.h_scale[(int64_t)cb * args.rows + r]);
@@ -169,8 +170,8 @@ __global__ void __launch_bounds__(kActThreads) act8_bprop_kernel(const __grid_co
       }
     }
     T* dh = static_cast<T*>(args.dh) + (int64_t)r * args.ldh + c0;
-    store_float8<XT>(dh, dg, n, args.vec_dh != 0);
-    if constexpr (GATED) store_float8<XT>(dh + args.cols, du, n, args.vec_du != 0);
+    store_float8<XT, EDGE>(dh, dg, n, args.vec_dh != 0);
+    if constexpr (GATED) store_float8<XT, EDGE>(dh + args.cols, du, n, args.vec_du != 0);
   }
 }
 

@@ -58,28 +58,41 @@ __device__ __forceinline__ float2 unpack2(uint32_t two) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
-// Eight values in 8 bytes.  FIX: infinities become NaN (E4M3) or infinity (E5M2), where the
-// conversion above would give the largest number; needed only where a block holds one.
-template <int QT>
-__device__ __forceinline__ uint2 pack8(const float (&v)[8], float inv, bool fix) {
-  uint32_t w[2];
+// The bytes of infinities among eight packed values: NaN (E4M3) or infinity (E5M2), where the
+// conversion gives the largest number.  Out of line: few blocks hold one.
+static __device__ __noinline__ uint2 infinities8(uint2 w, float v0, float v1, float v2, float v3, float v4, float v5,
+                                                 float v6, float v7, uint32_t code) {
+  const float v[8] = {v0, v1, v2, v3, v4, v5, v6, v7};
+  uint32_t o[2] = {w.x, w.y};
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const uint32_t a = pack2<QT>(v[4 * h] * inv, v[4 * h + 1] * inv);
-    const uint32_t b = pack2<QT>(v[4 * h + 2] * inv, v[4 * h + 3] * inv);
-    w[h] = a | (b << 16);
-  }
-  if (fix) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (isinf(v[i])) {
-        const uint32_t code = (v[i] < 0 ? 0x80u : 0u) | (QT == MAXDNN_E4M3 ? 0x7Fu : 0x7Cu);
-        const int sh = 8 * (i & 3);
-        w[i >> 2] = (w[i >> 2] & ~(0xFFu << sh)) | (code << sh);
-      }
+  for (int i = 0; i < 8; ++i) {
+    if (isinf(v[i])) {
+      const int sh = 8 * (i & 3);
+      o[i >> 2] = (o[i >> 2] & ~(0xFFu << sh)) | ((code | (v[i] < 0 ? 0x80u : 0u)) << sh);
     }
   }
-  return make_uint2(w[0], w[1]);
+  return make_uint2(o[0], o[1]);
+}
+
+// Eight values times `inv` in 8 bytes.  fix: the block holds an infinity.
+template <int QT>
+__device__ __forceinline__ uint2 pack8(const float (&v)[8], float inv, bool fix) {
+  uint2 w;
+  w.x = pack2<QT>(v[0] * inv, v[1] * inv) | (pack2<QT>(v[2] * inv, v[3] * inv) << 16);
+  w.y = pack2<QT>(v[4] * inv, v[5] * inv) | (pack2<QT>(v[6] * inv, v[7] * inv) << 16);
+  if (fix) w = infinities8(w, v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], QT == MAXDNN_E4M3 ? 0x7Fu : 0x7Cu);
+  return w;
+}
+
+template <int QT>
+__device__ __forceinline__ uint32_t scale_byte(float m);
+
+// Both 8-bit types in one kernel: the type is the same for the whole launch.
+__device__ __forceinline__ uint32_t scale_byte_of(float m, bool e5m2) {
+  return e5m2 ? scale_byte<MAXDNN_E5M2>(m) : scale_byte<MAXDNN_E4M3>(m);
+}
+__device__ __forceinline__ uint2 pack8_as(const float (&v)[8], float inv, bool fix, bool e5m2) {
+  return e5m2 ? pack8<MAXDNN_E5M2>(v, inv, fix) : pack8<MAXDNN_E4M3>(v, inv, fix);
 }
 
 // ---- scales ----
@@ -129,30 +142,51 @@ template <> struct Raw8<MAXDNN_E4M3> { uint2 a; };
 template <> struct Raw8<MAXDNN_E5M2> { uint2 a; };
 
 // Loads `n` (0..8) values at `p`; the rest are zeros.  vec: p is aligned for the wide load.
-template <int DT>
+// EDGE = false: vectors are whole (n is 0 or 8) and aligned.  Kernels are built for both: a branch
+// between the two forms makes the loaded registers move when the branches join, which waits for each load in
+// turn (a layer norm with 16 loads a lane took 9.7 us a row that way).
+template <int DT, bool EDGE>
 __device__ __forceinline__ Raw8<DT> load_raw8(const typename ElemOf<DT>::T* p, int n, bool vec) {
   typedef typename ElemOf<DT>::T T;
   Raw8<DT> r;
-  if (n == 8 && vec) {
+  if (!EDGE || (n == 8 && vec)) {
     if constexpr (DT == MAXDNN_F32) {
-      r.a = __ldg(reinterpret_cast<const uint4*>(p));
-      r.b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
+      r.a = r.b = make_uint4(0, 0, 0, 0);
+      if (EDGE || n) {
+        r.a = __ldg(reinterpret_cast<const uint4*>(p));
+        r.b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
+      }
     } else if constexpr (is_fp8(DT)) {
-      r.a = __ldg(reinterpret_cast<const uint2*>(p));
+      r.a = make_uint2(0, 0);
+      if (EDGE || n) r.a = __ldg(reinterpret_cast<const uint2*>(p));
     } else {
-      r.a = __ldg(reinterpret_cast<const uint4*>(p));
+      r.a = make_uint4(0, 0, 0, 0);
+      if (EDGE || n) r.a = __ldg(reinterpret_cast<const uint4*>(p));
     }
   } else {
-    uint32_t w[8 * sizeof(T) / 4];
+    // value by value into the top of the register chain, which moves down (a loop: the edge of a
+    // matrix is not worth eight copies of this code)
+    constexpr int kWords = 2 * (int)sizeof(T);
+    uint32_t w[kWords];
 #pragma unroll
-    for (int i = 0; i < (int)(8 * sizeof(T) / 4); ++i) w[i] = 0;
-#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0;
+#pragma unroll 1
     for (int i = 0; i < 8; ++i) {
+      uint32_t top = 0;
       if (i < n) {
-        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(p[i]);
-        else if constexpr (sizeof(T) == 2)
-          w[i >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
-        else w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+        if constexpr (sizeof(T) == 4) top = __float_as_uint(p[i]);
+        else if constexpr (sizeof(T) == 2) top = (uint32_t)reinterpret_cast<const uint16_t*>(p)[i];
+        else top = (uint32_t)p[i];
+      }
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int k = 0; k + 1 < kWords; ++k) w[k] = w[k + 1];
+        w[kWords - 1] = top;
+      } else {
+        constexpr int kBits = 8 * (int)sizeof(T);
+#pragma unroll
+        for (int k = 0; k + 1 < kWords; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], kBits);
+        w[kWords - 1] = (w[kWords - 1] >> kBits) | (top << (32 - kBits));
       }
     }
     if constexpr (DT == MAXDNN_F32) {
@@ -200,6 +234,14 @@ __device__ __forceinline__ void to_float8(const Raw8<DT>& r, float (&v)[8]) {
   }
 }
 
+// Hides that the registers are what an earlier conversion saw, so that the values are converted
+// again where they are used instead of being kept as fp32.
+template <int DT>
+__device__ __forceinline__ void convert_again(Raw8<DT>& r) {
+  if constexpr (DT == MAXDNN_BF16 || DT == MAXDNN_F16)
+    asm volatile("" : "+r"(r.a.x), "+r"(r.a.y), "+r"(r.a.z), "+r"(r.a.w));
+}
+
 template <int DT>
 __device__ __forceinline__ typename ElemOf<DT>::T from_float(float v) {
   if constexpr (DT == MAXDNN_F32) return v;
@@ -207,41 +249,60 @@ __device__ __forceinline__ typename ElemOf<DT>::T from_float(float v) {
   else return __float2half_rn(v);
 }
 
-template <int DT>
+// Stores the first `n` values.  EDGE = false: n is 0 or 8 and p is aligned.
+template <int DT, bool EDGE = true>
 __device__ __forceinline__ void store_float8(typename ElemOf<DT>::T* p, const float (&v)[8], int n, bool vec) {
   static_assert(!is_fp8(DT), "8-bit values are stored by store_bytes8");
-  if (n == 8 && vec) {
-    if constexpr (DT == MAXDNN_F32) {
-      reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-      reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-      uint32_t w[4];
+  constexpr int kWords = 2 * (int)sizeof(typename ElemOf<DT>::T);
+  uint32_t w[kWords];
+  if constexpr (DT == MAXDNN_F32) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (DT == MAXDNN_BF16) {
-          const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-          w[i] = *reinterpret_cast<const uint32_t*>(&t);
-        } else {
-          const __half2 t = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-          w[i] = *reinterpret_cast<const uint32_t*>(&t);
-        }
-      }
-      *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = from_float<DT>(v[i]);
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (DT == MAXDNN_BF16) {
+        const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&t);
+      } else {
+        const __half2 t = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&t);
+      }
+    }
+  }
+  if (!EDGE && n == 0) return;
+  if (!EDGE || (n == 8 && vec)) {
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    if constexpr (DT == MAXDNN_F32) reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  } else {
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+      if constexpr (DT == MAXDNN_F32) {
+        reinterpret_cast<uint32_t*>(p)[i] = w[0];
+#pragma unroll
+        for (int k = 0; k + 1 < kWords; ++k) w[k] = w[k + 1];
+      } else {
+        reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)w[0];
+#pragma unroll
+        for (int k = 0; k + 1 < kWords; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
+        w[kWords - 1] >>= 16;
+      }
+    }
   }
 }
 
+template <bool EDGE>
 __device__ __forceinline__ void store_bytes8(uint8_t* p, uint2 w, int n, bool vec) {
-  if (n == 8 && vec) {
+  if (!EDGE && n == 0) return;
+  if (!EDGE || (n == 8 && vec)) {
     *reinterpret_cast<uint2*>(p) = w;
   } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+      p[i] = (uint8_t)w.x;
+      w.x = __funnelshift_r(w.x, w.y, 8);
+      w.y >>= 8;
+    }
   }
 }
 

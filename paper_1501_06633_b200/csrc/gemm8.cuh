@@ -74,9 +74,10 @@ __device__ __forceinline__ void tma_load_2d_hint(uint32_t dst, const CUtensorMap
       : "memory");
 }
 
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
 
@@ -102,6 +103,37 @@ __device__ __forceinline__ void gemm8_tile(int m_tiles, int n_tiles, int t, int*
   const int in = t - group * per_group;
   *mt = first + in % height;
   *nt = in / height;
+}
+
+// The end of a tile that `split` CTAs of a cluster share: CTA `rank` adds the CTAs' totals
+// ([column][row] at `base` of each CTA's shared memory) for its part of the columns, in CTA order,
+// and stores them.  A thread takes four rows of a column; all CTAs' loads are in flight at once.
+template <int NT, int THREADS, class Args>
+__device__ __forceinline__ void gemm8_add_split(const Args& args, uint32_t base, int split, int rank, int unit) {
+  const int cols = NT / split;
+  int mt, nt;
+  gemm8_tile(args.m_tiles, args.n_tiles, unit, &mt, &nt);
+  for (int e = threadIdx.x; e < cols * (kGemm8TileM / 4); e += THREADS) {
+    const int row = 4 * (e & (kGemm8TileM / 4 - 1)), col = rank * cols + e / (kGemm8TileM / 4);
+    const uint32_t off = base + 4u * (uint32_t)(col * kGemm8TileM + row);
+    float4 part[kGemm8MaxSplit];
+#pragma unroll
+    for (int r = 0; r < kGemm8MaxSplit; ++r)
+      if (r < split) part[r] = ld_cluster_f32x4(map_to_cta(off, (uint32_t)r));
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < kGemm8MaxSplit; ++r)
+      if (r < split) {
+        v[0] += part[r].x; v[1] += part[r].y; v[2] += part[r].z; v[3] += part[r].w;
+      }
+    const int m = mt * kGemm8TileM + row, n = nt * NT + col;
+    if (n < args.N) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (m + i < args.M)
+          gemm8_store1(args.c, args.c_type, (int64_t)(m + i) * args.c_row + (int64_t)n * args.c_col, v[i]);
+    }
+  }
 }
 
 // SBV: the columns have a scale each (else one for 128 of them).
@@ -340,21 +372,9 @@ gemm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
   tcgen05_fence_before();
   __syncthreads();
   if (split > 1) {
-    // one tile per cluster: CTA `rank` adds up and stores its part of the columns
     cluster_arrive();
     cluster_wait();
-    const int cols = NT / split;
-    int mt, nt;
-    gemm8_tile(args.m_tiles, args.n_tiles, unit, &mt, &nt);
-    constexpr int kThreads = gemm8_threads(NT);
-    for (int e = threadIdx.x; e < cols * kGemm8TileM; e += kThreads) {
-      const int row = e & (kGemm8TileM - 1), col = rank * cols + (e >> 7);
-      const uint32_t off = base + 4u * (uint32_t)(col * kGemm8TileM + row);
-      float v = 0.f;
-      for (int r = 0; r < split; ++r) v += ld_cluster_f32(map_to_cta(off, (uint32_t)r));
-      const int m = mt * kGemm8TileM + row, n = nt * NT + col;
-      if (m < args.M && n < args.N) gemm8_store1(args.c, args.c_type, (int64_t)m * args.c_row + (int64_t)n * args.c_col, v);
-    }
+    gemm8_add_split<NT, gemm8_threads(NT)>(args, base, split, rank, unit);
     cluster_arrive();
     cluster_wait();
   }

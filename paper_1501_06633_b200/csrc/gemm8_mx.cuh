@@ -149,8 +149,11 @@ __device__ __forceinline__ void mx_store_scales(uint8_t* dst, int lane, const ui
   for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(p + 16 * i) = w[i];
 }
 
+// Few columns: two CTAs share an SM, so that one's copies run while the other starts or ends.
+__host__ __device__ constexpr int mx_ctas_per_sm(int nt) { return nt <= 32 ? 2 : 1; }
+
 template <int NT, bool PAIR>
-__global__ void __launch_bounds__(kMxThreads, 1)
+__global__ void __launch_bounds__(kMxThreads, mx_ctas_per_sm(NT))
 gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                 const __grid_constant__ CUtensorMap map_c, const __grid_constant__ Gemm8MxArgs args) {
   constexpr int kBuf = mx_buffers(NT);
@@ -531,21 +534,9 @@ gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     cluster_arrive();      // neither CTA leaves while its peer may still use its memory or barriers
     cluster_wait();
   } else if (split > 1) {
-    // one tile per cluster: CTA `rank` adds up and stores its part of the columns
     cluster_arrive();
     cluster_wait();
-    const int cols = NT / split;
-    int mt, nt;
-    gemm8_tile(args.m_tiles, args.n_tiles, unit, &mt, &nt);
-    for (int e = threadIdx.x; e < cols * kGemm8TileM; e += kMxThreads) {
-      const int row = e & (kGemm8TileM - 1), col = rank * cols + (e >> 7);
-      const uint32_t off = base + 4u * (uint32_t)(col * kGemm8TileM + row);
-      float v = 0.f;
-      for (int r = 0; r < split; ++r) v += ld_cluster_f32(map_to_cta(off, (uint32_t)r));
-      const int m = mt * kGemm8TileM + row, n = nt * NT + col;
-      if (m < args.M && n < args.N)
-        gemm8_store1(args.c, args.c_type, (int64_t)m * args.c_row + (int64_t)n * args.c_col, v);
-    }
+    gemm8_add_split<NT, kMxThreads>(args, base, split, rank, unit);
     cluster_arrive();
     cluster_wait();
   }

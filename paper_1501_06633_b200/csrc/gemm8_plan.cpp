@@ -38,17 +38,22 @@ maxdnn_status check_gemm8(const maxdnn_gemm8_desc* d) {
   return MAXDNN_OK;
 }
 
-// One candidate of the search below.
-struct Shape { int mx, pair, nt; };
+// One tile shape of the search below, with what it measured (microseconds): a block of the
+// reduction in a long run, and what a tile takes besides (ring fill, reading and storing the result).
+struct Shape { int mx, pair, nt; double block, tile; };
 
 maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* plan) {
-  static const Shape kShapes[] = {{1, 0, 16}, {1, 0, 32}, {1, 0, 64}, {1, 0, 128},
-                                  {1, 1, 128}, {1, 1, 192}, {1, 1, 224}, {1, 1, 256},
-                                  {0, 0, 16}, {0, 0, 32}, {0, 0, 64}, {0, 0, 128}, {0, 0, 256}};
+  static const Shape kShapes[] = {
+      {1, 0, 16, 0.20, 1.6}, {1, 0, 32, 0.20, 1.6}, {1, 0, 64, 0.21, 1.8}, {1, 0, 128, 0.28, 2.0},
+      {1, 1, 128, 0.255, 3.1}, {1, 1, 192, 0.32, 3.6}, {1, 1, 224, 0.37, 3.8}, {1, 1, 256, 0.42, 4.0},
+      {0, 0, 16, 0.35, 1.6}, {0, 0, 32, 0.38, 1.6}, {0, 0, 64, 0.45, 1.8}, {0, 0, 128, 0.65, 2.0},
+      {0, 0, 256, 1.05, 3.0}};
   static const int kSplit[4] = {1, 2, 4, 8};
   const int k_blocks = (d.K + kGemm8BlockK - 1) / kGemm8BlockK;
   const int mx = d.a_scale_type == MAXDNN_E8M0 && d.b_scale_type == MAXDNN_E8M0;
   const int c_bytes = d.c_type == MAXDNN_F32 ? 4 : 2;
+  // no shape is faster than reading the operands and writing the result
+  const double memory = 5.0 + ((double)d.M * d.K + (double)d.N * d.K + (double)d.M * d.N * c_bytes) / 5.8e6;
   double best = 0;
   bool found = false;
   for (int swap = 0; swap < 2; ++swap) {
@@ -63,13 +68,9 @@ maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* pl
       const int64_t m_tiles = (M + tile_m - 1) / tile_m, n_tiles = (N + s.nt - 1) / s.nt;
       const int64_t tiles = m_tiles * n_tiles;
       const int b_stage = b_major == MAXDNN_MAJOR_MN ? std::max(rows_b, 128) * 128 : rows_b * 128;
-      const int slots = s.pair ? sm_count / 2 : sm_count;        // tiles that run side by side
+      const int slots = s.pair ? sm_count / 2 : mx && s.nt <= 32 ? 2 * sm_count : sm_count;   // tiles that run side by side
       // an fp32 result is added up from accumulators of sixteen blocks (gemm8_mx.cuh)
       const int chunk = mx ? (d.c_type == MAXDNN_F32 ? 16 : std::max(k_blocks, 1)) : 1;
-      // clocks of one block: its MMAs, filling its stage, reading and adding the product
-      const double mma = 2.0 * s.nt, fill = (16384 + b_stage) / 56.0, add = mx ? 0.0 : 100.0 + 4.0 * s.nt;
-      double per_block = std::max(mma, std::max(add, fill)) + 20.0;
-      if (mx && s.nt > 224) per_block += 500.0 / chunk;          // its one accumulator is emptied in between
       for (int split : kSplit) {
         if (option_is_set(OPT_GEMM8_SPLIT) && option(OPT_GEMM8_SPLIT) != split) continue;
         if (split > k_blocks || (split > 1 && s.pair)) continue;
@@ -77,7 +78,14 @@ maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* pl
         const int64_t units = split == 1 ? std::min<int64_t>(tiles, slots) : tiles;
         const int64_t waves = (tiles * split + slots - 1) / slots;
         const int64_t blocks = (k_blocks + split - 1) / split;
-        const double t = (double)waves * ((double)blocks * per_block + 800.0) + 1500.0 + (split > 1 ? 1500.0 + 4.0 * s.nt : 0.0);
+        // 3.4 us is a call with one block; sharing a tile costs an exchange of totals; two CTAs on
+        // an SM share its issue slots
+        const double crowd = s.nt <= 32 && mx ? std::max(1.0, 0.4 + 0.6 * (double)std::min<int64_t>(tiles * split, slots) / sm_count) : 1.0;
+        const double run = 3.4 + (double)(waves * blocks) * s.block * crowd + s.tile * (1.0 + (double)(waves - 1) / 3.0) +
+                           (split > 1 ? 1.0 + 0.008 * s.nt : 0.0);
+        // every tile reads its operands from the second-level cache
+        const double fill = 5.0 + (double)tiles * k_blocks * (16384 + b_stage) * (s.pair ? 2 : 1) / 11.0e6;
+        const double t = std::max(std::max(run, fill), memory) + 0.05 * run;
         if (found && t >= best) continue;
         found = true;
         best = t;
@@ -109,7 +117,17 @@ maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* pl
     fixed += warps * 2 * cw * 4;
   }
   const int per_stage = 16384 + plan->b_stage_bytes + 16;
+  // a CTA of one tile needs no more stages than it has blocks; two CTAs of an SM share its memory
+  const int blocks = (k_blocks + plan->split - 1) / plan->split;
+  const int ctas_per_tile = plan->pair ? 2 : plan->split;
+  const bool one_tile = (int64_t)plan->m_tiles * plan->n_tiles * ctas_per_tile <= plan->grid;
   plan->stages = std::min(12, (232448 - fixed) / per_stage);
+  if (plan->mx && plan->tile_n <= 32 && plan->grid > sm_count) plan->stages = std::min(plan->stages, (115200 - fixed) / per_stage);
+  if (one_tile) plan->stages = std::max(2, std::min(plan->stages, blocks));
+  if (plan->split > 1) {        // the totals take the place of the ring
+    const int need = plan->tile_n * kGemm8TileM * 4, ring = per_stage - 16;
+    plan->stages = std::max(plan->stages, (need + ring - 1) / ring);
+  }
   plan->smem_bytes = fixed + plan->stages * per_stage;
   return MAXDNN_OK;
 }

@@ -28,7 +28,8 @@ struct LayerNormArgs {
   float* partial;              // [grid][2][cols] sums of a CTA's rows: dy xh, dy
   int64_t ldx, ldy, ldq;
   int32_t rows, cols, w_type;
-  int32_t vec_x, vec_y;
+  int32_t vec_x, vec_y, vec_w; // rows (weights) allow the wide loads
+  int32_t q_e5m2;
   float eps, inv_cols;
 };
 
@@ -51,85 +52,118 @@ __device__ __forceinline__ float row_sum(float v, float* slot, int warps, int la
   return s;
 }
 
-// WARP_ROW: each warp of the CTA has a row of its own; else the CTA has one.
-template <int XT, int QT, int J, bool WARP_ROW>
-__global__ void __launch_bounds__(WARP_ROW ? 128 : 512)
+// Packs eight values of a row block (16 lanes) and stores them with the block's scale.
+template <bool EDGE>
+__device__ __forceinline__ void norm_pack(const float (&v)[8], bool e5m2, uint8_t* q, uint8_t* s, int n, int lane) {
+  float m = max_over_block_lanes(max8(v));
+  const bool fix = isinf(m);
+  if (__any_sync(0xFFFFFFFFu, fix)) m = max_over_block_lanes(finite_max8(v));
+  const uint32_t byte = scale_byte_of(m, e5m2);
+  store_bytes8<EDGE>(q, pack8_as(v, inv_scale_of(byte), fix, e5m2), n, true);
+  if ((lane & 15) == 0 && n > 0) *s = (uint8_t)byte;
+}
+
+// Eight neighbouring weights.
+template <bool EDGE>
+__device__ __forceinline__ void load_weights8(const void* p, int c, int n, int type, bool vec, float none, float (&w)[8]) {
+  if (!p || n == 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = none;
+  } else if (type == MAXDNN_F32) {
+    to_float8<MAXDNN_F32>(load_raw8<MAXDNN_F32, EDGE>(static_cast<const float*>(p) + c, n, vec), w);
+  } else if (type == MAXDNN_BF16) {
+    to_float8<MAXDNN_BF16>(load_raw8<MAXDNN_BF16, EDGE>(static_cast<const __nv_bfloat16*>(p) + c, n, vec), w);
+  } else {
+    to_float8<MAXDNN_F16>(load_raw8<MAXDNN_F16, EDGE>(static_cast<const __half*>(p) + c, n, vec), w);
+  }
+}
+
+// WR warps have a row, vector j of the row's thread t at column 8 (t + 32 WR j); a CTA of eight
+// warps has 8 / WR rows at a time.  The row stays as it was loaded (4 J registers of 16-bit values) and is
+// converted again for each of the three sums; a warp alone needs no barrier, and its J loads of
+// 16 bytes a lane are all in flight.  8192 x 4096 bf16 with packed y and x: a CTA per row with the row
+// as fp32 registers took 102 us.
+constexpr int kNormThreads = 256;
+template <int XT, int J, int WR, bool EDGE>
+__global__ void __launch_bounds__(kNormThreads, J >= 16 || (J >= 8 && XT == MAXDNN_F32) ? 2 : J >= 4 ? 3 : 4)
 layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
   typedef typename ElemOf<XT>::T T;
-  __shared__ float slots[2][kNormMaxWarps];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  const int t = WARP_ROW ? lane : (int)threadIdx.x;
-  const int threads = WARP_ROW ? 32 : (int)blockDim.x;
-  const int per_cta = WARP_ROW ? warps : 1;
+  __shared__ float slots[8 / WR][2][WR];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int group = warp / WR, in_row = warp % WR, t = in_row * 32 + lane;
   const T* x = static_cast<const T*>(args.x);
   T* y = static_cast<T*>(args.y);
-  float g[J][8], b[J][8];
+  // sum over the row's threads
+  auto total = [&](float v, int slot) {
+    v = warp_sum(v);
+    if constexpr (WR > 1) {
+      if (lane == 0) slots[group][slot][in_row] = v;
+      asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(WR * 32) : "memory");
+      v = 0.f;
 #pragma unroll
-  for (int j = 0; j < J; ++j)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int c = 8 * (t + threads * j) + i;
-      g[j][i] = (args.gamma && c < args.cols) ? load_weight(args.gamma, c, args.w_type) : 1.f;
-      b[j][i] = (args.beta && c < args.cols) ? load_weight(args.beta, c, args.w_type) : 0.f;
+      for (int w = 0; w < WR; ++w) v += slots[group][slot][w];
     }
-  for (int64_t r = (int64_t)blockIdx.x * per_cta + (WARP_ROW ? warp : 0); r < args.rows;
-       r += (int64_t)gridDim.x * per_cta) {
-    float v[J][8];
+    return v;
+  };
+  for (int64_t r = (int64_t)blockIdx.x * (8 / WR) + group; r < args.rows; r += (int64_t)gridDim.x * (8 / WR)) {
+    Raw8<XT> raw[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int c = 8 * (t + 32 * WR * j);
+      raw[j] = load_raw8<XT, EDGE>(x + r * args.ldx + c, min(max(args.cols - c, 0), 8), args.vec_x != 0);
+    }
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      const int c = 8 * (t + threads * j);
-      to_float8<XT>(load_raw8<XT>(x + r * args.ldx + c, min(max(args.cols - c, 0), 8), args.vec_x != 0), v[j]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum += v[j][i];
+      float v[8];
+      to_float8<XT>(raw[j], v);
+      sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
     }
-    const float mean = row_sum<WARP_ROW>(sum, slots[0], warps, lane, warp) * args.inv_cols;
+    const float mean = total(sum, 0) * args.inv_cols;
     float sq = 0.f;
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+    for (int j = 0; j < J; ++j) {
+      const int n = args.cols - 8 * (t + 32 * WR * j);
+      float v[8], part = 0.f;
+      convert_again(raw[j]);
+      to_float8<XT>(raw[j], v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float d = 8 * (t + threads * j) + i < args.cols ? v[j][i] - mean : 0.f;
-        sq = fmaf(d, d, sq);
+        const float d = v[i] - mean;
+        if (EDGE ? i < n : n > 0) part = fmaf(d, d, part);
       }
-    const float var = row_sum<WARP_ROW>(sq, slots[1], warps, lane, warp) * args.inv_cols;
-    const float rstd = 1.f / sqrtf(var + args.eps);
+      sq += part;
+    }
+    const float rstd = 1.f / sqrtf(total(sq, 1) * args.inv_cols + args.eps);
     if (t == 0) {
       if (args.mean) args.mean[r] = mean;
       if (args.rstd) args.rstd[r] = rstd;
     }
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      const int c = 8 * (t + threads * j);
+      const int c = 8 * (t + 32 * WR * j);
       const int n = min(max(args.cols - c, 0), 8);
-      if (args.c) {
-        float m = max_over_block_lanes(max8(v[j]));
-        const bool fix = isinf(m);
-        if (__any_sync(0xFFFFFFFFu, fix)) m = max_over_block_lanes(finite_max8(v[j]));
-        const uint32_t byte = scale_byte<QT>(m);
-        store_bytes8(args.c + r * args.ldq + c, pack8<QT>(v[j], inv_scale_of(byte), fix), n, true);
-        if ((lane & 15) == 0 && n > 0) args.sc[(int64_t)(c >> 7) * args.rows + r] = (uint8_t)byte;
-      }
-      float o[8];
+      float v[8];
+      convert_again(raw[j]);
+      to_float8<XT>(raw[j], v);
+      if (args.c) norm_pack<EDGE>(v, args.q_e5m2, args.c + r * args.ldq + c, args.sc + (int64_t)(c >> 7) * args.rows + r, n, lane);
+      if (!args.y && !args.q) continue;
+      asm volatile("" ::: "memory");      // the weights of one vector at a time: their registers are short
+      float g[8], b[8];
+      load_weights8<EDGE>(args.gamma, c, n, args.w_type, args.vec_w != 0, 1.f, g);
+      load_weights8<EDGE>(args.beta, c, n, args.w_type, args.vec_w != 0, 0.f, b);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = i < n ? fmaf((v[j][i] - mean) * rstd, g[j][i], b[j][i]) : 0.f;
-      if (args.y) store_float8<XT>(y + r * args.ldy + c, o, n, args.vec_y != 0);
-      if (args.q) {
-        float m = max_over_block_lanes(max8(o));
-        const bool fix = isinf(m);
-        if (__any_sync(0xFFFFFFFFu, fix)) m = max_over_block_lanes(finite_max8(o));
-        const uint32_t byte = scale_byte<QT>(m);
-        store_bytes8(args.q + r * args.ldq + c, pack8<QT>(o, inv_scale_of(byte), fix), n, true);
-        if ((lane & 15) == 0 && n > 0) args.s[(int64_t)(c >> 7) * args.rows + r] = (uint8_t)byte;
-      }
+      for (int i = 0; i < 8; ++i) v[i] = (EDGE ? i < n : n > 0) ? fmaf((v[i] - mean) * rstd, g[i], b[i]) : 0.f;
+      if (args.y) store_float8<XT, EDGE>(y + r * args.ldy + c, v, n, args.vec_y != 0);
+      if (args.q) norm_pack<EDGE>(v, args.q_e5m2, args.q + r * args.ldq + c, args.s + (int64_t)(c >> 7) * args.rows + r, n, lane);
     }
-    // no barrier here: a thread reaches the next row's first write of slots[0] only after the
-    // second sum's barrier, which follows every read of slots[0] of this row (slots[1] likewise)
+    // no barrier here: a thread reaches the next row's first write of a slot only after the
+    // second sum's barrier, which follows every read of the first slot (and the other way round)
   }
 }
 
 // XT: the type of x (wide, or packed rows); YT: of dy and dx.
-template <int XT, int YT, int J, bool WARP_ROW>
+template <int XT, int YT, int J, bool WARP_ROW, bool EDGE>
 __global__ void __launch_bounds__(WARP_ROW ? 128 : 512)
 layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
   typedef typename ElemOf<XT>::T TX;
@@ -162,14 +196,14 @@ layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
     for (int j = 0; j < J; ++j) {
       const int c = 8 * (t + threads * j);
       const int n = min(max(args.cols - c, 0), 8);
-      to_float8<XT>(load_raw8<XT>(x + r * args.ldx + c, n, args.vec_x != 0), xh[j]);
-      to_float8<YT>(load_raw8<YT>(dy + r * args.ldy + c, n, args.vec_y != 0), e[j]);
+      to_float8<XT>(load_raw8<XT, EDGE>(x + r * args.ldx + c, n, args.vec_x != 0), xh[j]);
+      to_float8<YT>(load_raw8<YT, EDGE>(dy + r * args.ldy + c, n, args.vec_y != 0), e[j]);
       float scale = 1.f;
       if constexpr (is_fp8(XT)) scale = n > 0 ? e8m0_value(args.x_scale[(int64_t)(c >> 7) * args.rows + r]) : 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         if constexpr (is_fp8(XT)) xh[j][i] *= scale;
-        xh[j][i] = i < n ? (xh[j][i] - mean) * rstd : 0.f;
+        xh[j][i] = (EDGE ? i < n : n > 0) ? (xh[j][i] - mean) * rstd : 0.f;
         dg[j][i] = fmaf(e[j][i], xh[j][i], dg[j][i]);
         db[j][i] += e[j][i];
         e[j][i] *= g[j][i];
@@ -200,7 +234,7 @@ layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
       float o[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) o[i] = rstd * (e[j][i] - s1 - xh[j][i] * s2);
-      store_float8<YT>(dx + r * args.ldy + c, o, n, args.vec_y != 0);
+      store_float8<YT, EDGE>(dx + r * args.ldy + c, o, n, args.vec_y != 0);
     }
   }
   if (!args.partial) return;
@@ -261,8 +295,9 @@ __global__ void __launch_bounds__(256) layer_norm_fold_kernel(const float* parti
 
 // Rows too long for the registers of a CTA: the same sums with the row read again for each (it
 // comes from the second-level cache).  One CTA of 1024 threads per row, 8192 columns at a time.
-template <int XT, int QT>
+template <int XT>
 __global__ void __launch_bounds__(1024) layer_norm_fprop_long_kernel(const __grid_constant__ LayerNormArgs args) {
+  constexpr bool EDGE = true;
   typedef typename ElemOf<XT>::T T;
   __shared__ float slots[2][kNormMaxWarps];
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -276,7 +311,7 @@ __global__ void __launch_bounds__(1024) layer_norm_fprop_long_kernel(const __gri
         const int c = 8 * t + 8192 * j;
         const int n = min(max(args.cols - c, 0), 8);
         float v[8];
-        to_float8<XT>(load_raw8<XT>(x + r * args.ldx + c, n, args.vec_x != 0), v);
+        to_float8<XT>(load_raw8<XT, EDGE>(x + r * args.ldx + c, n, args.vec_x != 0), v);
         if (pass == 0) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) acc += v[i];
@@ -287,29 +322,14 @@ __global__ void __launch_bounds__(1024) layer_norm_fprop_long_kernel(const __gri
             acc = fmaf(d, d, acc);
           }
         } else {
-          if (args.c) {
-            float m = max_over_block_lanes(max8(v));
-            const bool fix = isinf(m);
-            if (__any_sync(0xFFFFFFFFu, fix)) m = max_over_block_lanes(finite_max8(v));
-            const uint32_t byte = scale_byte<QT>(m);
-            store_bytes8(args.c + r * args.ldq + c, pack8<QT>(v, inv_scale_of(byte), fix), n, true);
-            if ((lane & 15) == 0 && n > 0) args.sc[(int64_t)(c >> 7) * args.rows + r] = (uint8_t)byte;
-          }
+          if (args.c) norm_pack<EDGE>(v, args.q_e5m2, args.c + r * args.ldq + c, args.sc + (int64_t)(c >> 7) * args.rows + r, n, lane);
+          float g[8], b[8];
+          load_weights8<EDGE>(args.gamma, c, n, args.w_type, args.vec_w != 0, 1.f, g);
+          load_weights8<EDGE>(args.beta, c, n, args.w_type, args.vec_w != 0, 0.f, b);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float g = (args.gamma && i < n) ? load_weight(args.gamma, c + i, args.w_type) : 1.f;
-            const float b = (args.beta && i < n) ? load_weight(args.beta, c + i, args.w_type) : 0.f;
-            v[i] = i < n ? fmaf((v[i] - mean) * rstd, g, b) : 0.f;
-          }
-          if (args.y) store_float8<XT>(y + r * args.ldy + c, v, n, args.vec_y != 0);
-          if (args.q) {
-            float m = max_over_block_lanes(max8(v));
-            const bool fix = isinf(m);
-            if (__any_sync(0xFFFFFFFFu, fix)) m = max_over_block_lanes(finite_max8(v));
-            const uint32_t byte = scale_byte<QT>(m);
-            store_bytes8(args.q + r * args.ldq + c, pack8<QT>(v, inv_scale_of(byte), fix), n, true);
-            if ((lane & 15) == 0 && n > 0) args.s[(int64_t)(c >> 7) * args.rows + r] = (uint8_t)byte;
-          }
+          for (int i = 0; i < 8; ++i) v[i] = (EDGE ? i < n : n > 0) ? fmaf((v[i] - mean) * rstd, g[i], b[i]) : 0.f;
+          if (args.y) store_float8<XT, EDGE>(y + r * args.ldy + c, v, n, args.vec_y != 0);
+          if (args.q) norm_pack<EDGE>(v, args.q_e5m2, args.q + r * args.ldq + c, args.s + (int64_t)(c >> 7) * args.rows + r, n, lane);
         }
       }
       if (pass == 2) break;
@@ -329,6 +349,7 @@ __global__ void __launch_bounds__(1024) layer_norm_fprop_long_kernel(const __gri
 // (this CTA alone writes them, each thread always the same columns).
 template <int XT, int YT>
 __global__ void __launch_bounds__(1024) layer_norm_bprop_long_kernel(const __grid_constant__ LayerNormArgs args) {
+  constexpr bool EDGE = true;
   typedef typename ElemOf<XT>::T TX;
   typedef typename ElemOf<YT>::T TY;
   __shared__ float slots[2][2][kNormMaxWarps];
@@ -347,8 +368,8 @@ __global__ void __launch_bounds__(1024) layer_norm_bprop_long_kernel(const __gri
         const int c = 8 * t + 8192 * j;
         const int n = min(max(args.cols - c, 0), 8);
         float xh[8], e[8];
-        to_float8<XT>(load_raw8<XT>(x + r * args.ldx + c, n, args.vec_x != 0), xh);
-        to_float8<YT>(load_raw8<YT>(dy + r * args.ldy + c, n, args.vec_y != 0), e);
+        to_float8<XT>(load_raw8<XT, EDGE>(x + r * args.ldx + c, n, args.vec_x != 0), xh);
+        to_float8<YT>(load_raw8<YT, EDGE>(dy + r * args.ldy + c, n, args.vec_y != 0), e);
         float scale = 1.f;
         if constexpr (is_fp8(XT)) scale = n > 0 ? e8m0_value(args.x_scale[(int64_t)(c >> 7) * args.rows + r]) : 0.f;
         float o[8];
@@ -370,7 +391,7 @@ __global__ void __launch_bounds__(1024) layer_norm_bprop_long_kernel(const __gri
             o[i] = rstd * (e[i] * g - s1 - xh[i] * s2);
           }
         }
-        if (pass == 1) store_float8<YT>(static_cast<TY*>(args.dx) + r * args.ldy + c, o, n, args.vec_y != 0);
+        if (pass == 1) store_float8<YT, EDGE>(static_cast<TY*>(args.dx) + r * args.ldy + c, o, n, args.vec_y != 0);
       }
       if (pass == 1) break;
       s1 = warp_sum(s1);

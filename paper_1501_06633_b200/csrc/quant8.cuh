@@ -22,9 +22,10 @@ struct Quant8Args {
   int32_t rows, cols;
   int32_t col_blocks;          // blocks of 128 columns
   int32_t vec_x;               // rows of x allow the wide load
+  int32_t e5m2;
 };
 
-template <int XT, int QT>
+template <int XT, bool EDGE>
 __global__ void __launch_bounds__(kQuantThreads) quant8_kernel(const __grid_constant__ Quant8Args args) {
   typedef typename ElemOf<XT>::T T;
   __shared__ float col_part[kQuantThreads / 32][kBlock8];   // per warp: maxima of its rows
@@ -43,7 +44,7 @@ __global__ void __launch_bounds__(kQuantThreads) quant8_kernel(const __grid_cons
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const int r = r0 + rg + 16 * k;
-    raw[k] = load_raw8<XT>(x + (int64_t)r * args.ldx + c0, r < args.rows ? n : 0, args.vec_x != 0);
+    raw[k] = load_raw8<XT, EDGE>(x + (int64_t)r * args.ldx + c0, r < args.rows ? n : 0, args.vec_x != 0);
     if constexpr (is_fp8(XT))
       xs[k] = r < args.rows ? e8m0_value(args.x_scale[(int64_t)cb * args.rows + r]) : 0.f;
   }
@@ -91,13 +92,13 @@ __global__ void __launch_bounds__(kQuantThreads) quant8_kernel(const __grid_cons
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = isinf(v[i]) ? v[i] : v[i] * inv_col[i];
     }
-    store_bytes8(q + (int64_t)r * args.ldq + c0, pack8<QT>(v, inv_row, fix), n, true);
+    store_bytes8<EDGE>(q + (int64_t)r * args.ldq + c0, pack8_as(v, inv_row, fix, args.e5m2 != 0), n, true);
   };
 
   if (args.q_row) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const uint32_t b = scale_byte<QT>(max_over_block_lanes(row_max[k]));
+      const uint32_t b = scale_byte_of(max_over_block_lanes(row_max[k]), args.e5m2 != 0);
       if ((t & 15) == 0) row_byte[rg + 16 * k] = (uint8_t)b;
       store(args.q_row, k, inv_scale_of(b), nullptr);
     }
@@ -118,7 +119,7 @@ __global__ void __launch_bounds__(kQuantThreads) quant8_kernel(const __grid_cons
     float m = 0.f;
 #pragma unroll
     for (int w = 0; w < kQuantThreads / 32; ++w) m = fmaxf(m, col_part[w][t]);
-    const uint32_t b = scale_byte<QT>(m);
+    const uint32_t b = scale_byte_of(m, args.e5m2 != 0);
     col_inv[t] = inv_scale_of(b);
     if (args.q_col && cb * kBlock8 + t < args.cols)
       args.s_col[(int64_t)rb * args.cols + cb * kBlock8 + t] = (uint8_t)b;
@@ -135,7 +136,8 @@ __global__ void __launch_bounds__(kQuantThreads) quant8_kernel(const __grid_cons
     for (int k = 0; k < 8; ++k) store(args.q_col, k, 1.f, inv);
   }
   if (args.q_tile) {
-    const uint32_t b = scale_byte<QT>(fmaxf(fmaxf(warp_max[0], warp_max[1]), fmaxf(warp_max[2], warp_max[3])));
+    const float m = fmaxf(fmaxf(warp_max[0], warp_max[1]), fmaxf(warp_max[2], warp_max[3]));
+    const uint32_t b = scale_byte_of(m, args.e5m2 != 0);
 #pragma unroll
     for (int k = 0; k < 8; ++k) store(args.q_tile, k, inv_scale_of(b), nullptr);
     if (t == 0) args.s_tile[(int64_t)rb * args.col_blocks + cb] = (uint8_t)b;
@@ -153,7 +155,7 @@ struct Dequant8Args {
 };
 
 // The same tile and the same eight columns x eight rows in each thread.
-template <int XT, int QT>
+template <int XT, int QT, bool EDGE>
 __global__ void __launch_bounds__(kQuantThreads) dequant8_kernel(const __grid_constant__ Dequant8Args args) {
   typedef typename ElemOf<XT>::T T;
   const int t = threadIdx.x;
@@ -167,7 +169,7 @@ __global__ void __launch_bounds__(kQuantThreads) dequant8_kernel(const __grid_co
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const int r = r0 + 16 * k;
-    raw[k] = load_raw8<QT>(args.q + (int64_t)r * args.ldq + c0, r < args.rows ? n : 0, args.vec_q != 0);
+    raw[k] = load_raw8<QT, EDGE>(args.q + (int64_t)r * args.ldq + c0, r < args.rows ? n : 0, args.vec_q != 0);
     byte[k] = 127;
     if (args.block == MAXDNN_BLOCK_ROW && r < args.rows) byte[k] = args.s[(int64_t)cb * args.rows + r];
   }
@@ -192,7 +194,7 @@ __global__ void __launch_bounds__(kQuantThreads) dequant8_kernel(const __grid_co
     const float m = e8m0_value(byte[k]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = args.block == MAXDNN_BLOCK_ROW ? v[i] * m : v[i] * s[i];
-    store_float8<XT>(static_cast<T*>(args.x) + (int64_t)r * args.ldx + c0, v, n, args.vec_x != 0);
+    store_float8<XT, EDGE>(static_cast<T*>(args.x) + (int64_t)r * args.ldx + c0, v, n, args.vec_x != 0);
   }
 }
 
