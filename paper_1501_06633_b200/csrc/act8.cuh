@@ -28,41 +28,43 @@ struct Act8Args {
   int64_t ldh, lda, ldq, ldc;
   int32_t rows, cols, col_blocks;
   int32_t vec_h, vec_u, vec_a, vec_cu, vec_dh, vec_du;
-  int32_t e5m2;                // the packed results'
 };
 
-// f and, where asked for, f'.
+// 1 / (1 + exp(-x)) from the hardware's exponential and reciprocal.  The exponential's relative
+// error grows with |x| (1e-7 |x|), but enters s as s (1 - s) of it, which falls as exp(-|x|): the
+// error of s stays below 2e-7.
+__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+
+// f and, where asked for, f'.  (1 + tanh z) / 2 is the sigmoid of 2 z.
 template <int ACT, bool GRAD>
 __device__ __forceinline__ void activation(float g, float* f, float* df) {
   if constexpr (ACT == MAXDNN_ACT_SILU) {
-    const float s = 1.f / (1.f + expf(-g));
+    const float s = sigmoid(g);
     *f = g * s;
     if (GRAD) *df = s * fmaf(g, 1.f - s, 1.f);
   } else if constexpr (ACT == MAXDNN_ACT_GELU) {
     const float p = 0.5f * (1.f + erff(g * 0.70710678118654752f));
     *f = g * p;
-    if (GRAD) *df = fmaf(g * 0.39894228040143268f, expf(-0.5f * g * g), p);
+    if (GRAD) *df = fmaf(g * 0.39894228040143268f, __expf(-0.5f * g * g), p);
   } else {
-    const float k = 0.79788456080286536f;                    // sqrt(2 / pi)
-    const float t = tanhf(k * fmaf(0.044715f * g * g, g, g));
-    const float p = 0.5f * (1.f + t);
+    const float k = 1.5957691216057308f;                    // 2 sqrt(2 / pi)
+    const float q = fminf(g * g, 1e8f);                     // far out p (1 - p) is 0: no 0 x inf
+    const float p = sigmoid(k * g * fmaf(0.044715f, q, 1.f));
     *f = g * p;
-    if (GRAD) *df = fmaf(0.5f * g * (1.f - t * t), k * fmaf(0.134145f, fminf(g * g, 1e8f), 1.f), p);   // no 0 x inf
+    if (GRAD) *df = fmaf(g * p * (1.f - p), k * fmaf(0.134145f, q, 1.f), p);
   }
 }
 
 // Packs eight values of a row block; returns the scale byte.
-template <bool EDGE>
-__device__ __forceinline__ uint32_t pack_row8(const float (&v)[8], bool e5m2, uint8_t* p, int n, bool vec, bool live) {
-  float m = max_over_block_lanes(max8(v));
-  const bool fix = isinf(m);
-  if (__any_sync(0xFFFFFFFFu, fix)) m = max_over_block_lanes(finite_max8(v));
-  const uint32_t byte = scale_byte_of(m, e5m2);
-  if (live) store_bytes8<EDGE>(p, pack8_as(v, inv_scale_of(byte), fix, e5m2), n, vec);
+template <int QT, bool EDGE>
+__device__ __forceinline__ uint32_t pack_row8(const F2 (&v)[4], uint8_t* p, int n, bool vec, bool live) {
+  bool fix;
+  const uint32_t byte = block_byte<QT>(v, &fix);
+  if (live) store_bytes8<EDGE>(p, pack8<QT>(v, inv_scale_of(byte), fix), n, vec);
   return byte;
 }
 
-template <int XT, int ACT, bool GATED, bool EDGE>
+template <int XT, int QT, int ACT, bool GATED, bool EDGE>
 __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_constant__ Act8Args args) {
   typedef typename ElemOf<XT>::T T;
   __shared__ uint8_t bytes[3][kActRows];
@@ -84,15 +86,19 @@ __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_co
   for (int k = 0; k < 4; ++k) {
     const int r = r0 + (t >> 4) + 16 * k;
     const bool live = r < args.rows && n > 0;
+    F2 v[4];
     float g[8], u[8], a[8];
-    to_float8<XT>(rg[k], g);
-    if constexpr (GATED) to_float8<XT>(ru[k], u);
+    to_pairs<XT>(rg[k], v);
+    to_floats(v, g);
     if (args.c) {
-      uint8_t* c = args.c + (int64_t)r * args.ldc + c0;
-      uint32_t b = pack_row8<EDGE>(g, args.e5m2 != 0, c, n, true, live);
+      const uint32_t b = pack_row8<QT, EDGE>(v, args.c + (int64_t)r * args.ldc + c0, n, true, live);
       if ((t & 15) == 0) bytes[1][(t >> 4) + 16 * k] = (uint8_t)b;
-      if constexpr (GATED) {
-        b = pack_row8<EDGE>(u, args.e5m2 != 0, c + args.cols, n, args.vec_cu != 0, live);
+    }
+    if constexpr (GATED) {
+      to_pairs<XT>(ru[k], v);
+      to_floats(v, u);
+      if (args.c) {
+        const uint32_t b = pack_row8<QT, EDGE>(v, args.c + (int64_t)r * args.ldc + args.cols + c0, n, args.vec_cu != 0, live);
         if ((t & 15) == 0) bytes[2][(t >> 4) + 16 * k] = (uint8_t)b;
       }
     }
@@ -105,7 +111,9 @@ __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_co
     if (args.a && live)
       store_float8<XT, EDGE>(static_cast<T*>(args.a) + (int64_t)r * args.lda + c0, a, n, args.vec_a != 0);
     if (args.q) {
-      const uint32_t b = pack_row8<EDGE>(a, args.e5m2 != 0, args.q + (int64_t)r * args.ldq + c0, n, true, live);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = f2(a[2 * i], a[2 * i + 1]);
+      const uint32_t b = pack_row8<QT, EDGE>(v, args.q + (int64_t)r * args.ldq + c0, n, true, live);
       if ((t & 15) == 0) bytes[0][(t >> 4) + 16 * k] = (uint8_t)b;
     }
   }

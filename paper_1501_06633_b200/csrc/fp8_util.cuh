@@ -37,6 +37,46 @@ __host__ __device__ constexpr bool is_wide(int dt) {
   return dt == MAXDNN_F32 || dt == MAXDNN_BF16 || dt == MAXDNN_F16;
 }
 
+// ---- pairs of fp32 values in one 64-bit register: two adds, multiplies or fused
+// multiply-adds for one issue slot (each rounded as the single operation is) ----
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ F2 f2(float both) { return f2(both, both); }
+__device__ __forceinline__ float2 unf2(F2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ float sum2(F2 v) {
+  const float2 t = unf2(v);
+  return t.x + t.y;
+}
+// The largest magnitude of three values; NaN do not count.
+__device__ __forceinline__ float max3abs(float a, float b, float c) {
+  float r;
+  asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 // ---- two 8-bit values <-> fp32 (low byte first) ----
 template <int QT>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -76,23 +116,24 @@ static __device__ __noinline__ uint2 infinities8(uint2 w, float v0, float v1, fl
 
 // Eight values times `inv` in 8 bytes.  fix: the block holds an infinity.
 template <int QT>
-__device__ __forceinline__ uint2 pack8(const float (&v)[8], float inv, bool fix) {
-  uint2 w;
-  w.x = pack2<QT>(v[0] * inv, v[1] * inv) | (pack2<QT>(v[2] * inv, v[3] * inv) << 16);
-  w.y = pack2<QT>(v[4] * inv, v[5] * inv) | (pack2<QT>(v[6] * inv, v[7] * inv) << 16);
-  if (fix) w = infinities8(w, v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], QT == MAXDNN_E4M3 ? 0x7Fu : 0x7Cu);
+__device__ __forceinline__ uint2 pack8(const F2 (&v)[4], const F2 (&inv)[4], bool fix) {
+  uint32_t h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 t = unf2(mul2(v[i], inv[i]));
+    h[i] = pack2<QT>(t.x, t.y);
+  }
+  uint2 w = make_uint2(__byte_perm(h[0], h[1], 0x5410), __byte_perm(h[2], h[3], 0x5410));
+  if (fix) {
+    const float2 a = unf2(v[0]), b = unf2(v[1]), c = unf2(v[2]), d = unf2(v[3]);
+    w = infinities8(w, a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y, QT == MAXDNN_E4M3 ? 0x7Fu : 0x7Cu);
+  }
   return w;
 }
-
 template <int QT>
-__device__ __forceinline__ uint32_t scale_byte(float m);
-
-// Both 8-bit types in one kernel: the type is the same for the whole launch.
-__device__ __forceinline__ uint32_t scale_byte_of(float m, bool e5m2) {
-  return e5m2 ? scale_byte<MAXDNN_E5M2>(m) : scale_byte<MAXDNN_E4M3>(m);
-}
-__device__ __forceinline__ uint2 pack8_as(const float (&v)[8], float inv, bool fix, bool e5m2) {
-  return e5m2 ? pack8<MAXDNN_E5M2>(v, inv, fix) : pack8<MAXDNN_E4M3>(v, inv, fix);
+__device__ __forceinline__ uint2 pack8(const F2 (&v)[4], float inv, bool fix) {
+  const F2 k = f2(inv), all[4] = {k, k, k, k};
+  return pack8<QT>(v, all, fix);
 }
 
 // ---- scales ----
@@ -120,17 +161,29 @@ __device__ __forceinline__ float max_over_block_lanes(float m) {
 }
 
 // Largest magnitude of eight values; NaN do not count, infinities do (see finite_max8).
-__device__ __forceinline__ float max8(const float (&v)[8]) {
+__device__ __forceinline__ float max8(const F2 (&v)[4]) {
+  const float2 a = unf2(v[0]), b = unf2(v[1]), c = unf2(v[2]), d = unf2(v[3]);
+  return max3abs(max3abs(a.x, a.y, b.x), max3abs(b.y, c.x, c.y), max3abs(d.x, d.y, 0.f));
+}
+static __device__ __noinline__ float finite_max8(F2 v0, F2 v1, F2 v2, F2 v3) {
+  const F2 v[4] = {v0, v1, v2, v3};
   float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[i]));
+  for (int i = 0; i < 4; ++i) {
+    const float2 t = unf2(v[i]);
+    m = fmaxf(m, isinf(t.x) ? 0.f : fabsf(t.x));
+    m = fmaxf(m, isinf(t.y) ? 0.f : fabsf(t.y));
+  }
   return m;
 }
-__device__ __forceinline__ float finite_max8(const float (&v)[8]) {
-  float m = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = fmaxf(m, isinf(v[i]) ? 0.f : fabsf(v[i]));
-  return m;
+// The scale byte of a row block whose lanes hold eight values each (16 lanes); *fix: it holds an
+// infinity.  All lanes of the warp take part.
+template <int QT>
+__device__ __forceinline__ uint32_t block_byte(const F2 (&v)[4], bool* fix) {
+  float m = max_over_block_lanes(max8(v));
+  *fix = isinf(m);
+  if (__any_sync(0xFFFFFFFFu, *fix)) m = max_over_block_lanes(finite_max8(v[0], v[1], v[2], v[3]));
+  return scale_byte<QT>(m);
 }
 
 // ---- eight neighbouring values as they lie in memory ----
@@ -234,6 +287,30 @@ __device__ __forceinline__ void to_float8(const Raw8<DT>& r, float (&v)[8]) {
   }
 }
 
+// The same values as pairs.
+template <int DT>
+__device__ __forceinline__ void to_pairs(const Raw8<DT>& r, F2 (&v)[4]) {
+  if constexpr (DT == MAXDNN_F32) {
+    v[0] = ((F2)r.a.y << 32) | r.a.x;
+    v[1] = ((F2)r.a.w << 32) | r.a.z;
+    v[2] = ((F2)r.b.y << 32) | r.b.x;
+    v[3] = ((F2)r.b.w << 32) | r.b.z;
+  } else {
+    float f[8];
+    to_float8<DT>(r, f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = f2(f[2 * i], f[2 * i + 1]);
+  }
+}
+__device__ __forceinline__ void to_floats(const F2 (&v)[4], float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 t = unf2(v[i]);
+    f[2 * i] = t.x;
+    f[2 * i + 1] = t.y;
+  }
+}
+
 // Hides that the registers are what an earlier conversion saw, so that the values are converted
 // again where they are used instead of being kept as fp32.
 template <int DT>
@@ -289,6 +366,13 @@ __device__ __forceinline__ void store_float8(typename ElemOf<DT>::T* p, const fl
       }
     }
   }
+}
+
+template <int DT, bool EDGE>
+__device__ __forceinline__ void store_pairs(typename ElemOf<DT>::T* p, const F2 (&v)[4], int n, bool vec) {
+  float f[8];
+  to_floats(v, f);
+  store_float8<DT, EDGE>(p, f, n, vec);
 }
 
 template <bool EDGE>

@@ -2,16 +2,12 @@
 // launches.
 #include <cstring>
 
+#include "api8.h"
 #include "gemm8.cuh"
 #include "gemm8_mx.cuh"
-#include "plan.h"
-#include "runtime.h"
 
 namespace maxdnn {
 namespace {
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-int64_t blocks_of(int64_t n) { return (n + kBlock8 - 1) / kBlock8; }
 
 struct Operand {
   const void *p, *s;

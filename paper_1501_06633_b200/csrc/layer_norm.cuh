@@ -6,13 +6,14 @@
 //   dx = rstd (g dy - s1 - xh s2),  s1 = sum(g dy) / C,  s2 = sum(g dy xh) / C
 //   dg = sum over rows of dy xh,  db = sum over rows of dy
 //
-// A row is read once and stays in registers: T threads (a warp, or a whole CTA) hold it as
+// A row is read once and stays in registers: T threads (a warp, or several) hold it as
 // vectors of eight columns, vector j of thread t at column 8 (t + T j).  The variance is summed from the
 // differences to the mean, not from squares, so a row far from zero loses nothing.  All sums are
 // in 32 bits.  Sixteen neighbouring lanes hold a block of 128 columns, so the packed forms take
 // four shuffles each.
 #pragma once
 #include "fp8_util.cuh"
+#include "ptx_util.cuh"
 
 namespace maxdnn {
 
@@ -35,57 +36,87 @@ struct LayerNormArgs {
 
 constexpr int kNormMaxWarps = 32;
 
-// Sum over the T threads of a row (T = 32: a warp).  `slot` alternates between two calls.
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
   return v;
 }
-template <bool WARP_ROW>
-__device__ __forceinline__ float row_sum(float v, float* slot, int warps, int lane, int warp) {
-  v = warp_sum(v);
-  if constexpr (WARP_ROW) return v;
-  if (lane == 0) slot[warp] = v;
-  __syncthreads();
-  float s = 0.f;
-  for (int w = 0; w < warps; ++w) s += slot[w];
-  return s;
-}
 
-// Packs eight values of a row block (16 lanes) and stores them with the block's scale.
-template <bool EDGE>
-__device__ __forceinline__ void norm_pack(const float (&v)[8], bool e5m2, uint8_t* q, uint8_t* s, int n, int lane) {
-  float m = max_over_block_lanes(max8(v));
-  const bool fix = isinf(m);
-  if (__any_sync(0xFFFFFFFFu, fix)) m = max_over_block_lanes(finite_max8(v));
-  const uint32_t byte = scale_byte_of(m, e5m2);
-  store_bytes8<EDGE>(q, pack8_as(v, inv_scale_of(byte), fix, e5m2), n, true);
+// Packs eight values of a row block (16 lanes) and stores them with the block's scale.  QT: the
+// 8-bit type, or kEitherFp8: `e5m2` tells.
+constexpr int kEitherFp8 = 0;
+template <int QT, bool EDGE>
+__device__ __forceinline__ void norm_pack(const F2 (&v)[4], bool e5m2, uint8_t* q, uint8_t* s, int n, int lane) {
+  bool fix;
+  uint32_t byte;
+  uint2 w;
+  if (QT == MAXDNN_E5M2 || (QT == kEitherFp8 && e5m2)) {
+    byte = block_byte<MAXDNN_E5M2>(v, &fix);
+    w = pack8<MAXDNN_E5M2>(v, inv_scale_of(byte), fix);
+  } else {
+    byte = block_byte<MAXDNN_E4M3>(v, &fix);
+    w = pack8<MAXDNN_E4M3>(v, inv_scale_of(byte), fix);
+  }
+  store_bytes8<EDGE>(q, w, n, true);
   if ((lane & 15) == 0 && n > 0) *s = (uint8_t)byte;
 }
 
 // Eight neighbouring weights.
 template <bool EDGE>
-__device__ __forceinline__ void load_weights8(const void* p, int c, int n, int type, bool vec, float none, float (&w)[8]) {
+__device__ __forceinline__ void load_weights8(const void* p, int c, int n, int type, bool vec, float none, F2 (&w)[4]) {
   if (!p || n == 0) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = none;
+    for (int i = 0; i < 4; ++i) w[i] = f2(none);
   } else if (type == MAXDNN_F32) {
-    to_float8<MAXDNN_F32>(load_raw8<MAXDNN_F32, EDGE>(static_cast<const float*>(p) + c, n, vec), w);
+    to_pairs<MAXDNN_F32>(load_raw8<MAXDNN_F32, EDGE>(static_cast<const float*>(p) + c, n, vec), w);
   } else if (type == MAXDNN_BF16) {
-    to_float8<MAXDNN_BF16>(load_raw8<MAXDNN_BF16, EDGE>(static_cast<const __nv_bfloat16*>(p) + c, n, vec), w);
+    to_pairs<MAXDNN_BF16>(load_raw8<MAXDNN_BF16, EDGE>(static_cast<const __nv_bfloat16*>(p) + c, n, vec), w);
   } else {
-    to_float8<MAXDNN_F16>(load_raw8<MAXDNN_F16, EDGE>(static_cast<const __half*>(p) + c, n, vec), w);
+    to_pairs<MAXDNN_F16>(load_raw8<MAXDNN_F16, EDGE>(static_cast<const __half*>(p) + c, n, vec), w);
   }
+}
+
+// y of eight columns; columns at and after n become zeros (they take part in the block's maximum).
+template <bool EDGE>
+__device__ __forceinline__ void normalise8(F2 (&v)[4], F2 minus_mean, F2 rstd, const F2 (&g)[4], const F2 (&b)[4], int n) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = fma2(mul2(add2(v[i], minus_mean), rstd), g[i], b[i]);
+  if (EDGE) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 t = unf2(v[i]);
+      v[i] = f2(2 * i < n ? t.x : 0.f, 2 * i + 1 < n ? t.y : 0.f);
+    }
+  } else if (n == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = 0;
+  }
+}
+
+// Sum of squares of the differences to the mean, of the first n of eight columns.
+template <bool EDGE>
+__device__ __forceinline__ float squares8(const F2 (&v)[4], F2 minus_mean, int n) {
+  F2 part = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    F2 d = add2(v[i], minus_mean);
+    if (EDGE) {
+      const float2 t = unf2(d);
+      d = f2(2 * i < n ? t.x : 0.f, 2 * i + 1 < n ? t.y : 0.f);
+    }
+    part = fma2(d, d, part);
+  }
+  return EDGE || n > 0 ? sum2(part) : 0.f;
 }
 
 // WR warps have a row, vector j of the row's thread t at column 8 (t + 32 WR j); a CTA of eight
 // warps has 8 / WR rows at a time.  The row stays as it was loaded (4 J registers of 16-bit values) and is
-// converted again for each of the three sums; a warp alone needs no barrier, and its J loads of
-// 16 bytes a lane are all in flight.  8192 x 4096 bf16 with packed y and x: a CTA per row with the row
-// as fp32 registers took 102 us.
+// converted again for each of the three sums.  J is at most 4 up to 8192 columns: with 16 vectors to a lane the
+// unrolled code no longer fits the instruction cache (8192 x 4096 with packed y and x: a third of
+// the stalls were for instructions, 89 us).
 constexpr int kNormThreads = 256;
-template <int XT, int J, int WR, bool EDGE>
-__global__ void __launch_bounds__(kNormThreads, J >= 16 || (J >= 8 && XT == MAXDNN_F32) ? 2 : J >= 4 ? 3 : 4)
+template <int XT, int QT, int J, int WR, bool EDGE>
+__global__ void __launch_bounds__(kNormThreads, J > 4 ? 2 : XT == MAXDNN_F32 || EDGE ? 3 : 4)
 layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
   typedef typename ElemOf<XT>::T T;
   __shared__ float slots[8 / WR][2][WR];
@@ -112,27 +143,22 @@ layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
       const int c = 8 * (t + 32 * WR * j);
       raw[j] = load_raw8<XT, EDGE>(x + r * args.ldx + c, min(max(args.cols - c, 0), 8), args.vec_x != 0);
     }
-    float sum = 0.f;
+    F2 sum = 0;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      float v[8];
-      to_float8<XT>(raw[j], v);
-      sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+      F2 v[4];
+      to_pairs<XT>(raw[j], v);
+      sum = add2(sum, add2(add2(v[0], v[1]), add2(v[2], v[3])));
     }
-    const float mean = total(sum, 0) * args.inv_cols;
+    const float mean = total(sum2(sum), 0) * args.inv_cols;
+    const F2 minus_mean = f2(-mean);
     float sq = 0.f;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      const int n = args.cols - 8 * (t + 32 * WR * j);
-      float v[8], part = 0.f;
+      F2 v[4];
       convert_again(raw[j]);
-      to_float8<XT>(raw[j], v);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float d = v[i] - mean;
-        if (EDGE ? i < n : n > 0) part = fmaf(d, d, part);
-      }
-      sq += part;
+      to_pairs<XT>(raw[j], v);
+      sq += squares8<EDGE>(v, minus_mean, min(max(args.cols - 8 * (t + 32 * WR * j), 0), 8));
     }
     const float rstd = 1.f / sqrtf(total(sq, 1) * args.inv_cols + args.eps);
     if (t == 0) {
@@ -143,26 +169,68 @@ layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
     for (int j = 0; j < J; ++j) {
       const int c = 8 * (t + 32 * WR * j);
       const int n = min(max(args.cols - c, 0), 8);
-      float v[8];
+      F2 v[4];
       convert_again(raw[j]);
-      to_float8<XT>(raw[j], v);
-      if (args.c) norm_pack<EDGE>(v, args.q_e5m2, args.c + r * args.ldq + c, args.sc + (int64_t)(c >> 7) * args.rows + r, n, lane);
+      to_pairs<XT>(raw[j], v);
+      if (args.c)
+        norm_pack<QT, EDGE>(v, args.q_e5m2, args.c + r * args.ldq + c, args.sc + (int64_t)(c >> 7) * args.rows + r, n, lane);
       if (!args.y && !args.q) continue;
-      asm volatile("" ::: "memory");      // the weights of one vector at a time: their registers are short
-      float g[8], b[8];
+      F2 g[4], b[4];
       load_weights8<EDGE>(args.gamma, c, n, args.w_type, args.vec_w != 0, 1.f, g);
       load_weights8<EDGE>(args.beta, c, n, args.w_type, args.vec_w != 0, 0.f, b);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = (EDGE ? i < n : n > 0) ? fmaf((v[i] - mean) * rstd, g[i], b[i]) : 0.f;
-      if (args.y) store_float8<XT, EDGE>(y + r * args.ldy + c, v, n, args.vec_y != 0);
-      if (args.q) norm_pack<EDGE>(v, args.q_e5m2, args.q + r * args.ldq + c, args.s + (int64_t)(c >> 7) * args.rows + r, n, lane);
+      normalise8<EDGE>(v, minus_mean, f2(rstd), g, b, n);
+      if (args.y) store_pairs<XT, EDGE>(y + r * args.ldy + c, v, n, args.vec_y != 0);
+      if (args.q)
+        norm_pack<QT, EDGE>(v, args.q_e5m2, args.q + r * args.ldq + c, args.s + (int64_t)(c >> 7) * args.rows + r, n, lane);
     }
     // no barrier here: a thread reaches the next row's first write of a slot only after the
     // second sum's barrier, which follows every read of the first slot (and the other way round)
   }
 }
 
-// XT: the type of x (wide, or packed rows); YT: of dy and dx.
+// Sum over the 1024 threads of a CTA.  `slot` alternates between two calls.
+__device__ __forceinline__ float cta_sum(float v, float* slot, int lane, int warp) {
+  v = warp_sum(v);
+  if (lane == 0) slot[warp] = v;
+  __syncthreads();
+  float s = 0.f;
+  for (int w = 0; w < kNormMaxWarps; ++w) s += slot[w];
+  return s;
+}
+
+// Eight columns of the backward pass as they come from memory: xh and gamma dy, with this row's
+// part of dg and db added up.
+template <int XT, int YT, bool EDGE>
+__device__ __forceinline__ void norm_back8(const Raw8<XT>& rx, const Raw8<YT>& rdy, float scale, float mean, float rstd,
+                                           const F2 (&g)[4], int n, F2 (&xh)[4], F2 (&e)[4], F2 (&dg)[4], F2 (&db)[4],
+                                           F2* s1, F2* s2) {
+  to_pairs<XT>(rx, xh);
+  to_pairs<YT>(rdy, e);
+  const F2 k = f2(scale), mm = f2(-mean), rs = f2(rstd);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    xh[i] = mul2(is_fp8(XT) ? fma2(xh[i], k, mm) : add2(xh[i], mm), rs);
+    if (EDGE) {
+      const float2 t = unf2(xh[i]);
+      xh[i] = f2(2 * i < n ? t.x : 0.f, 2 * i + 1 < n ? t.y : 0.f);
+    }
+    dg[i] = fma2(e[i], xh[i], dg[i]);
+    db[i] = add2(db[i], e[i]);
+    e[i] = mul2(e[i], g[i]);
+    *s1 = add2(*s1, e[i]);
+    *s2 = fma2(e[i], xh[i], *s2);
+  }
+}
+
+// rstd (e - s1 - xh s2) of eight columns.
+__device__ __forceinline__ void norm_dx8(const F2 (&xh)[4], const F2 (&e)[4], float rstd, float s1, float s2, F2 (&o)[4]) {
+  const F2 m1 = f2(-s1), m2 = f2(-s2), rs = f2(rstd);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = mul2(rs, fma2(xh[i], m2, add2(e[i], m1)));
+}
+
+// XT: the type of x (wide, or packed rows); YT: of dy and dx.  WARP_ROW: each warp of the CTA has
+// a row of its own; else the CTA has one.  (Rows of up to 1024 columns, and rows whose vectors are not whole.)
 template <int XT, int YT, int J, bool WARP_ROW, bool EDGE>
 __global__ void __launch_bounds__(WARP_ROW ? 128 : 512)
 layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
@@ -177,42 +245,36 @@ layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
   const TX* x = static_cast<const TX*>(args.x);
   const TY* dy = static_cast<const TY*>(args.dy);
   TY* dx = static_cast<TY*>(args.dx);
-  float g[J][8], dg[J][8], db[J][8];
+  F2 g[J][4], dg[J][4], db[J][4];
 #pragma unroll
-  for (int j = 0; j < J; ++j)
+  for (int j = 0; j < J; ++j) {
+    const int c = 8 * (t + threads * j);
+    load_weights8<true>(args.gamma, c, min(max(args.cols - c, 0), 8), args.w_type, args.vec_w != 0, 1.f, g[j]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int c = 8 * (t + threads * j) + i;
-      g[j][i] = (args.gamma && c < args.cols) ? load_weight(args.gamma, c, args.w_type) : 1.f;
-      dg[j][i] = db[j][i] = 0.f;
-    }
+    for (int i = 0; i < 4; ++i) dg[j][i] = db[j][i] = 0;
+  }
   int flip = 0;
   for (int64_t r = (int64_t)blockIdx.x * per_cta + (WARP_ROW ? warp : 0); r < args.rows;
        r += (int64_t)gridDim.x * per_cta, flip ^= 1) {
     const float mean = args.mean[r], rstd = args.rstd[r];
-    float xh[J][8], e[J][8];
-    float s1 = 0.f, s2 = 0.f;
+    Raw8<XT> rx[J];
+    Raw8<YT> rdy[J];
+    float scale[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int c = 8 * (t + threads * j);
       const int n = min(max(args.cols - c, 0), 8);
-      to_float8<XT>(load_raw8<XT, EDGE>(x + r * args.ldx + c, n, args.vec_x != 0), xh[j]);
-      to_float8<YT>(load_raw8<YT, EDGE>(dy + r * args.ldy + c, n, args.vec_y != 0), e[j]);
-      float scale = 1.f;
-      if constexpr (is_fp8(XT)) scale = n > 0 ? e8m0_value(args.x_scale[(int64_t)(c >> 7) * args.rows + r]) : 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (is_fp8(XT)) xh[j][i] *= scale;
-        xh[j][i] = (EDGE ? i < n : n > 0) ? (xh[j][i] - mean) * rstd : 0.f;
-        dg[j][i] = fmaf(e[j][i], xh[j][i], dg[j][i]);
-        db[j][i] += e[j][i];
-        e[j][i] *= g[j][i];
-        s1 += e[j][i];
-        s2 = fmaf(e[j][i], xh[j][i], s2);
-      }
+      rx[j] = load_raw8<XT, EDGE>(x + r * args.ldx + c, n, args.vec_x != 0);
+      rdy[j] = load_raw8<YT, EDGE>(dy + r * args.ldy + c, n, args.vec_y != 0);
+      scale[j] = 1.f;
+      if constexpr (is_fp8(XT)) scale[j] = n > 0 ? e8m0_value(args.x_scale[(int64_t)(c >> 7) * args.rows + r]) : 0.f;
     }
-    s1 = warp_sum(s1);
-    s2 = warp_sum(s2);
+    F2 xh[J][4], e[J][4], p1 = 0, p2 = 0;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+      norm_back8<XT, YT, EDGE>(rx[j], rdy[j], scale[j], mean, rstd, g[j], min(max(args.cols - 8 * (t + threads * j), 0), 8),
+                               xh[j], e[j], dg[j], db[j], &p1, &p2);
+    float s1 = warp_sum(sum2(p1)), s2 = warp_sum(sum2(p2));
     if constexpr (!WARP_ROW) {
       if (lane == 0) {
         slots[flip][0][warp] = s1;
@@ -230,11 +292,9 @@ layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int c = 8 * (t + threads * j);
-      const int n = min(max(args.cols - c, 0), 8);
-      float o[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = rstd * (e[j][i] - s1 - xh[j][i] * s2);
-      store_float8<YT, EDGE>(dx + r * args.ldy + c, o, n, args.vec_y != 0);
+      F2 o[4];
+      norm_dx8(xh[j], e[j], rstd, s1, s2, o);
+      store_pairs<YT, EDGE>(dx + r * args.ldy + c, o, min(max(args.cols - c, 0), 8), args.vec_y != 0);
     }
   }
   if (!args.partial) return;
@@ -242,6 +302,9 @@ layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
   float* out = args.partial + (int64_t)blockIdx.x * 2 * args.cols;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
+    float a[J][8];
+#pragma unroll
+    for (int j = 0; j < J; ++j) to_floats(which ? db[j] : dg[j], a[j]);
     if constexpr (WARP_ROW) {
       for (int w = 0; w < warps; ++w) {
         if (warp == w) {
@@ -250,8 +313,7 @@ layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               float& f = fold[(i * J + j) * 32 + lane];
-              const float a = which ? db[j][i] : dg[j][i];
-              f = w == 0 ? a : f + a;
+              f = w == 0 ? a[j][i] : f + a[j][i];
             }
         }
         __syncthreads();
@@ -267,37 +329,189 @@ layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int c = 8 * (t + threads * j) + i;
-          if (c < args.cols) out[(int64_t)which * args.cols + c] = which ? db[j][i] : dg[j][i];
+          if (c < args.cols) out[(int64_t)which * args.cols + c] = a[j][i];
         }
     }
   }
 }
 
-// dg and db from the CTAs' sums, in CTA order.  A CTA takes 32 columns; its eight warps take
-// every eighth sum each and are added in warp order.
-__global__ void __launch_bounds__(256) layer_norm_fold_kernel(const float* partial, int parts, int cols,
-                                                              float* dgamma, float* dbeta) {
-  __shared__ float part[8][33];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t c = (int64_t)blockIdx.x * 32 + lane;     // of the 2 x cols sums
-  float s = 0.f;
-  if (c < 2 * (int64_t)cols)
-    for (int p = warp; p < parts; p += 8) s += partial[(int64_t)p * 2 * cols + c];
-  part[warp][lane] = s;
-  __syncthreads();
-  if (warp != 0 || c >= 2 * (int64_t)cols) return;
-  s = 0.f;
+// The same for rows of 1025 to 8192 columns of whole vectors, with the rows to come on their way:
+// a CTA has neighbouring rows, and every thread copies its own vectors of the next rows into its
+// own places of a ring in shared memory (asynchronous copies of 8 or 16 bytes; nothing is exchanged
+// through the ring, so it needs no barrier).  Statistics and scale bytes of kNormChunk rows are fetched
+// at once.
+constexpr int kNormChunk = 32;
+
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+  if constexpr (BYTES == 8) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+  } else {
 #pragma unroll
-  for (int w = 0; w < 8; ++w) s += part[w][lane];
-  if (c < cols) { if (dgamma) dgamma[c] = s; }
-  else if (dbeta) dbeta[c - cols] = s;
+    for (int i = 0; i < BYTES; i += 16)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + i), "l"(static_cast<const uint8_t*>(src) + i) : "memory");
+  }
+}
+
+// Bytes of shared memory: the ring, then scale bytes and statistics of a chunk of rows.
+__host__ __device__ constexpr int norm_ring_row(int x_bytes, int y_bytes, int threads, int j) {
+  return threads * j * 8 * (x_bytes + y_bytes);
+}
+
+template <int XT, int YT, int J>
+__global__ void __launch_bounds__(512, J == 1 ? 2 : 1)
+layer_norm_bprop_ring_kernel(const __grid_constant__ LayerNormArgs args, int depth) {
+  typedef typename ElemOf<XT>::T TX;
+  typedef typename ElemOf<YT>::T TY;
+  constexpr int XB = 8 * (int)sizeof(TX), YB = 8 * (int)sizeof(TY);
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ float slots[2][2][16];
+  __shared__ float stats[2][kNormChunk];
+  const int t = threadIdx.x, threads = blockDim.x, lane = t & 31, warp = t >> 5, warps = threads >> 5;
+  const int row_bytes = norm_ring_row((int)sizeof(TX), (int)sizeof(TY), threads, J);
+  uint8_t* scales = ring + (size_t)depth * row_bytes;      // [block][row of the chunk]
+  const int blocks = (args.cols + kBlock8 - 1) / kBlock8;
+  const int64_t r0 = (int64_t)args.rows * blockIdx.x / gridDim.x, r1 = (int64_t)args.rows * (blockIdx.x + 1) / gridDim.x;
+  const TX* x = static_cast<const TX*>(args.x);
+  const TY* dy = static_cast<const TY*>(args.dy);
+  TY* dx = static_cast<TY*>(args.dx);
+  // this thread's places in a ring slot: J x values, then J dy values
+  auto x_at = [&](int slot, int j) { return (size_t)slot * row_bytes + (size_t)(j * threads + t) * XB; };
+  auto y_at = [&](int slot, int j) {
+    return (size_t)slot * row_bytes + (size_t)J * threads * XB + (size_t)(j * threads + t) * YB;
+  };
+  const uint32_t ring_u = smem_u32(ring);
+  auto fetch = [&](int64_t r, int slot) {
+    if (r < r1) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const int c = 8 * (t + threads * j);
+        if (c < args.cols) {
+          copy_async<XB>(ring_u + (uint32_t)x_at(slot, j), x + r * args.ldx + c);
+          copy_async<YB>(ring_u + (uint32_t)y_at(slot, j), dy + r * args.ldy + c);
+        }
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  F2 g[J][4], dg[J][4], db[J][4];
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int c = 8 * (t + threads * j);
+    load_weights8<true>(args.gamma, c, c < args.cols ? 8 : 0, args.w_type, args.vec_w != 0, 1.f, g[j]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dg[j][i] = db[j][i] = 0;
+  }
+  for (int d = 0; d < depth - 1; ++d) fetch(r0 + d, d);
+  int flip = 0, slot = 0;
+  for (int64_t chunk = r0; chunk < r1; chunk += kNormChunk) {
+    const int in_chunk = (int)(r1 - chunk < kNormChunk ? r1 - chunk : kNormChunk);
+    __syncthreads();           // the last chunk's statistics have been read
+    if (t < in_chunk) {
+      stats[0][t] = args.mean[chunk + t];
+      stats[1][t] = args.rstd[chunk + t];
+    }
+    if constexpr (is_fp8(XT)) {
+      for (int i = t; i < blocks * kNormChunk; i += threads) {
+        const int row = i % kNormChunk;
+        if (row < in_chunk) scales[i] = args.x_scale[(int64_t)(i / kNormChunk) * args.rows + chunk + row];
+      }
+    }
+    __syncthreads();
+    for (int k = 0; k < in_chunk; ++k, flip ^= 1) {
+      // the copies of the row `depth - 1` ahead go where the row before this one was
+      const int64_t r = chunk + k;
+      fetch(r + depth - 1, slot == 0 ? depth - 1 : slot - 1);
+      if (depth == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+      else if (depth == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+      else asm volatile("cp.async.wait_group 1;" ::: "memory");
+      const float mean = stats[0][k], rstd = stats[1][k];
+      F2 xh[J][4], e[J][4], p1 = 0, p2 = 0;
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const int c = 8 * (t + threads * j);
+        Raw8<XT> rx = {};
+        Raw8<YT> rdy = {};
+        float scale = 0.f;
+        if (c < args.cols) {
+          rx = *reinterpret_cast<const Raw8<XT>*>(ring + x_at(slot, j));
+          rdy = *reinterpret_cast<const Raw8<YT>*>(ring + y_at(slot, j));
+          if constexpr (is_fp8(XT)) scale = e8m0_value(scales[(c >> 7) * kNormChunk + k]);
+        }
+        norm_back8<XT, YT, false>(rx, rdy, scale, mean, rstd, g[j], 8, xh[j], e[j], dg[j], db[j], &p1, &p2);
+      }
+      float s1 = warp_sum(sum2(p1)), s2 = warp_sum(sum2(p2));
+      if (lane == 0) {
+        slots[flip][0][warp] = s1;
+        slots[flip][1][warp] = s2;
+      }
+      __syncthreads();
+      s1 = s2 = 0.f;
+      for (int w = 0; w < warps; ++w) {
+        s1 += slots[flip][0][w];
+        s2 += slots[flip][1][w];
+      }
+      s1 *= args.inv_cols;
+      s2 *= args.inv_cols;
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const int c = 8 * (t + threads * j);
+        F2 o[4];
+        norm_dx8(xh[j], e[j], rstd, s1, s2, o);
+        store_pairs<YT, false>(dx + r * args.ldy + c, o, c < args.cols ? 8 : 0, true);
+      }
+      slot = slot + 1 == depth ? 0 : slot + 1;
+    }
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  if (!args.partial) return;
+  float* out = args.partial + (int64_t)blockIdx.x * 2 * args.cols;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int c = 8 * (t + threads * j);
+    if (c >= args.cols) continue;
+    float a[8], b[8];
+    to_floats(dg[j], a);
+    to_floats(db[j], b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      out[c + i] = a[i];
+      out[(int64_t)args.cols + c + i] = b[i];
+    }
+  }
+}
+
+// dg and db from the CTAs' sums, in CTA order.  A CTA takes 32 of the 2 x cols columns; each of its
+// 16 warps takes every sixteenth sum, four at a time, and the warps' results are added in warp order.
+__global__ void __launch_bounds__(512) layer_norm_fold_kernel(const float* partial, int parts, int cols,
+                                                              float* dgamma, float* dbeta) {
+  __shared__ float part[16][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t c = (int64_t)blockIdx.x * 32 + lane, pitch = 2 * (int64_t)cols;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (c < pitch) {
+    const float* at = partial + c;
+    int p = warp;
+    for (; p + 48 < parts; p += 64) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] += at[(int64_t)(p + 16 * i) * pitch];
+    }
+    for (; p < parts; p += 16) s[0] += at[(int64_t)p * pitch];
+  }
+  part[warp][lane] = (s[0] + s[1]) + (s[2] + s[3]);
+  __syncthreads();
+  if (warp != 0 || c >= pitch) return;
+  float total = 0.f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) total += part[w][lane];
+  if (c < cols) { if (dgamma) dgamma[c] = total; }
+  else if (dbeta) dbeta[c - cols] = total;
 }
 
 // Rows too long for the registers of a CTA: the same sums with the row read again for each (it
 // comes from the second-level cache).  One CTA of 1024 threads per row, 8192 columns at a time.
 template <int XT>
 __global__ void __launch_bounds__(1024) layer_norm_fprop_long_kernel(const __grid_constant__ LayerNormArgs args) {
-  constexpr bool EDGE = true;
   typedef typename ElemOf<XT>::T T;
   __shared__ float slots[2][kNormMaxWarps];
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -310,30 +524,26 @@ __global__ void __launch_bounds__(1024) layer_norm_fprop_long_kernel(const __gri
       for (int j = 0; j < steps; ++j) {
         const int c = 8 * t + 8192 * j;
         const int n = min(max(args.cols - c, 0), 8);
-        float v[8];
-        to_float8<XT>(load_raw8<XT, EDGE>(x + r * args.ldx + c, n, args.vec_x != 0), v);
+        F2 v[4];
+        to_pairs<XT>(load_raw8<XT, true>(x + r * args.ldx + c, n, args.vec_x != 0), v);
         if (pass == 0) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) acc += v[i];
+          acc += sum2(add2(add2(v[0], v[1]), add2(v[2], v[3])));
         } else if (pass == 1) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float d = i < n ? v[i] - mean : 0.f;
-            acc = fmaf(d, d, acc);
-          }
+          acc += squares8<true>(v, f2(-mean), n);
         } else {
-          if (args.c) norm_pack<EDGE>(v, args.q_e5m2, args.c + r * args.ldq + c, args.sc + (int64_t)(c >> 7) * args.rows + r, n, lane);
-          float g[8], b[8];
-          load_weights8<EDGE>(args.gamma, c, n, args.w_type, args.vec_w != 0, 1.f, g);
-          load_weights8<EDGE>(args.beta, c, n, args.w_type, args.vec_w != 0, 0.f, b);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = (EDGE ? i < n : n > 0) ? fmaf((v[i] - mean) * rstd, g[i], b[i]) : 0.f;
-          if (args.y) store_float8<XT, EDGE>(y + r * args.ldy + c, v, n, args.vec_y != 0);
-          if (args.q) norm_pack<EDGE>(v, args.q_e5m2, args.q + r * args.ldq + c, args.s + (int64_t)(c >> 7) * args.rows + r, n, lane);
+          if (args.c)
+            norm_pack<kEitherFp8, true>(v, args.q_e5m2, args.c + r * args.ldq + c, args.sc + (int64_t)(c >> 7) * args.rows + r, n, lane);
+          F2 g[4], b[4];
+          load_weights8<true>(args.gamma, c, n, args.w_type, args.vec_w != 0, 1.f, g);
+          load_weights8<true>(args.beta, c, n, args.w_type, args.vec_w != 0, 0.f, b);
+          normalise8<true>(v, f2(-mean), f2(rstd), g, b, n);
+          if (args.y) store_pairs<XT, true>(y + r * args.ldy + c, v, n, args.vec_y != 0);
+          if (args.q)
+            norm_pack<kEitherFp8, true>(v, args.q_e5m2, args.q + r * args.ldq + c, args.s + (int64_t)(c >> 7) * args.rows + r, n, lane);
         }
       }
       if (pass == 2) break;
-      acc = row_sum<false>(acc, slots[pass], 32, lane, warp) * args.inv_cols;
+      acc = cta_sum(acc, slots[pass], lane, warp) * args.inv_cols;
       if (pass == 0) mean = acc;
       else rstd = 1.f / sqrtf(acc + args.eps);
       acc = 0.f;

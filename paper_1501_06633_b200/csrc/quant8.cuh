@@ -6,7 +6,8 @@
 // (8 (t mod 16)) of the eight rows t/16 + 16 k, as they lie in memory: 16 lanes cover a row
 // block, and eight loads of 16 bytes are in flight in each thread.  Row maxima are shuffles over
 // those 16 lanes; column maxima are a maximum over the thread's rows, a shuffle between the two
-// halves of the warp and one pass through shared memory.
+// halves of the warp and one pass through shared memory.  The values are converted again for each
+// form instead of being kept as fp32 (64 registers of a thread).
 #pragma once
 #include "fp8_util.cuh"
 
@@ -22,10 +23,9 @@ struct Quant8Args {
   int32_t rows, cols;
   int32_t col_blocks;          // blocks of 128 columns
   int32_t vec_x;               // rows of x allow the wide load
-  int32_t e5m2;
 };
 
-template <int XT, bool EDGE>
+template <int XT, int QT, bool EDGE>
 __global__ void __launch_bounds__(kQuantThreads) quant8_kernel(const __grid_constant__ Quant8Args args) {
   typedef typename ElemOf<XT>::T T;
   __shared__ float col_part[kQuantThreads / 32][kBlock8];   // per warp: maxima of its rows
@@ -49,77 +49,97 @@ __global__ void __launch_bounds__(kQuantThreads) quant8_kernel(const __grid_cons
       xs[k] = r < args.rows ? e8m0_value(args.x_scale[(int64_t)cb * args.rows + r]) : 0.f;
   }
   // the eight values of one of the thread's rows
-  auto values = [&](int k, float (&v)[8]) {
-    to_float8<XT>(raw[k], v);
+  auto values = [&](int k, F2 (&v)[4]) {
+    convert_again(raw[k]);
+    to_pairs<XT>(raw[k], v);
     if constexpr (is_fp8(XT)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= xs[k];
+      for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], f2(xs[k]));
     }
   };
+  const bool cols_wanted = args.q_col || args.q_tile;
   float row_max[8], col_max[8];
-  bool inf = false;
 #pragma unroll
   for (int i = 0; i < 8; ++i) col_max[i] = 0.f;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    float v[8];
+  for (int k = 0; k < 8; k += 2) {
+    F2 v[4], w[4];
     values(k, v);
+    values(k + 1, w);
     row_max[k] = max8(v);
-    inf |= isinf(row_max[k]);
+    row_max[k + 1] = max8(w);
+    if (cols_wanted) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) col_max[i] = fmaxf(col_max[i], fabsf(v[i]));
+      for (int i = 0; i < 4; ++i) {
+        const float2 a = unf2(v[i]), b = unf2(w[i]);
+        col_max[2 * i] = max3abs(col_max[2 * i], a.x, b.x);
+        col_max[2 * i + 1] = max3abs(col_max[2 * i + 1], a.y, b.y);
+      }
+    }
   }
-  const bool fix = __syncthreads_or(inf) != 0;   // rare: a tile that holds an infinity
+  float most = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) most = fmaxf(most, row_max[k]);
+  const bool fix = __syncthreads_or(isinf(most)) != 0;   // rare: a tile that holds an infinity
   if (fix) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) col_max[i] = 0.f;
-#pragma unroll
+#pragma unroll 1
     for (int k = 0; k < 8; ++k) {
-      float v[8];
-      values(k, v);
-      row_max[k] = finite_max8(v);
+      // one row at a time, from memory again: registers cannot be indexed
+      const int r = r0 + rg + 16 * k;
+      float f[8];
+      to_float8<XT>(load_raw8<XT, true>(x + (int64_t)r * args.ldx + c0, r < args.rows ? n : 0, args.vec_x != 0), f);
+      float scale = 1.f, m = 0.f;
+      if constexpr (is_fp8(XT)) scale = r < args.rows ? e8m0_value(args.x_scale[(int64_t)cb * args.rows + r]) : 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) col_max[i] = fmaxf(col_max[i], isinf(v[i]) ? 0.f : fabsf(v[i]));
+      for (int i = 0; i < 8; ++i) {
+        const float a = is_fp8(XT) ? f[i] * scale : f[i];
+        const float b = isinf(a) ? 0.f : fabsf(a);
+        m = fmaxf(m, b);
+        col_max[i] = fmaxf(col_max[i], b);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) row_max[j] = j == k ? m : row_max[j];
     }
   }
 
-  auto store = [&](uint8_t* q, int k, float inv_row, const float* inv_col) {
+  auto store = [&](uint8_t* q, int k, const F2 (&inv)[4]) {
     const int r = r0 + rg + 16 * k;
     if (r >= args.rows) return;
-    float v[8];
+    F2 v[4];
     values(k, v);
-    if (inv_col) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = isinf(v[i]) ? v[i] : v[i] * inv_col[i];
-    }
-    store_bytes8<EDGE>(q + (int64_t)r * args.ldq + c0, pack8_as(v, inv_row, fix, args.e5m2 != 0), n, true);
+    store_bytes8<EDGE>(q + (int64_t)r * args.ldq + c0, pack8<QT>(v, inv, fix), n, true);
   };
 
   if (args.q_row) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const uint32_t b = scale_byte_of(max_over_block_lanes(row_max[k]), args.e5m2 != 0);
+      const uint32_t b = scale_byte<QT>(max_over_block_lanes(row_max[k]));
       if ((t & 15) == 0) row_byte[rg + 16 * k] = (uint8_t)b;
-      store(args.q_row, k, inv_scale_of(b), nullptr);
+      const F2 inv = f2(inv_scale_of(b)), all[4] = {inv, inv, inv, inv};
+      store(args.q_row, k, all);
     }
   }
-  if (args.q_col || args.q_tile) {
+  if (cols_wanted) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) col_max[i] = fmaxf(col_max[i], __shfl_xor_sync(0xFFFFFFFFu, col_max[i], 16));
     if (lane < 16) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) col_part[warp][8 * lane + i] = col_max[i];
+      for (int i = 0; i < 8; i += 4)
+        *reinterpret_cast<float4*>(&col_part[warp][8 * lane + i]) =
+            make_float4(col_max[i], col_max[i + 1], col_max[i + 2], col_max[i + 3]);
     }
   }
   __syncthreads();
   if (args.q_row && t < kBlock8 && r0 + t < args.rows)
     args.s_row[(int64_t)cb * args.rows + r0 + t] = row_byte[t];
-  if (!args.q_col && !args.q_tile) return;
+  if (!cols_wanted) return;
   if (t < kBlock8) {
     float m = 0.f;
 #pragma unroll
     for (int w = 0; w < kQuantThreads / 32; ++w) m = fmaxf(m, col_part[w][t]);
-    const uint32_t b = scale_byte_of(m, args.e5m2 != 0);
+    const uint32_t b = scale_byte<QT>(m);
     col_inv[t] = inv_scale_of(b);
     if (args.q_col && cb * kBlock8 + t < args.cols)
       args.s_col[(int64_t)rb * args.cols + cb * kBlock8 + t] = (uint8_t)b;
@@ -129,17 +149,20 @@ __global__ void __launch_bounds__(kQuantThreads) quant8_kernel(const __grid_cons
   }
   __syncthreads();
   if (args.q_col) {
-    float inv[8];
+    F2 inv[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) inv[i] = col_inv[8 * (t & 15) + i];
+    for (int i = 0; i < 4; ++i) {
+      const float2 c = *reinterpret_cast<const float2*>(&col_inv[8 * (t & 15) + 2 * i]);
+      inv[i] = f2(c.x, c.y);
+    }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) store(args.q_col, k, 1.f, inv);
+    for (int k = 0; k < 8; ++k) store(args.q_col, k, inv);
   }
   if (args.q_tile) {
-    const float m = fmaxf(fmaxf(warp_max[0], warp_max[1]), fmaxf(warp_max[2], warp_max[3]));
-    const uint32_t b = scale_byte_of(m, args.e5m2 != 0);
+    const uint32_t b = scale_byte<QT>(fmaxf(fmaxf(warp_max[0], warp_max[1]), fmaxf(warp_max[2], warp_max[3])));
+    const F2 inv = f2(inv_scale_of(b)), all[4] = {inv, inv, inv, inv};
 #pragma unroll
-    for (int k = 0; k < 8; ++k) store(args.q_tile, k, inv_scale_of(b), nullptr);
+    for (int k = 0; k < 8; ++k) store(args.q_tile, k, all);
     if (t == 0) args.s_tile[(int64_t)rb * args.col_blocks + cb] = (uint8_t)b;
   }
 }

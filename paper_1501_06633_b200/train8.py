@@ -113,7 +113,8 @@ def _library():
         # what torch.cuda.current_device() and current_stream().cuda_stream return, without the
         # objects around them: a small layer's call is bound by the host
         _current_device, _current_raw_stream = torch.cuda.current_device, _raw_stream
-        if hasattr(torch._C, "_cuda_getDevice") and hasattr(torch._C, "_cuda_getCurrentRawStream"):
+        if (torch.cuda.is_available() and hasattr(torch._C, "_cuda_getDevice")
+                and hasattr(torch._C, "_cuda_getCurrentRawStream")):
             torch.cuda.init()
             _current_device, _current_raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
         _TYPES = ((torch.float32,), (torch.bfloat16,), (torch.float16,),
