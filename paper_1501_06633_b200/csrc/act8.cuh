@@ -55,13 +55,22 @@ __device__ __forceinline__ void activation(float g, float* f, float* df) {
   }
 }
 
-// Packs eight values of a row block; returns the scale byte.
+// Packs eight values each of two row blocks and keeps their scale bytes (null: nowhere).
 template <int QT, bool EDGE>
-__device__ __forceinline__ uint32_t pack_row8(const F2 (&v)[4], uint8_t* p, int n, bool vec, bool live) {
-  bool fix;
-  const uint32_t byte = block_byte<QT>(v, &fix);
-  if (live) store_bytes8<EDGE>(p, pack8<QT>(v, inv_scale_of(byte), fix), n, vec);
-  return byte;
+__device__ __forceinline__ void pack_rows8(const F2 (&v)[4], const F2 (&w)[4], uint8_t* pv, uint8_t* pw, int n, bool vec_v,
+                                           bool vec_w, bool live_v, bool live_w, uint8_t* sv, uint8_t* sw, bool first) {
+  uint32_t bv, bw;
+  bool fv = false, fw = false;
+  if (block_bytes<QT>(max8(v), max8(w), &bv, &bw)) {
+    bv = exact_byte<QT>(v, &fv);
+    bw = exact_byte<QT>(w, &fw);
+  }
+  if (live_v) store_bytes8<EDGE>(pv, pack8<QT>(v, inv_scale_of(bv), fv), n, vec_v);
+  if (live_w) store_bytes8<EDGE>(pw, pack8<QT>(w, inv_scale_of(bw), fw), n, vec_w);
+  if (first) {
+    *sv = (uint8_t)bv;
+    *sw = (uint8_t)bw;
+  }
 }
 
 template <int XT, int QT, int ACT, bool GATED, bool EDGE>
@@ -72,7 +81,7 @@ __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_co
   const int cb = blockIdx.x % args.col_blocks;
   const int rb = blockIdx.x / args.col_blocks;
   const int r0 = rb * kActRows, c0 = cb * kBlock8 + 8 * (t & 15);
-  const int n = min(max(args.cols - c0, 0), 8);
+  const int n = vector_cols<EDGE>(args.cols, c0);
   const T* h = static_cast<const T*>(args.h);
   Raw8<XT> rg[4], ru[GATED ? 4 : 1];
 #pragma unroll
@@ -82,39 +91,53 @@ __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_co
     rg[k] = load_raw8<XT, EDGE>(h + (int64_t)r * args.ldh + c0, nr, args.vec_h != 0);
     if constexpr (GATED) ru[k] = load_raw8<XT, EDGE>(h + (int64_t)r * args.ldh + args.cols + c0, nr, args.vec_u != 0);
   }
+  const bool first = (t & 15) == 0;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int r = r0 + (t >> 4) + 16 * k;
-    const bool live = r < args.rows && n > 0;
-    F2 v[4];
-    float g[8], u[8], a[8];
-    to_pairs<XT>(rg[k], v);
-    to_floats(v, g);
+  for (int k = 0; k < 4; k += 2) {       // two rows at a time: their blocks share the shuffles
+    const int row = (t >> 4) + 16 * k, r = r0 + row;
+    const bool live[2] = {r < args.rows && n > 0, r + 16 < args.rows && n > 0};
+    F2 v[2][4];
+    float g[2][8], u[2][8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      to_pairs<XT>(rg[k + i], v[i]);
+      to_floats(v[i], g[i]);
+    }
     if (args.c) {
-      const uint32_t b = pack_row8<QT, EDGE>(v, args.c + (int64_t)r * args.ldc + c0, n, true, live);
-      if ((t & 15) == 0) bytes[1][(t >> 4) + 16 * k] = (uint8_t)b;
+      uint8_t* c = args.c + (int64_t)r * args.ldc + c0;
+      pack_rows8<QT, EDGE>(v[0], v[1], c, c + 16 * args.ldc, n, true, true, live[0], live[1], &bytes[1][row],
+                           &bytes[1][row + 16], first);
     }
     if constexpr (GATED) {
-      to_pairs<XT>(ru[k], v);
-      to_floats(v, u);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        to_pairs<XT>(ru[k + i], v[i]);
+        to_floats(v[i], u[i]);
+      }
       if (args.c) {
-        const uint32_t b = pack_row8<QT, EDGE>(v, args.c + (int64_t)r * args.ldc + args.cols + c0, n, args.vec_cu != 0, live);
-        if ((t & 15) == 0) bytes[2][(t >> 4) + 16 * k] = (uint8_t)b;
+        uint8_t* c = args.c + (int64_t)r * args.ldc + args.cols + c0;
+        pack_rows8<QT, EDGE>(v[0], v[1], c, c + 16 * args.ldc, n, args.vec_cu != 0, args.vec_cu != 0, live[0], live[1],
+                             &bytes[2][row], &bytes[2][row + 16], first);
       }
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float f, unused;
-      activation<ACT, false>(g[i], &f, &unused);
-      a[i] = GATED ? f * u[i] : f;
-    }
-    if (args.a && live)
-      store_float8<XT, EDGE>(static_cast<T*>(args.a) + (int64_t)r * args.lda + c0, a, n, args.vec_a != 0);
-    if (args.q) {
+    for (int i = 0; i < 2; ++i) {
+      float a[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = f2(a[2 * i], a[2 * i + 1]);
-      const uint32_t b = pack_row8<QT, EDGE>(v, args.q + (int64_t)r * args.ldq + c0, n, true, live);
-      if ((t & 15) == 0) bytes[0][(t >> 4) + 16 * k] = (uint8_t)b;
+      for (int e = 0; e < 8; ++e) {
+        float f, unused;
+        activation<ACT, false>(g[i][e], &f, &unused);
+        a[e] = GATED ? f * u[i][e] : f;
+      }
+      if (args.a && live[i])
+        store_float8<XT, EDGE>(static_cast<T*>(args.a) + (int64_t)(r + 16 * i) * args.lda + c0, a, n, args.vec_a != 0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i][e] = f2(a[2 * e], a[2 * e + 1]);
+    }
+    if (args.q) {
+      uint8_t* q = args.q + (int64_t)r * args.ldq + c0;
+      pack_rows8<QT, EDGE>(v[0], v[1], q, q + 16 * args.ldq, n, true, true, live[0], live[1], &bytes[0][row],
+                           &bytes[0][row + 16], first);
     }
   }
   __syncthreads();
@@ -136,7 +159,7 @@ __global__ void __launch_bounds__(kActThreads) act8_bprop_kernel(const __grid_co
   const int cb = blockIdx.x % args.col_blocks;
   const int rb = blockIdx.x / args.col_blocks;
   const int r0 = rb * kActRows + (t >> 4), c0 = cb * kBlock8 + 8 * (t & 15);
-  const int n = min(max(args.cols - c0, 0), 8);
+  const int n = vector_cols<EDGE>(args.cols, c0);
   if (n == 0) return;
   const TH* h = static_cast<const TH*>(args.h);
   const int64_t ldh = is_fp8(HT) ? args.ldc : args.ldh;

@@ -176,14 +176,35 @@ static __device__ __noinline__ float finite_max8(F2 v0, F2 v1, F2 v2, F2 v3) {
   }
   return m;
 }
-// The scale byte of a row block whose lanes hold eight values each (16 lanes); *fix: it holds an
-// infinity.  All lanes of the warp take part.
+// The scale bytes of two row blocks from the largest magnitudes of their lanes (16 lanes each, all
+// lanes of the warp take part).  The exponent of a block's largest magnitude is the largest of its
+// lanes' (rounded up where the mantissa is above 1.75: monotonic), so two blocks' exponents go
+// through the shuffles as halves of one word.  rare: a block has exponent 0 (zeros or subnormals)
+// or 255 (an infinity, or values near the largest); the caller then takes exact_byte.
 template <int QT>
-__device__ __forceinline__ uint32_t block_byte(const F2 (&v)[4], bool* fix) {
-  float m = max_over_block_lanes(max8(v));
-  *fix = isinf(m);
-  if (__any_sync(0xFFFFFFFFu, *fix)) m = max_over_block_lanes(finite_max8(v[0], v[1], v[2], v[3]));
-  return scale_byte<QT>(m);
+__device__ __forceinline__ bool block_bytes(float m0, float m1, uint32_t* b0, uint32_t* b1) {
+  constexpr uint32_t kTop = QT == MAXDNN_E4M3 ? 8 : 15;
+  const uint32_t e0 = (__float_as_uint(m0) + 0x1FFFFFu) >> 23, e1 = (__float_as_uint(m1) + 0x1FFFFFu) >> 23;
+  uint32_t e = e0 | (e1 << 16);
+#pragma unroll
+  for (int d = kLanesPerBlock / 2; d > 0; d >>= 1) e = __vmaxu2(e, __shfl_xor_sync(0xFFFFFFFFu, e, d));
+  const uint32_t lo = e & 0xFFFFu, hi = e >> 16;
+  *b0 = (uint32_t)max((int)(lo - kTop), 1);
+  *b1 = (uint32_t)max((int)(hi - kTop), 1);
+  return __any_sync(0xFFFFFFFFu, lo - 1u >= 254u || hi - 1u >= 254u);
+}
+
+// The byte of one block from its lanes' values themselves; *fix: it holds an infinity.
+template <int QT>
+__device__ __forceinline__ uint32_t exact_byte(const F2 (&v)[4], bool* fix) {
+  *fix = isinf(max_over_block_lanes(max8(v)));
+  return scale_byte<QT>(max_over_block_lanes(finite_max8(v[0], v[1], v[2], v[3])));
+}
+
+// Columns of a vector of eight that starts at column c.
+template <bool EDGE>
+__device__ __forceinline__ int vector_cols(int cols, int c) {
+  return EDGE ? min(max(cols - c, 0), 8) : c < cols ? 8 : 0;
 }
 
 // ---- eight neighbouring values as they lie in memory ----

@@ -42,23 +42,32 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Packs eight values of a row block (16 lanes) and stores them with the block's scale.  QT: the
-// 8-bit type, or kEitherFp8: `e5m2` tells.
+// Packs eight values each of two row blocks (16 lanes) and stores them with the blocks' scales.
+template <int QT, bool EDGE>
+__device__ __forceinline__ void norm_pack_as(const F2 (&v)[4], const F2 (&w)[4], uint8_t* qv, uint8_t* qw, uint8_t* sv,
+                                             uint8_t* sw, int nv, int nw, int lane) {
+  uint32_t bv, bw;
+  bool fv = false, fw = false;
+  if (block_bytes<QT>(max8(v), max8(w), &bv, &bw)) {
+    bv = exact_byte<QT>(v, &fv);
+    bw = exact_byte<QT>(w, &fw);
+  }
+  store_bytes8<EDGE>(qv, pack8<QT>(v, inv_scale_of(bv), fv), nv, true);
+  store_bytes8<EDGE>(qw, pack8<QT>(w, inv_scale_of(bw), fw), nw, true);
+  if ((lane & 15) == 0) {
+    if (nv > 0) *sv = (uint8_t)bv;
+    if (nw > 0) *sw = (uint8_t)bw;
+  }
+}
+// QT: the 8-bit type, or kEitherFp8: `e5m2` tells.
 constexpr int kEitherFp8 = 0;
 template <int QT, bool EDGE>
-__device__ __forceinline__ void norm_pack(const F2 (&v)[4], bool e5m2, uint8_t* q, uint8_t* s, int n, int lane) {
-  bool fix;
-  uint32_t byte;
-  uint2 w;
-  if (QT == MAXDNN_E5M2 || (QT == kEitherFp8 && e5m2)) {
-    byte = block_byte<MAXDNN_E5M2>(v, &fix);
-    w = pack8<MAXDNN_E5M2>(v, inv_scale_of(byte), fix);
-  } else {
-    byte = block_byte<MAXDNN_E4M3>(v, &fix);
-    w = pack8<MAXDNN_E4M3>(v, inv_scale_of(byte), fix);
-  }
-  store_bytes8<EDGE>(q, w, n, true);
-  if ((lane & 15) == 0 && n > 0) *s = (uint8_t)byte;
+__device__ __forceinline__ void norm_pack(const F2 (&v)[4], const F2 (&w)[4], bool e5m2, uint8_t* qv, uint8_t* qw,
+                                          uint8_t* sv, uint8_t* sw, int nv, int nw, int lane) {
+  if (QT == MAXDNN_E5M2 || (QT == kEitherFp8 && e5m2))
+    norm_pack_as<MAXDNN_E5M2, EDGE>(v, w, qv, qw, sv, sw, nv, nw, lane);
+  else
+    norm_pack_as<MAXDNN_E4M3, EDGE>(v, w, qv, qw, sv, sw, nv, nw, lane);
 }
 
 // Eight neighbouring weights.
@@ -141,7 +150,7 @@ layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int c = 8 * (t + 32 * WR * j);
-      raw[j] = load_raw8<XT, EDGE>(x + r * args.ldx + c, min(max(args.cols - c, 0), 8), args.vec_x != 0);
+      raw[j] = load_raw8<XT, EDGE>(x + r * args.ldx + c, vector_cols<EDGE>(args.cols, c), args.vec_x != 0);
     }
     F2 sum = 0;
 #pragma unroll
@@ -158,30 +167,48 @@ layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
       F2 v[4];
       convert_again(raw[j]);
       to_pairs<XT>(raw[j], v);
-      sq += squares8<EDGE>(v, minus_mean, min(max(args.cols - 8 * (t + 32 * WR * j), 0), 8));
+      sq += squares8<EDGE>(v, minus_mean, vector_cols<EDGE>(args.cols, 8 * (t + 32 * WR * j)));
     }
     const float rstd = 1.f / sqrtf(total(sq, 1) * args.inv_cols + args.eps);
     if (t == 0) {
       if (args.mean) args.mean[r] = mean;
       if (args.rstd) args.rstd[r] = rstd;
     }
+    // two vectors at a time (J = 1: one, with zeros for the other)
+    constexpr int kPair = J > 1 ? 2 : 1, kStep = 256 * WR;
+    const int c0 = 8 * t;
+    const int64_t scale_step = (int64_t)(kStep / kBlock8) * args.rows;
+    uint8_t* cp = args.c ? args.c + r * args.ldq + c0 : nullptr;
+    uint8_t* qp = args.q ? args.q + r * args.ldq + c0 : nullptr;
+    uint8_t* scp = args.sc + (int64_t)(c0 >> 7) * args.rows + r;
+    uint8_t* sqp = args.s + (int64_t)(c0 >> 7) * args.rows + r;
+    T* yp = y ? y + r * args.ldy + c0 : nullptr;
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int c = 8 * (t + 32 * WR * j);
-      const int n = min(max(args.cols - c, 0), 8);
-      F2 v[4];
-      convert_again(raw[j]);
-      to_pairs<XT>(raw[j], v);
+    for (int j = 0; j < J; j += kPair) {
+      F2 v[2][4] = {};
+      int n[2] = {0, 0};
+#pragma unroll
+      for (int i = 0; i < kPair; ++i) {
+        n[i] = vector_cols<EDGE>(args.cols, c0 + kStep * (j + i));
+        convert_again(raw[j + i]);
+        to_pairs<XT>(raw[j + i], v[i]);
+      }
       if (args.c)
-        norm_pack<QT, EDGE>(v, args.q_e5m2, args.c + r * args.ldq + c, args.sc + (int64_t)(c >> 7) * args.rows + r, n, lane);
+        norm_pack<QT, EDGE>(v[0], v[1], args.q_e5m2, cp + kStep * j, cp + kStep * (j + 1), scp + scale_step * j,
+                            scp + scale_step * (j + 1), n[0], n[1], lane);
       if (!args.y && !args.q) continue;
-      F2 g[4], b[4];
-      load_weights8<EDGE>(args.gamma, c, n, args.w_type, args.vec_w != 0, 1.f, g);
-      load_weights8<EDGE>(args.beta, c, n, args.w_type, args.vec_w != 0, 0.f, b);
-      normalise8<EDGE>(v, minus_mean, f2(rstd), g, b, n);
-      if (args.y) store_pairs<XT, EDGE>(y + r * args.ldy + c, v, n, args.vec_y != 0);
+#pragma unroll
+      for (int i = 0; i < kPair; ++i) {
+        const int c = c0 + kStep * (j + i);
+        F2 g[4], b[4];
+        load_weights8<EDGE>(args.gamma, c, n[i], args.w_type, args.vec_w != 0, 1.f, g);
+        load_weights8<EDGE>(args.beta, c, n[i], args.w_type, args.vec_w != 0, 0.f, b);
+        normalise8<EDGE>(v[i], minus_mean, f2(rstd), g, b, n[i]);
+        if (args.y) store_pairs<XT, EDGE>(yp + kStep * (j + i), v[i], n[i], args.vec_y != 0);
+      }
       if (args.q)
-        norm_pack<QT, EDGE>(v, args.q_e5m2, args.q + r * args.ldq + c, args.s + (int64_t)(c >> 7) * args.rows + r, n, lane);
+        norm_pack<QT, EDGE>(v[0], v[1], args.q_e5m2, qp + kStep * j, qp + kStep * (j + 1), sqp + scale_step * j,
+                            sqp + scale_step * (j + 1), n[0], n[1], lane);
     }
     // no barrier here: a thread reaches the next row's first write of a slot only after the
     // second sum's barrier, which follows every read of the first slot (and the other way round)
@@ -358,16 +385,19 @@ __host__ __device__ constexpr int norm_ring_row(int x_bytes, int y_bytes, int th
   return threads * j * 8 * (x_bytes + y_bytes);
 }
 
-template <int XT, int YT, int J>
-__global__ void __launch_bounds__(512, J == 1 ? 2 : 1)
+// J vectors in each thread of WARPS warps.  Fewer threads with more columns each take fewer
+// instructions (the row's two sums are one exchange per warp), and more registers.
+template <int XT, int YT, int J, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, 16 / WARPS)
 layer_norm_bprop_ring_kernel(const __grid_constant__ LayerNormArgs args, int depth) {
   typedef typename ElemOf<XT>::T TX;
   typedef typename ElemOf<YT>::T TY;
   constexpr int XB = 8 * (int)sizeof(TX), YB = 8 * (int)sizeof(TY);
   extern __shared__ __align__(16) uint8_t ring[];
-  __shared__ float slots[2][2][16];
+  __shared__ __align__(16) float slots[2][2][WARPS];
   __shared__ float stats[2][kNormChunk];
-  const int t = threadIdx.x, threads = blockDim.x, lane = t & 31, warp = t >> 5, warps = threads >> 5;
+  constexpr int threads = 32 * WARPS;
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int row_bytes = norm_ring_row((int)sizeof(TX), (int)sizeof(TY), threads, J);
   uint8_t* scales = ring + (size_t)depth * row_bytes;      // [block][row of the chunk]
   const int blocks = (args.cols + kBlock8 - 1) / kBlock8;
@@ -440,17 +470,24 @@ layer_norm_bprop_ring_kernel(const __grid_constant__ LayerNormArgs args, int dep
         }
         norm_back8<XT, YT, false>(rx, rdy, scale, mean, rstd, g[j], 8, xh[j], e[j], dg[j], db[j], &p1, &p2);
       }
-      float s1 = warp_sum(sum2(p1)), s2 = warp_sum(sum2(p2));
-      if (lane == 0) {
-        slots[flip][0][warp] = s1;
-        slots[flip][1][warp] = s2;
-      }
+      // both sums in six shuffles: the halves of the warp take one each
+      float s1 = sum2(p1), s2 = sum2(p2);
+      const float other = __shfl_xor_sync(0xFFFFFFFFu, lane < 16 ? s2 : s1, 16);
+      float mine = (lane < 16 ? s1 : s2) + other;
+#pragma unroll
+      for (int d = 8; d > 0; d >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, d);
+      if ((lane & 15) == 0) slots[flip][lane >> 4][warp] = mine;
       __syncthreads();
-      s1 = s2 = 0.f;
-      for (int w = 0; w < warps; ++w) {
-        s1 += slots[flip][0][w];
-        s2 += slots[flip][1][w];
+      F2 t1 = 0, t2 = 0;
+#pragma unroll
+      for (int w = 0; w < WARPS; w += 4) {
+        const float4 a = *reinterpret_cast<const float4*>(&slots[flip][0][w]);
+        const float4 b = *reinterpret_cast<const float4*>(&slots[flip][1][w]);
+        t1 = add2(t1, add2(f2(a.x, a.y), f2(a.z, a.w)));
+        t2 = add2(t2, add2(f2(b.x, b.y), f2(b.z, b.w)));
       }
+      s1 = sum2(t1);
+      s2 = sum2(t2);
       s1 *= args.inv_cols;
       s2 *= args.inv_cols;
 #pragma unroll
@@ -524,7 +561,7 @@ __global__ void __launch_bounds__(1024) layer_norm_fprop_long_kernel(const __gri
       for (int j = 0; j < steps; ++j) {
         const int c = 8 * t + 8192 * j;
         const int n = min(max(args.cols - c, 0), 8);
-        F2 v[4];
+        F2 v[4], none[4] = {};
         to_pairs<XT>(load_raw8<XT, true>(x + r * args.ldx + c, n, args.vec_x != 0), v);
         if (pass == 0) {
           acc += sum2(add2(add2(v[0], v[1]), add2(v[2], v[3])));
@@ -532,14 +569,16 @@ __global__ void __launch_bounds__(1024) layer_norm_fprop_long_kernel(const __gri
           acc += squares8<true>(v, f2(-mean), n);
         } else {
           if (args.c)
-            norm_pack<kEitherFp8, true>(v, args.q_e5m2, args.c + r * args.ldq + c, args.sc + (int64_t)(c >> 7) * args.rows + r, n, lane);
+            norm_pack<kEitherFp8, true>(v, none, args.q_e5m2, args.c + r * args.ldq + c, nullptr,
+                                        args.sc + (int64_t)(c >> 7) * args.rows + r, nullptr, n, 0, lane);
           F2 g[4], b[4];
           load_weights8<true>(args.gamma, c, n, args.w_type, args.vec_w != 0, 1.f, g);
           load_weights8<true>(args.beta, c, n, args.w_type, args.vec_w != 0, 0.f, b);
           normalise8<true>(v, f2(-mean), f2(rstd), g, b, n);
           if (args.y) store_pairs<XT, true>(y + r * args.ldy + c, v, n, args.vec_y != 0);
           if (args.q)
-            norm_pack<kEitherFp8, true>(v, args.q_e5m2, args.q + r * args.ldq + c, args.s + (int64_t)(c >> 7) * args.rows + r, n, lane);
+            norm_pack<kEitherFp8, true>(v, none, args.q_e5m2, args.q + r * args.ldq + c, nullptr,
+                                        args.s + (int64_t)(c >> 7) * args.rows + r, nullptr, n, 0, lane);
         }
       }
       if (pass == 2) break;

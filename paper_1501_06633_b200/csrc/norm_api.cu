@@ -16,9 +16,9 @@ NormShape norm_shape(const maxdnn_layer_norm_desc& d) {
   if (cols <= 1024) return {32, 4, 0, 0};
   if (cols > 8192) return {0, 0, 0, 0};
   if (cols % 8 == 0 && vec_ok(d.x_type, d.ldx) && vec_ok(d.y_type, d.ldy)) {
-    const int t = cols <= 2048 ? 256 : 512, j = cols <= 4096 ? 1 : 2;
+    const int t = cols <= 2048 ? 128 : cols <= 4096 ? 256 : 512, j = 2;
     const int row = norm_ring_row(elem_bytes(d.x_type), elem_bytes(d.y_type), t, j);
-    const int room = t == 256 ? 48 * 1024 : j == 1 ? 100 * 1024 : 200 * 1024;    // of 227 KB, by CTAs per SM
+    const int room = t / 128 * 50 * 1024;    // of 227 KB: four, two or one CTA per SM
     const int depth = room / row;
     return {t, j, 1, depth < 2 ? 2 : depth > 4 ? 4 : depth};
   }
@@ -39,7 +39,7 @@ maxdnn_status check_layer_norm(const maxdnn_layer_norm_desc* d) {
 // CTAs of the backward pass: each leaves one row of sums.
 int norm_bprop_grid(const maxdnn_layer_norm_desc& d, int sm_count, const NormShape& s) {
   const int64_t units = s.threads == 32 ? ((int64_t)d.rows + 3) / 4 : d.rows;
-  const int per_sm = s.threads == 0 ? 1 : s.threads == 32 ? 4 : s.ring ? (s.j == 2 ? 1 : 1024 / s.threads) : s.threads >= 512 ? 1 : 512 / s.threads;
+  const int per_sm = s.threads == 0 ? 1 : s.threads == 32 ? 4 : s.ring ? 512 / s.threads : s.threads >= 512 ? 1 : 512 / s.threads;
   const int64_t most = (int64_t)sm_count * per_sm;
   return (int)(units < most ? units : most);
 }
@@ -186,14 +186,16 @@ maxdnn_status layer_norm_bprop(const maxdnn_layer_norm_desc* d, const void* dy, 
     if (sh.ring) {
       const int smem = sh.depth * norm_ring_row(elem_bytes(X), elem_bytes(Y), sh.threads, sh.j) +
                        (is_fp8(X) ? (int)blocks_of(d->cols) * kNormChunk : 0);
-      auto kern = sh.j == 1 ? layer_norm_bprop_ring_kernel<X, Y, 1> : layer_norm_bprop_ring_kernel<X, Y, 2>;
-      static std::atomic<bool> done[2][64];
-      if (!done[sh.j - 1][dev.index].load(std::memory_order_acquire)) {
+      auto kern = sh.threads == 128 ? layer_norm_bprop_ring_kernel<X, Y, 2, 4>
+                  : sh.threads == 256 ? layer_norm_bprop_ring_kernel<X, Y, 2, 8> : layer_norm_bprop_ring_kernel<X, Y, 2, 16>;
+      static std::atomic<bool> done[3][64];
+      const int slot = sh.threads == 128 ? 0 : sh.threads == 256 ? 1 : 2;
+      if (!done[slot][dev.index].load(std::memory_order_acquire)) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024) != cudaSuccess) {
           cudaGetLastError();
           return MAXDNN_CUDA_ERROR;
         }
-        done[sh.j - 1][dev.index].store(true, std::memory_order_release);
+        done[slot][dev.index].store(true, std::memory_order_release);
       }
       kern<<<grid, sh.threads, smem, stream>>>(a, sh.depth);
       return launched();

@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(kQuantThreads) quant8_kernel(const __grid_cons
   const int cb = blockIdx.x % args.col_blocks;
   const int rb = blockIdx.x / args.col_blocks;
   const int r0 = rb * kBlock8, c0 = cb * kBlock8 + 8 * (t & 15);
-  const int n = min(max(args.cols - c0, 0), 8);
+  const int n = vector_cols<EDGE>(args.cols, c0);
   const int rg = t >> 4;
   const T* x = static_cast<const T*>(args.x);
   Raw8<XT> raw[8];
@@ -114,11 +114,18 @@ __global__ void __launch_bounds__(kQuantThreads) quant8_kernel(const __grid_cons
 
   if (args.q_row) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const uint32_t b = scale_byte<QT>(max_over_block_lanes(row_max[k]));
-      if ((t & 15) == 0) row_byte[rg + 16 * k] = (uint8_t)b;
-      const F2 inv = f2(inv_scale_of(b)), all[4] = {inv, inv, inv, inv};
-      store(args.q_row, k, all);
+    for (int k = 0; k < 8; k += 2) {
+      uint32_t b[2];
+      if (block_bytes<QT>(row_max[k], row_max[k + 1], &b[0], &b[1])) {
+        b[0] = scale_byte<QT>(max_over_block_lanes(row_max[k]));
+        b[1] = scale_byte<QT>(max_over_block_lanes(row_max[k + 1]));
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if ((t & 15) == 0) row_byte[rg + 16 * (k + i)] = (uint8_t)b[i];
+        const F2 inv = f2(inv_scale_of(b[i])), all[4] = {inv, inv, inv, inv};
+        store(args.q_row, k + i, all);
+      }
     }
   }
   if (cols_wanted) {
@@ -185,7 +192,7 @@ __global__ void __launch_bounds__(kQuantThreads) dequant8_kernel(const __grid_co
   const int cb = blockIdx.x % args.col_blocks;
   const int rb = blockIdx.x / args.col_blocks;
   const int r0 = rb * kBlock8 + (t >> 4), c0 = cb * kBlock8 + 8 * (t & 15);
-  const int n = min(max(args.cols - c0, 0), 8);
+  const int n = vector_cols<EDGE>(args.cols, c0);
   if (n == 0) return;
   Raw8<QT> raw[8];
   uint32_t byte[8];

@@ -145,7 +145,7 @@ def _mat(t, dtype, rows, cols, ld, what):
     """Address of a [rows][cols] matrix with row pitch ld: a 2-d view with these strides, or any
     contiguous tensor of rows x cols elements where ld = cols."""
     try:
-        if (t.shape == (rows, cols) and t.stride() == (ld, 1) and t.dtype in _TYPES[dtype]
+        if (t.is_cuda and t.shape == (rows, cols) and t.stride() == (ld, 1) and t.dtype in _TYPES[dtype]
                 and t.get_device() == _current_device()):
             return t.data_ptr()
     except (AttributeError, IndexError):
