@@ -47,5 +47,36 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+BINDING = os.path.join(HERE, "_train8.so")
+BINDING_SOURCE = os.path.join(CSRC, "train8_binding.cpp")
+
+
+def build_binding(force: bool = False) -> str:
+    """Compile the marshalling module of the 8-bit training operators (host C++ against the
+    installed torch's headers) if it is missing or older than its sources; return its path."""
+    deps = (BINDING_SOURCE, os.path.join(HERE, "..", "include", "maxdnn.h"), os.path.abspath(__file__))
+    if not force and os.path.exists(BINDING) and all(os.path.getmtime(p) <= os.path.getmtime(BINDING) for p in deps):
+        return BINDING
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    tmp = BINDING + ".tmp.%d" % os.getpid()
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-fPIC", "-shared", "-w",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), "-I" + sysconfig.get_paths()["include"],
+           "-I" + os.path.join(cuda, "include")] + ["-I" + p for p in cpp_extension.include_paths()] + \
+          ["-o", tmp, BINDING_SOURCE, "-L" + libs, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        if os.path.exists(tmp):
+            os.remove(tmp)
+        raise RuntimeError("compiling the binding failed:\n%s\n%s" % (" ".join(cmd), res.stdout + res.stderr))
+    os.replace(tmp, BINDING)
+    return BINDING
+
+
 if __name__ == "__main__":
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    print(build_binding(force="--force" in sys.argv))

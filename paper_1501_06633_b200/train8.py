@@ -101,12 +101,34 @@ class Act8Desc(ctypes.Structure):
 _lib = None
 
 
+class _NoPlain:
+    """Stands in where the marshalling module is not built: every call goes through the checks below."""
+
+    quant8 = dequant8 = gemm8 = layer_norm_fprop = layer_norm_bprop = act8_fprop = act8_bprop = staticmethod(lambda *a: -1)
+
+
+_plain = _NoPlain
+
+
+def _load_plain(lib):
+    """The module that checks and passes on the arguments of plain calls (csrc/train8_binding.cpp)."""
+    if not torch.cuda.is_available():
+        return _NoPlain
+    try:
+        from . import _train8
+    except ImportError:
+        return _NoPlain
+    _train8.bind(*(ctypes.cast(getattr(lib, "maxdnn_" + n), ctypes.c_void_p).value for n in (
+        "quant8", "dequant8", "gemm8", "layer_norm_fprop", "layer_norm_bprop", "act8_fprop", "act8_bprop")))
+    return _train8
+
+
 def _raw_stream(device):
     return torch.cuda.current_stream(device).cuda_stream
 
 
 def _library():
-    global _lib, torch, _TYPES, _current_device, _current_raw_stream
+    global _lib, torch, _TYPES, _current_device, _current_raw_stream, _plain
     if _lib is None:
         lib = load_library()
         import torch
@@ -132,6 +154,7 @@ def _library():
                 ("maxdnn_act8_bprop", [P(Act8Desc)] + [_vp] * 5)):
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = ctypes.c_int, args
+        _plain = _load_plain(lib)
         _lib = lib
     return _lib
 
@@ -219,6 +242,11 @@ def empty_scales(block, rows, cols, device="cuda"):
 def quant8(desc: Quant8Desc, x, row=None, col=None, tile=None, x_scale=None, stream=None) -> None:
     """maxdnn_quant8: packs x into the forms asked for; row, col, tile: (values, scales)."""
     lib = _library()
+    none = (None, None)
+    status = _plain.quant8(desc, x, x_scale, *(row or none), *(col or none), *(tile or none),
+                           None if stream is None else stream.cuda_stream)
+    if status >= 0:
+        return _raise(status, "maxdnn_quant8")
     r, c = desc.rows, desc.cols
     px = _mat(x, desc.x_type, r, c, desc.ldx, "x")
     ps = None if desc.x_type < DTYPE_E4M3 else _scales(x_scale, _n_scales(BLOCK_ROW, r, c), "x_scale")
@@ -231,6 +259,10 @@ def quant8(desc: Quant8Desc, x, row=None, col=None, tile=None, x_scale=None, str
 def dequant8(desc: Quant8Desc, q, s, x, block=BLOCK_ROW, stream=None) -> None:
     """maxdnn_dequant8: the values that a packed matrix stands for."""
     lib = _library()
+    status = _plain.dequant8(desc, block, q, s, x,
+                           None if stream is None else stream.cuda_stream)
+    if status >= 0:
+        return _raise(status, "maxdnn_dequant8")
     r, c = desc.rows, desc.cols
     _raise(lib.maxdnn_dequant8(
         ctypes.byref(desc), block, _mat(q, desc.q_type, r, c, desc.ldq, "q"),
@@ -248,6 +280,10 @@ def _operand(t, s, dtype, major, block, scale_type, mn, k, ld, what):
 def gemm8(desc: Gemm8Desc, a, a_scale, b, b_scale, c, stream=None) -> None:
     """maxdnn_gemm8: C[m, n] = sum_k a[m, k] b[n, k] of packed matrices."""
     lib = _library()
+    status = _plain.gemm8(desc, a, a_scale, b, b_scale, c,
+                           None if stream is None else stream.cuda_stream)
+    if status >= 0:
+        return _raise(status, "maxdnn_gemm8")
     M, N, K = desc.M, desc.N, desc.K
     pa, psa = _operand(a, a_scale, desc.a_type, desc.a_major, desc.a_block, desc.a_scale_type, M, K, desc.lda, "a")
     pb, psb = _operand(b, b_scale, desc.b_type, desc.b_major, desc.b_block, desc.b_scale_type, N, K, desc.ldb, "b")
@@ -259,6 +295,11 @@ def layer_norm_fprop(desc: LayerNormDesc, x, gamma=None, beta=None, y=None, mean
                      checkpoint=None, stream=None) -> None:
     """maxdnn_layer_norm_fprop; packed: (q, s) of y, checkpoint: (c, sc) of x."""
     lib = _library()
+    none = (None, None)
+    status = _plain.layer_norm_fprop(desc, x, gamma, beta, y, mean, rstd, *(packed or none), *(checkpoint or none),
+                           None if stream is None else stream.cuda_stream)
+    if status >= 0:
+        return _raise(status, "maxdnn_layer_norm_fprop")
     r, c = desc.rows, desc.cols
     f32, w, n = _TYPES[DTYPE_F32], _TYPES[desc.w_type], _n_scales(BLOCK_ROW, r, c)
     q, s = _pair(packed, desc.q_type, r, c, desc.ldq, n, "packed")
@@ -282,6 +323,10 @@ def layer_norm_bprop(desc: LayerNormDesc, dy, x, gamma, mean, rstd, dx, dgamma=N
                      x_scale=None, stream=None) -> None:
     """maxdnn_layer_norm_bprop; x: wide, or the checkpoint with its x_scale."""
     lib = _library()
+    status = _plain.layer_norm_bprop(desc, dy, x, x_scale, gamma, mean, rstd, dx, dgamma, dbeta, workspace,
+                           None if stream is None else stream.cuda_stream)
+    if status >= 0:
+        return _raise(status, "maxdnn_layer_norm_bprop")
     r, c, f32 = desc.rows, desc.cols, _TYPES[DTYPE_F32]
     if workspace is not None:
         _on_device(workspace, "workspace")
@@ -300,6 +345,11 @@ def layer_norm_bprop(desc: LayerNormDesc, dy, x, gamma, mean, rstd, dx, dgamma=N
 def act8_fprop(desc: Act8Desc, h, a=None, packed=None, checkpoint=None, stream=None) -> None:
     """maxdnn_act8_fprop; packed: (q, s) of the result, checkpoint: (c, sc) of h."""
     lib = _library()
+    none = (None, None)
+    status = _plain.act8_fprop(desc, h, a, *(packed or none), *(checkpoint or none),
+                           None if stream is None else stream.cuda_stream)
+    if status >= 0:
+        return _raise(status, "maxdnn_act8_fprop")
     r, c, many = desc.rows, desc.cols, 1 + desc.gated
     n = _n_scales(BLOCK_ROW, r, c)
     q, s = _pair(packed, desc.q_type, r, c, desc.ldq, n, "packed")
@@ -312,6 +362,10 @@ def act8_fprop(desc: Act8Desc, h, a=None, packed=None, checkpoint=None, stream=N
 def act8_bprop(desc: Act8Desc, da, h, dh, h_scale=None, stream=None) -> None:
     """maxdnn_act8_bprop; h: wide, or the checkpoint with its h_scale."""
     lib = _library()
+    status = _plain.act8_bprop(desc, da, h, h_scale, dh,
+                           None if stream is None else stream.cuda_stream)
+    if status >= 0:
+        return _raise(status, "maxdnn_act8_bprop")
     r, c, many = desc.rows, desc.cols, 1 + desc.gated
     packed = desc.h_type >= DTYPE_E4M3
     _raise(lib.maxdnn_act8_bprop(
