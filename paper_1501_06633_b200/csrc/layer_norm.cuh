@@ -133,6 +133,26 @@ layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
   const int group = warp / WR, in_row = warp % WR, t = in_row * 32 + lane;
   const T* x = static_cast<const T*>(args.x);
   T* y = static_cast<T*>(args.y);
+  // The weights as fp32 in shared memory, for every row of the CTA: whatever their type, and where
+  // there are none.  (Few rows, J < 4: each is read where it is used.)
+  constexpr bool kShared = J >= 4 && !EDGE;
+  extern __shared__ __align__(16) float weights[];
+  const int padded = 256 * WR * J;
+  if constexpr (kShared) {
+    if (args.y || args.q) {
+      for (int c = 8 * (int)threadIdx.x; c < padded; c += 8 * kNormThreads) {
+        const int n = vector_cols<EDGE>(args.cols, c);
+        F2 w[4];
+        load_weights8<EDGE>(args.gamma, c, n, args.w_type, true, 1.f, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<F2*>(&weights[c + 2 * i]) = w[i];
+        load_weights8<EDGE>(args.beta, c, n, args.w_type, true, 0.f, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<F2*>(&weights[padded + c + 2 * i]) = w[i];
+      }
+    }
+    __syncthreads();
+  }
   // sum over the row's threads
   auto total = [&](float v, int slot) {
     v = warp_sum(v);
@@ -201,8 +221,18 @@ layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
       for (int i = 0; i < kPair; ++i) {
         const int c = c0 + kStep * (j + i);
         F2 g[4], b[4];
-        load_weights8<EDGE>(args.gamma, c, n[i], args.w_type, args.vec_w != 0, 1.f, g);
-        load_weights8<EDGE>(args.beta, c, n[i], args.w_type, args.vec_w != 0, 0.f, b);
+        if constexpr (kShared) {
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            const ulonglong2 gg = *reinterpret_cast<const ulonglong2*>(&weights[c + 2 * e]);
+            const ulonglong2 bb = *reinterpret_cast<const ulonglong2*>(&weights[padded + c + 2 * e]);
+            g[e] = gg.x; g[e + 1] = gg.y;
+            b[e] = bb.x; b[e + 1] = bb.y;
+          }
+        } else {
+          load_weights8<EDGE>(args.gamma, c, n[i], args.w_type, args.vec_w != 0, 1.f, g);
+          load_weights8<EDGE>(args.beta, c, n[i], args.w_type, args.vec_w != 0, 0.f, b);
+        }
         normalise8<EDGE>(v[i], minus_mean, f2(rstd), g, b, n[i]);
         if (args.y) store_pairs<XT, EDGE>(yp + kStep * (j + i), v[i], n[i], args.vec_y != 0);
       }
@@ -233,10 +263,12 @@ __device__ __forceinline__ void norm_back8(const Raw8<XT>& rx, const Raw8<YT>& r
                                            F2* s1, F2* s2) {
   to_pairs<XT>(rx, xh);
   to_pairs<YT>(rdy, e);
-  const F2 k = f2(scale), mm = f2(-mean), rs = f2(rstd);
+  // (scale x - mean) rstd as one multiply-add; the rounding of mean rstd is of the size that the
+  // mean itself was rounded by
+  const F2 k = f2(is_fp8(XT) ? scale * rstd : rstd), mm = f2(-mean * rstd);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    xh[i] = mul2(is_fp8(XT) ? fma2(xh[i], k, mm) : add2(xh[i], mm), rs);
+    xh[i] = fma2(xh[i], k, mm);
     if (EDGE) {
       const float2 t = unf2(xh[i]);
       xh[i] = f2(2 * i < n ? t.x : 0.f, 2 * i + 1 < n ? t.y : 0.f);
@@ -251,9 +283,9 @@ __device__ __forceinline__ void norm_back8(const Raw8<XT>& rx, const Raw8<YT>& r
 
 // rstd (e - s1 - xh s2) of eight columns.
 __device__ __forceinline__ void norm_dx8(const F2 (&xh)[4], const F2 (&e)[4], float rstd, float s1, float s2, F2 (&o)[4]) {
-  const F2 m1 = f2(-s1), m2 = f2(-s2), rs = f2(rstd);
+  const F2 m1 = f2(-s1 * rstd), m2 = f2(-s2 * rstd), rs = f2(rstd);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = mul2(rs, fma2(xh[i], m2, add2(e[i], m1)));
+  for (int i = 0; i < 4; ++i) o[i] = fma2(xh[i], m2, fma2(e[i], rs, m1));
 }
 
 // XT: the type of x (wide, or packed rows); YT: of dy and dx.  WARP_ROW: each warp of the CTA has
@@ -468,6 +500,7 @@ layer_norm_bprop_ring_kernel(const __grid_constant__ LayerNormArgs args, int dep
           rdy = *reinterpret_cast<const Raw8<YT>*>(ring + y_at(slot, j));
           if constexpr (is_fp8(XT)) scale = e8m0_value(scales[(c >> 7) * kNormChunk + k]);
         }
+        // (columns past the end: dy = 0 keeps them out of every sum)
         norm_back8<XT, YT, false>(rx, rdy, scale, mean, rstd, g[j], 8, xh[j], e[j], dg[j], db[j], &p1, &p2);
       }
       // both sums in six shuffles: the halves of the warp take one each
@@ -526,6 +559,7 @@ __global__ void __launch_bounds__(512) layer_norm_fold_kernel(const float* parti
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t c = (int64_t)blockIdx.x * 32 + lane, pitch = 2 * (int64_t)cols;
   float s[4] = {0.f, 0.f, 0.f, 0.f};
+  asm volatile("griddepcontrol.wait;" ::: "memory");     // launched while the sums' kernel still runs
   if (c < pitch) {
     const float* at = partial + c;
     int p = warp;

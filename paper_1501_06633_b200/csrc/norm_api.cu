@@ -49,13 +49,29 @@ maxdnn_status launch_norm_rows(const LayerNormArgs& a, int sm_count, cudaStream_
   const int64_t units = ((int64_t)a.rows + 8 / WR - 1) / (8 / WR);
   const int64_t most = (int64_t)sm_count * 4;
   const unsigned grid = (unsigned)(units < most ? units : most);
-  if (!(a.vec_x && a.vec_y && a.vec_w && a.cols % 8 == 0))
+  if (!(a.vec_x && a.vec_y && a.vec_w && a.cols % 8 == 0)) {
     layer_norm_fprop_kernel<XT, kEitherFp8, J, WR, true><<<grid, kNormThreads, 0, stream>>>(a);
-  else if (a.q_e5m2)
-    layer_norm_fprop_kernel<XT, MAXDNN_E5M2, J, WR, false><<<grid, kNormThreads, 0, stream>>>(a);
-  else
-    layer_norm_fprop_kernel<XT, MAXDNN_E4M3, J, WR, false><<<grid, kNormThreads, 0, stream>>>(a);
-  return launched();
+    return launched();
+  }
+  const size_t smem = J >= 4 ? 2 * 256 * WR * J * sizeof(float) : 0;      // the weights: at most 64 KB (J = 8: 128)
+  auto run = [&](auto kern) {
+    static std::atomic<bool> done[2][64];
+    int dev = 0;
+    if (smem > 48 * 1024) {
+      std::atomic<bool>& flag = done[a.q_e5m2 ? 1 : 0][cudaGetDevice(&dev) == cudaSuccess ? dev & 63 : 0];
+      if (!flag.load(std::memory_order_acquire)) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+          cudaGetLastError();
+          return MAXDNN_CUDA_ERROR;
+        }
+        flag.store(true, std::memory_order_release);
+      }
+    }
+    kern<<<grid, kNormThreads, smem, stream>>>(a);
+    return launched();
+  };
+  if (a.q_e5m2) return run(layer_norm_fprop_kernel<XT, MAXDNN_E5M2, J, WR, false>);
+  return run(layer_norm_fprop_kernel<XT, MAXDNN_E4M3, J, WR, false>);
 }
 
 // Vectors of eight columns per thread (J) and warps per row (WR).  Few rows (fewer than the SMs
@@ -214,8 +230,20 @@ maxdnn_status layer_norm_bprop(const maxdnn_layer_norm_desc* d, const void* dy, 
     return run(yt, yt);
   });
   if (st != MAXDNN_OK || !sums) return st;
-  layer_norm_fold_kernel<<<(unsigned)((2 * (int64_t)d->cols + 31) / 32), 512, 0, stream>>>(a.partial, grid, d->cols,
-                                                                                          dgamma, dbeta);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((2 * (int64_t)d->cols + 31) / 32), 1, 1);
+  cfg.blockDim = dim3(512, 1, 1);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, layer_norm_fold_kernel, (const float*)a.partial, grid, (int)d->cols, dgamma, dbeta) !=
+      cudaSuccess) {
+    cudaGetLastError();
+    return MAXDNN_CUDA_ERROR;
+  }
   return launched();
 }
 
