@@ -53,25 +53,10 @@ maxdnn_status launch_norm_rows(const LayerNormArgs& a, int sm_count, cudaStream_
     layer_norm_fprop_kernel<XT, kEitherFp8, J, WR, true><<<grid, kNormThreads, 0, stream>>>(a);
     return launched();
   }
-  const size_t smem = J >= 4 ? 2 * 256 * WR * J * sizeof(float) : 0;      // the weights: at most 64 KB (J = 8: 128)
-  auto run = [&](auto kern) {
-    static std::atomic<bool> done[2][64];
-    int dev = 0;
-    if (smem > 48 * 1024) {
-      std::atomic<bool>& flag = done[a.q_e5m2 ? 1 : 0][cudaGetDevice(&dev) == cudaSuccess ? dev & 63 : 0];
-      if (!flag.load(std::memory_order_acquire)) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
-          cudaGetLastError();
-          return MAXDNN_CUDA_ERROR;
-        }
-        flag.store(true, std::memory_order_release);
-      }
-    }
-    kern<<<grid, kNormThreads, smem, stream>>>(a);
-    return launched();
-  };
-  if (a.q_e5m2) return run(layer_norm_fprop_kernel<XT, MAXDNN_E5M2, J, WR, false>);
-  return run(layer_norm_fprop_kernel<XT, MAXDNN_E4M3, J, WR, false>);
+  const size_t smem = norm_shared_weights(J, WR) ? 2 * 256 * WR * J * sizeof(float) : 0;     // at most 32 KB
+  if (a.q_e5m2) layer_norm_fprop_kernel<XT, MAXDNN_E5M2, J, WR, false><<<grid, kNormThreads, smem, stream>>>(a);
+  else layer_norm_fprop_kernel<XT, MAXDNN_E4M3, J, WR, false><<<grid, kNormThreads, smem, stream>>>(a);
+  return launched();
 }
 
 // Vectors of eight columns per thread (J) and warps per row (WR).  Few rows (fewer than the SMs

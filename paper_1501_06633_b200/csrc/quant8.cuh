@@ -26,7 +26,7 @@ struct Quant8Args {
 };
 
 template <int XT, int QT, bool EDGE>
-__global__ void __launch_bounds__(kQuantThreads) quant8_kernel(const __grid_constant__ Quant8Args args) {
+__global__ void __launch_bounds__(kQuantThreads, XT == MAXDNN_F32 ? 2 : 3) quant8_kernel(const __grid_constant__ Quant8Args args) {
   typedef typename ElemOf<XT>::T T;
   __shared__ float col_part[kQuantThreads / 32][kBlock8];   // per warp: maxima of its rows
   __shared__ float col_inv[kBlock8];
