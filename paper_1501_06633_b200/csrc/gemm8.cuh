@@ -105,17 +105,29 @@ __device__ __forceinline__ void gemm8_tile(int m_tiles, int n_tiles, int t, int*
   *nt = in / height;
 }
 
-// The end of a tile that `split` CTAs of a cluster share: CTA `rank` adds the CTAs' totals
-// ([column][row] at `base` of each CTA's shared memory) for its part of the columns, in CTA order,
-// and stores them.  A thread takes four rows of a column; all CTAs' loads are in flight at once.
+// The end of a tile that `split` CTAs of a cluster share: CTA `rank` adds the CTAs' totals for its
+// part of the tile, in CTA order, and stores them; all CTAs' loads are in flight at once.  The
+// totals are at `base` of each CTA's shared memory, laid out so that neighbouring threads store
+// neighbouring elements of C: [column][row] where C's rows are neighbours (exchanged roles), else
+// [row][column] with rows 16 bytes apart from a power of two.
+__host__ __device__ constexpr int gemm8_row_pitch(int nt) { return nt + 4; }        // floats
+
+template <int NT>
+__device__ __forceinline__ void gemm8_keep_total(float* mine, bool by_column, int row, int col, float v) {
+  mine[by_column ? col * kGemm8TileM + row : row * gemm8_row_pitch(NT) + col] = v;
+}
+
 template <int NT, int THREADS, class Args>
 __device__ __forceinline__ void gemm8_add_split(const Args& args, uint32_t base, int split, int rank, int unit) {
-  const int cols = NT / split;
+  const bool by_column = args.c_row == 1;
+  const int cols = NT / split, rows = kGemm8TileM / split;      // this CTA's part: columns, or rows
   int mt, nt;
   gemm8_tile(args.m_tiles, args.n_tiles, unit, &mt, &nt);
-  for (int e = threadIdx.x; e < cols * (kGemm8TileM / 4); e += THREADS) {
-    const int row = 4 * (e & (kGemm8TileM / 4 - 1)), col = rank * cols + e / (kGemm8TileM / 4);
-    const uint32_t off = base + 4u * (uint32_t)(col * kGemm8TileM + row);
+  for (int e = threadIdx.x; e < kGemm8TileM * NT / 4 / split; e += THREADS) {
+    // four neighbours: rows of a column, or columns of a row
+    const int row = by_column ? 4 * (e & (kGemm8TileM / 4 - 1)) : rank * rows + e / (NT / 4);
+    const int col = by_column ? rank * cols + e / (kGemm8TileM / 4) : 4 * (e % (NT / 4));
+    const uint32_t off = base + 4u * (uint32_t)(by_column ? col * kGemm8TileM + row : row * gemm8_row_pitch(NT) + col);
     float4 part[kGemm8MaxSplit];
 #pragma unroll
     for (int r = 0; r < kGemm8MaxSplit; ++r)
@@ -127,12 +139,11 @@ __device__ __forceinline__ void gemm8_add_split(const Args& args, uint32_t base,
         v[0] += part[r].x; v[1] += part[r].y; v[2] += part[r].z; v[3] += part[r].w;
       }
     const int m = mt * kGemm8TileM + row, n = nt * NT + col;
-    if (n < args.N) {
+    const int64_t at = (int64_t)m * args.c_row + (int64_t)n * args.c_col;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (m + i < args.M)
-          gemm8_store1(args.c, args.c_type, (int64_t)(m + i) * args.c_row + (int64_t)n * args.c_col, v[i]);
-    }
+    for (int i = 0; i < 4; ++i)
+      if (by_column ? (m + i < args.M && n < args.N) : (m < args.M && n + i < args.N))
+        gemm8_store1(args.c, args.c_type, at + i, v[i]);
   }
 }
 
@@ -360,11 +371,12 @@ gemm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
           }
         }
       } else {
-        // this CTA's totals as [column][row]: the ring is no longer in use (every block that was
+        // this CTA's totals where the ring was: it is no longer in use (every block that was
         // copied has been multiplied, and every product has been read)
         float* mine = reinterpret_cast<float*>(base_ptr);
 #pragma unroll
-        for (int i = 0; i < CW; ++i) mine[(part * CW + i) * kGemm8TileM + q * 32 + lane] = tot[i];
+        for (int i = 0; i < CW; ++i)
+          gemm8_keep_total<NT>(mine, args.c_row == 1, q * 32 + lane, part * CW + i, tot[i]);
       }
     }
   }

@@ -18,6 +18,7 @@ struct Gemm8Plan {
   int32_t tile_n;      // columns of a tile
   int32_t chunk;       // mx: blocks of the reduction per accumulator
   int32_t bulk_c;      // mx: C is stored by bulk tensor copies
+  int32_t staged_c;    // mx: C goes through staging tiles in shared memory
   int32_t split;       // CTAs that share a tile's reduction: 1, 2, 4 or 8
   int32_t m_tiles, n_tiles, k_blocks;
   int32_t stages;

@@ -116,6 +116,7 @@ maxdnn_status gemm8_mx(const RuntimeDevice& dev, const maxdnn_gemm8_desc& d, con
   args.b_stage_bytes = p.b_stage_bytes;
   args.c_type = d.c_type;
   args.bulk_c = p.bulk_c;
+  args.staged_c = p.staged_c;
   args.chunk = p.chunk;
   args.idesc = idesc | (1u << 23);          // scales are E8M0
   args.test_missing_arrival = (uint32_t)option(OPT_TEST_MISSING_ARRIVAL);

@@ -58,7 +58,8 @@ struct Gemm8MxArgs {
   int32_t a_mn, b_mn;
   int32_t b_stage_bytes;
   int32_t c_type;
-  int32_t bulk_c;              // C is stored by bulk tensor copies
+  int32_t bulk_c;              // C is stored by bulk tensor copies; 0: element by element
+  int32_t staged_c;            // C goes through staging tiles (bulk copies, or rows of odd pitch)
   int32_t chunk;               // blocks per accumulator
   uint32_t idesc;
   uint32_t test_missing_arrival;
@@ -169,8 +170,8 @@ gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   const int stages = args.stages;
   const uint32_t b_off = (uint32_t)stages * kAStage;
   const uint32_t st_off = b_off + (uint32_t)stages * (uint32_t)args.b_stage_bytes;
-  const uint32_t stg_bytes = args.c_type == MAXDNN_F32 ? 4096u : 2048u;   // 32 rows x 32 columns
-  const uint32_t sf_off = st_off + (args.bulk_c ? kMxEpiWarps * stg_bytes : 0u);
+  const uint32_t stg_bytes = args.c_type == MAXDNN_F32 || !args.bulk_c ? 4096u : 2048u;   // 32 rows x 32 columns
+  const uint32_t sf_off = st_off + (args.staged_c ? kMxEpiWarps * stg_bytes : 0u);
   const uint32_t bar_off = sf_off + kMxScaleBufs * kSfBytes;
   const uint32_t full_bar = base + bar_off;
   const uint32_t empty_bar = full_bar + 8u * stages;
@@ -462,14 +463,14 @@ gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       }
       if (!ok) break;
       if (!PAIR && split > 1) {
-        // this CTA's totals as [column][row], where the ring was
+        // this CTA's totals where the ring was
         float* mine = reinterpret_cast<float*>(base_ptr);
 #pragma unroll
         for (int u = 0; u < kUnits; ++u)
           if (u0 + u < kAllUnits) {
 #pragma unroll
             for (int i = 0; i < kUnitCols; ++i)
-              mine[((u0 + u) * 32 + i) * kGemm8TileM + q * 32 + lane] = tot[u][i];
+              gemm8_keep_total<NT>(mine, args.c_row == 1, q * 32 + lane, (u0 + u) * 32 + i, tot[u][i]);
           }
       } else if (args.bulk_c) {
         if constexpr (NT >= 32) {
@@ -510,6 +511,24 @@ gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
               tma_store_2d_hint(&map_c, stg, n0 + 32 * u, m_warp, policy);
               bulk_commit();
             }
+          }
+        }
+      } else if (args.staged_c) {
+        // rows that bulk copies cannot store: through the staging tile (column c of row r at c ^ r,
+        // which keeps both directions free of bank conflicts), a row of 32 neighbours at a time
+        float* tile_f = reinterpret_cast<float*>(stg_ptr);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+          if (u0 + u >= kAllUnits || n0 + 32 * u >= args.N) continue;
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < kUnitCols; ++i) tile_f[lane * 32 + (i ^ lane)] = tot[u][i];
+          __syncwarp();
+          const int n = n0 + 32 * u + lane;
+          if (lane < kUnitCols && n < args.N) {
+#pragma unroll 4
+            for (int rr = 0; rr < 32 && m_warp + rr < args.M; ++rr)
+              gemm8_store1(args.c, args.c_type, (int64_t)(m_warp + rr) * args.c_row + n, tile_f[rr * 32 + (lane ^ rr)]);
           }
         }
       } else if (m < args.M) {

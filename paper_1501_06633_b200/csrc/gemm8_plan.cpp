@@ -78,11 +78,13 @@ maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* pl
         const int64_t units = split == 1 ? std::min<int64_t>(tiles, slots) : tiles;
         const int64_t waves = (tiles * split + slots - 1) / slots;
         const int64_t blocks = (k_blocks + split - 1) / split;
-        // 3.4 us is a call with one block; sharing a tile costs an exchange of totals; two CTAs on
-        // an SM share its issue slots
+        // 3.4 us is a call with one block; sharing a tile costs an exchange of totals, and so does
+        // storing C without bulk copies; two CTAs on an SM share its issue slots
+        const bool bulk = mx && !swap && split == 1 && s.nt >= 32 && (d.ldc * c_bytes) % 16 == 0 &&
+                          ((int64_t)d.N * c_bytes) % 16 == 0;
         const double crowd = s.nt <= 32 && mx ? std::max(1.0, 0.4 + 0.6 * (double)std::min<int64_t>(tiles * split, slots) / sm_count) : 1.0;
         const double run = 3.4 + (double)(waves * blocks) * s.block * crowd + s.tile * (1.0 + (double)(waves - 1) / 3.0) +
-                           (split > 1 ? 1.0 + 0.008 * s.nt : 0.0);
+                           (split > 1 ? 1.0 + 0.008 * s.nt : bulk ? 0.0 : 0.8);
         // every tile reads its operands from the second-level cache
         const double fill = 5.0 + (double)tiles * k_blocks * (16384 + b_stage) * (s.pair ? 2 : 1) / 11.0e6;
         const double t = std::max(std::max(run, fill), memory) + 0.05 * run;
@@ -102,8 +104,8 @@ maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* pl
         plan->grid = (int32_t)(units * (s.pair ? 2 : split));
         // bulk copies of 32 rows x 32 columns: rows of C contiguous, starting and ending at
         // multiples of 16 bytes (a copy that is cut at the tensor's edge writes whole 16 bytes)
-        plan->bulk_c = mx && !swap && split == 1 && s.nt >= 32 && (d.ldc * c_bytes) % 16 == 0 &&
-                       ((int64_t)d.N * c_bytes) % 16 == 0;
+        plan->bulk_c = bulk;
+        plan->staged_c = mx && !swap && split == 1;
       }
     }
   }
@@ -111,7 +113,7 @@ maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* pl
   if ((int64_t)plan->m_tiles * plan->n_tiles > (1 << 30)) return MAXDNN_NOT_SUPPORTED;
   int fixed = 1024 + 192;
   if (plan->mx) {
-    fixed += (plan->bulk_c ? 8 * 32 * 32 * c_bytes : 0) + 8 * 128 * (4 + 4 * ((plan->tile_n + 127) / 128));
+    fixed += (plan->staged_c ? 8 * 32 * 32 * (plan->bulk_c ? c_bytes : 4) : 0) + 8 * 128 * (4 + 4 * ((plan->tile_n + 127) / 128));
   } else {
     const int warps = 4 * (plan->tile_n < 64 ? 1 : plan->tile_n / 64), cw = std::min(plan->tile_n, 64);
     fixed += warps * 2 * cw * 4;
@@ -125,7 +127,7 @@ maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* pl
   if (plan->mx && plan->tile_n <= 32 && plan->grid > sm_count) plan->stages = std::min(plan->stages, (115200 - fixed) / per_stage);
   if (one_tile) plan->stages = std::max(2, std::min(plan->stages, blocks));
   if (plan->split > 1) {        // the totals take the place of the ring
-    const int need = plan->tile_n * kGemm8TileM * 4, ring = per_stage - 16;
+    const int need = (plan->tile_n + 4) * kGemm8TileM * 4, ring = per_stage - 16;
     plan->stages = std::max(plan->stages, (need + ring - 1) / ring);
   }
   plan->smem_bytes = fixed + plan->stages * per_stage;
