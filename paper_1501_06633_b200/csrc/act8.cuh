@@ -27,7 +27,6 @@ struct Act8Args {
   void* dh;
   int64_t ldh, lda, ldq, ldc;
   int32_t rows, cols, col_blocks;
-  int32_t vec_h, vec_u, vec_a, vec_cu, vec_dh, vec_du;
 };
 
 // 1 / (1 + exp(-x)) from the hardware's exponential and reciprocal.  The exponential's relative
@@ -71,16 +70,16 @@ __device__ __forceinline__ void activation(float g, float* f, float* df) {
 
 // Packs eight values each of two row blocks and keeps their scale bytes (null: nowhere).
 template <int QT, bool EDGE>
-__device__ __forceinline__ void pack_rows8(const F2 (&v)[4], const F2 (&w)[4], uint8_t* pv, uint8_t* pw, int n, bool vec_v,
-                                           bool vec_w, bool live_v, bool live_w, uint8_t* sv, uint8_t* sw, bool first) {
+__device__ __forceinline__ void pack_rows8(const F2 (&v)[4], const F2 (&w)[4], uint8_t* pv, uint8_t* pw, int n,
+                                           bool live_v, bool live_w, uint8_t* sv, uint8_t* sw, bool first) {
   uint32_t bv, bw;
   bool fv = false, fw = false;
   if (block_bytes<QT>(max8(v), max8(w), &bv, &bw)) {
     bv = exact_byte<QT>(v, &fv);
     bw = exact_byte<QT>(w, &fw);
   }
-  if (live_v) store_bytes8<EDGE>(pv, pack8<QT>(v, inv_scale_of(bv), fv), n, vec_v);
-  if (live_w) store_bytes8<EDGE>(pw, pack8<QT>(w, inv_scale_of(bw), fw), n, vec_w);
+  if (live_v) store_bytes8<EDGE>(pv, pack8<QT>(v, inv_scale_of(bv), fv), n);
+  if (live_w) store_bytes8<EDGE>(pw, pack8<QT>(w, inv_scale_of(bw), fw), n);
   if (first) {
     *sv = (uint8_t)bv;
     *sw = (uint8_t)bw;
@@ -102,8 +101,8 @@ __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_co
   for (int k = 0; k < 4; ++k) {
     const int r = r0 + (t >> 4) + 16 * k;
     const int nr = r < args.rows ? n : 0;
-    rg[k] = load_raw8<XT, EDGE>(h + (int64_t)r * args.ldh + c0, nr, args.vec_h != 0);
-    if constexpr (GATED) ru[k] = load_raw8<XT, EDGE>(h + (int64_t)r * args.ldh + args.cols + c0, nr, args.vec_u != 0);
+    rg[k] = load_raw8<XT, EDGE>(h + (int64_t)r * args.ldh + c0, nr);
+    if constexpr (GATED) ru[k] = load_raw8<XT, EDGE>(h + (int64_t)r * args.ldh + args.cols + c0, nr);
   }
   const bool first = (t & 15) == 0;
 #pragma unroll
@@ -119,7 +118,7 @@ __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_co
     }
     if (args.c) {
       uint8_t* c = args.c + (int64_t)r * args.ldc + c0;
-      pack_rows8<QT, EDGE>(v[0], v[1], c, c + 16 * args.ldc, n, true, true, live[0], live[1], &bytes[1][row],
+      pack_rows8<QT, EDGE>(v[0], v[1], c, c + 16 * args.ldc, n, live[0], live[1], &bytes[1][row],
                            &bytes[1][row + 16], first);
     }
     if constexpr (GATED) {
@@ -130,7 +129,7 @@ __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_co
       }
       if (args.c) {
         uint8_t* c = args.c + (int64_t)r * args.ldc + args.cols + c0;
-        pack_rows8<QT, EDGE>(v[0], v[1], c, c + 16 * args.ldc, n, args.vec_cu != 0, args.vec_cu != 0, live[0], live[1],
+        pack_rows8<QT, EDGE>(v[0], v[1], c, c + 16 * args.ldc, n, live[0], live[1],
                              &bytes[2][row], &bytes[2][row + 16], first);
       }
     }
@@ -144,13 +143,13 @@ __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_co
         a[e] = GATED ? f * u[i][e] : f;
       }
       if (args.a && live[i])
-        store_float8<XT, EDGE>(static_cast<T*>(args.a) + (int64_t)(r + 16 * i) * args.lda + c0, a, n, args.vec_a != 0);
+        store_float8<XT, EDGE>(static_cast<T*>(args.a) + (int64_t)(r + 16 * i) * args.lda + c0, a, n);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[i][e] = f2(a[2 * e], a[2 * e + 1]);
     }
     if (args.q) {
       uint8_t* q = args.q + (int64_t)r * args.ldq + c0;
-      pack_rows8<QT, EDGE>(v[0], v[1], q, q + 16 * args.ldq, n, true, true, live[0], live[1], &bytes[0][row],
+      pack_rows8<QT, EDGE>(v[0], v[1], q, q + 16 * args.ldq, n, live[0], live[1], &bytes[0][row],
                            &bytes[0][row + 16], first);
     }
   }
@@ -184,9 +183,9 @@ __global__ void __launch_bounds__(kActThreads) act8_bprop_kernel(const __grid_co
   for (int k = 0; k < 4; ++k) {
     const int r = r0 + 16 * k;
     const int nr = r < args.rows ? n : 0;
-    rg[k] = load_raw8<HT, EDGE>(h + (int64_t)r * ldh + c0, nr, args.vec_h != 0);
-    if constexpr (GATED) ru[k] = load_raw8<HT, EDGE>(h + (int64_t)r * ldh + args.cols + c0, nr, args.vec_u != 0);
-    rd[k] = load_raw8<XT, EDGE>(static_cast<const T*>(args.da) + (int64_t)r * args.lda + c0, nr, args.vec_a != 0);
+    rg[k] = load_raw8<HT, EDGE>(h + (int64_t)r * ldh + c0, nr);
+    if constexpr (GATED) ru[k] = load_raw8<HT, EDGE>(h + (int64_t)r * ldh + args.cols + c0, nr);
+    rd[k] = load_raw8<XT, EDGE>(static_cast<const T*>(args.da) + (int64_t)r * args.lda + c0, nr);
     sg[k] = su[k] = 1.f;
     if (is_fp8(HT) && nr > 0) {
       sg[k] = e8m0_value(args.h_scale[(int64_t)cb * args.rows + r]);
@@ -215,8 +214,8 @@ __global__ void __launch_bounds__(kActThreads) act8_bprop_kernel(const __grid_co
       }
     }
     T* dh = static_cast<T*>(args.dh) + (int64_t)r * args.ldh + c0;
-    store_float8<XT, EDGE>(dh, dg, n, args.vec_dh != 0);
-    if constexpr (GATED) store_float8<XT, EDGE>(dh + args.cols, du, n, args.vec_du != 0);
+    store_float8<XT, EDGE>(dh, dg, n);
+    if constexpr (GATED) store_float8<XT, EDGE>(dh + args.cols, du, n);
   }
 }
 

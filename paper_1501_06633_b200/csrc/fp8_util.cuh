@@ -215,61 +215,69 @@ template <> struct Raw8<MAXDNN_F16> { uint4 a; };
 template <> struct Raw8<MAXDNN_E4M3> { uint2 a; };
 template <> struct Raw8<MAXDNN_E5M2> { uint2 a; };
 
-// Loads `n` (0..8) values at `p`; the rest are zeros.  vec: p is aligned for the wide load.
+// The four words that start `s` bytes (0..15) into eight.
+__device__ __forceinline__ uint4 words_at(uint4 lo, uint4 hi, uint32_t s) {
+  uint32_t w0 = lo.x, w1 = lo.y, w2 = lo.z, w3 = lo.w, w4 = hi.x;
+  if (s & 8u) { w0 = lo.z; w1 = lo.w; w2 = hi.x; w3 = hi.y; w4 = hi.z; }
+  if (s & 4u) { w0 = w1; w1 = w2; w2 = w3; w3 = w4; w4 = s & 8u ? hi.w : hi.y; }
+  const uint32_t sh = 8u * (s & 3u);
+  return make_uint4(__funnelshift_r(w0, w1, sh), __funnelshift_r(w1, w2, sh), __funnelshift_r(w2, w3, sh),
+                    __funnelshift_r(w3, w4, sh));
+}
+// Bytes [0, n) of a word, n counted from the word's first byte; zeros beyond.
+__device__ __forceinline__ uint32_t first_bytes(uint32_t w, int n) {
+  return n >= 4 ? w : n <= 0 ? 0u : w & (0xFFFFFFFFu >> (32 - 8 * n));
+}
+__device__ __forceinline__ uint4 first_bytes(uint4 v, int n) {
+  return make_uint4(first_bytes(v.x, n), first_bytes(v.y, n - 4), first_bytes(v.z, n - 8), first_bytes(v.w, n - 12));
+}
+
+// Loads `n` (0..8) values at `p`; the rest are zeros.
 // EDGE = false: vectors are whole (n is 0 or 8) and aligned.  Kernels are built for both: a branch
 // between the two forms makes the loaded registers move when the branches join, which waits for each load in
 // turn (a layer norm with 16 loads a lane took 9.7 us a row that way).
+// EDGE = true: the aligned 16 (8-bit types: 8) bytes that hold the first and the last value are
+// loaded and shifted; no load touches an aligned unit that holds none of the n values.
 template <int DT, bool EDGE>
-__device__ __forceinline__ Raw8<DT> load_raw8(const typename ElemOf<DT>::T* p, int n, bool vec) {
-  typedef typename ElemOf<DT>::T T;
+__device__ __forceinline__ Raw8<DT> load_raw8(const typename ElemOf<DT>::T* p, int n) {
   Raw8<DT> r;
-  if (!EDGE || (n == 8 && vec)) {
+  if constexpr (!EDGE) {
     if constexpr (DT == MAXDNN_F32) {
       r.a = r.b = make_uint4(0, 0, 0, 0);
-      if (EDGE || n) {
+      if (n) {
         r.a = __ldg(reinterpret_cast<const uint4*>(p));
         r.b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
       }
     } else if constexpr (is_fp8(DT)) {
       r.a = make_uint2(0, 0);
-      if (EDGE || n) r.a = __ldg(reinterpret_cast<const uint2*>(p));
+      if (n) r.a = __ldg(reinterpret_cast<const uint2*>(p));
     } else {
       r.a = make_uint4(0, 0, 0, 0);
-      if (EDGE || n) r.a = __ldg(reinterpret_cast<const uint4*>(p));
+      if (n) r.a = __ldg(reinterpret_cast<const uint4*>(p));
     }
   } else {
-    // value by value into the top of the register chain, which moves down (a loop: the edge of a
-    // matrix is not worth eight copies of this code)
-    constexpr int kWords = 2 * (int)sizeof(T);
-    uint32_t w[kWords];
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) w[i] = 0;
-#pragma unroll 1
-    for (int i = 0; i < 8; ++i) {
-      uint32_t top = 0;
-      if (i < n) {
-        if constexpr (sizeof(T) == 4) top = __float_as_uint(p[i]);
-        else if constexpr (sizeof(T) == 2) top = (uint32_t)reinterpret_cast<const uint16_t*>(p)[i];
-        else top = (uint32_t)p[i];
-      }
-      if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int k = 0; k + 1 < kWords; ++k) w[k] = w[k + 1];
-        w[kWords - 1] = top;
-      } else {
-        constexpr int kBits = 8 * (int)sizeof(T);
-#pragma unroll
-        for (int k = 0; k + 1 < kWords; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], kBits);
-        w[kWords - 1] = (w[kWords - 1] >> kBits) | (top << (32 - kBits));
-      }
-    }
-    if constexpr (DT == MAXDNN_F32) {
-      r.a = make_uint4(w[0], w[1], w[2], w[3]);
-      r.b = make_uint4(w[4], w[5], w[6], w[7]);
-    } else if constexpr (is_fp8(DT)) {
-      r.a = make_uint2(w[0], w[1]);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    const int bytes = n * (int)sizeof(typename ElemOf<DT>::T);
+    if constexpr (is_fp8(DT)) {
+      const uint32_t s = (uint32_t)(at & 7u);
+      const uint2* q = reinterpret_cast<const uint2*>(at - s);
+      uint2 lo = make_uint2(0, 0), hi = make_uint2(0, 0);
+      if (bytes > 0) lo = __ldg(q);
+      if ((int)s + bytes > 8) hi = __ldg(q + 1);
+      const uint4 v = words_at(make_uint4(lo.x, lo.y, hi.x, hi.y), make_uint4(0, 0, 0, 0), s);
+      r.a = make_uint2(first_bytes(v.x, bytes), first_bytes(v.y, bytes - 4));
     } else {
-      r.a = make_uint4(w[0], w[1], w[2], w[3]);
+      const uint32_t s = (uint32_t)(at & 15u);
+      const uint4* q = reinterpret_cast<const uint4*>(at - s);
+      uint4 c0 = make_uint4(0, 0, 0, 0), c1 = c0;
+      if (bytes > 0) c0 = __ldg(q);
+      if ((int)s + bytes > 16) c1 = __ldg(q + 1);
+      r.a = first_bytes(words_at(c0, c1, s), bytes);
+      if constexpr (DT == MAXDNN_F32) {
+        uint4 c2 = make_uint4(0, 0, 0, 0);
+        if ((int)s + bytes > 32) c2 = __ldg(q + 2);
+        r.b = first_bytes(words_at(c1, c2, s), bytes - 16);
+      }
     }
   }
   return r;
@@ -347,9 +355,10 @@ __device__ __forceinline__ typename ElemOf<DT>::T from_float(float v) {
   else return __float2half_rn(v);
 }
 
-// Stores the first `n` values.  EDGE = false: n is 0 or 8 and p is aligned.
-template <int DT, bool EDGE = true>
-__device__ __forceinline__ void store_float8(typename ElemOf<DT>::T* p, const float (&v)[8], int n, bool vec) {
+// Stores the first `n` values.  EDGE = false: n is 0 or 8 and p is aligned.  EDGE = true: whole
+// vectors in the widest pieces that p's alignment allows.
+template <int DT, bool EDGE>
+__device__ __forceinline__ void store_float8(typename ElemOf<DT>::T* p, const float (&v)[8], int n) {
   static_assert(!is_fp8(DT), "8-bit values are stored by store_bytes8");
   constexpr int kWords = 2 * (int)sizeof(typename ElemOf<DT>::T);
   uint32_t w[kWords];
@@ -368,10 +377,24 @@ __device__ __forceinline__ void store_float8(typename ElemOf<DT>::T* p, const fl
       }
     }
   }
-  if (!EDGE && n == 0) return;
-  if (!EDGE || (n == 8 && vec)) {
-    reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    if constexpr (DT == MAXDNN_F32) reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  if (n == 0) return;
+  const uint32_t s = EDGE ? (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u) : 0u;
+  if (!EDGE || (n == 8 && s == 0)) {
+#pragma unroll
+    for (int i = 0; i < kWords; i += 4)
+      reinterpret_cast<uint4*>(p)[i / 4] = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+  } else if (n == 8 && (s & 7u) == 0) {
+#pragma unroll
+    for (int i = 0; i < kWords; i += 2) reinterpret_cast<uint2*>(p)[i / 2] = make_uint2(w[i], w[i + 1]);
+  } else if (n == 8 && (s & 3u) == 0) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) reinterpret_cast<uint32_t*>(p)[i] = w[i];
+  } else if (n == 8) {               // 16-bit values at an odd place
+    uint16_t* h = reinterpret_cast<uint16_t*>(p);
+    h[0] = (uint16_t)w[0];
+#pragma unroll
+    for (int i = 0; i + 1 < kWords; ++i) *reinterpret_cast<uint32_t*>(h + 1 + 2 * i) = __funnelshift_r(w[i], w[i + 1], 16);
+    h[7] = (uint16_t)(w[kWords - 1] >> 16);
   } else {
 #pragma unroll 1
     for (int i = 0; i < n; ++i) {
@@ -390,17 +413,22 @@ __device__ __forceinline__ void store_float8(typename ElemOf<DT>::T* p, const fl
 }
 
 template <int DT, bool EDGE>
-__device__ __forceinline__ void store_pairs(typename ElemOf<DT>::T* p, const F2 (&v)[4], int n, bool vec) {
+__device__ __forceinline__ void store_pairs(typename ElemOf<DT>::T* p, const F2 (&v)[4], int n) {
   float f[8];
   to_floats(v, f);
-  store_float8<DT, EDGE>(p, f, n, vec);
+  store_float8<DT, EDGE>(p, f, n);
 }
 
+// The first `n` of eight bytes; EDGE as above.
 template <bool EDGE>
-__device__ __forceinline__ void store_bytes8(uint8_t* p, uint2 w, int n, bool vec) {
-  if (!EDGE && n == 0) return;
-  if (!EDGE || (n == 8 && vec)) {
+__device__ __forceinline__ void store_bytes8(uint8_t* p, uint2 w, int n) {
+  if (n == 0) return;
+  const uint32_t s = EDGE ? (uint32_t)(reinterpret_cast<uintptr_t>(p) & 7u) : 0u;
+  if (!EDGE || (n == 8 && s == 0)) {
     *reinterpret_cast<uint2*>(p) = w;
+  } else if (n == 8 && s == 4) {
+    reinterpret_cast<uint32_t*>(p)[0] = w.x;
+    reinterpret_cast<uint32_t*>(p)[1] = w.y;
   } else {
 #pragma unroll 1
     for (int i = 0; i < n; ++i) {
@@ -409,13 +437,6 @@ __device__ __forceinline__ void store_bytes8(uint8_t* p, uint2 w, int n, bool ve
       w.y >>= 8;
     }
   }
-}
-
-// A weight of run-time type (read once per kernel, not per row).
-__device__ __forceinline__ float load_weight(const void* p, int64_t i, int type) {
-  if (type == MAXDNN_F32) return static_cast<const float*>(p)[i];
-  if (type == MAXDNN_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-  return __half2float(static_cast<const __half*>(p)[i]);
 }
 
 }  // namespace maxdnn

@@ -360,9 +360,9 @@ gemm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
               float v[8];
 #pragma unroll
               for (int i = 0; i < 8; ++i) v[i] = tot[c + i];
-              if (args.c_type == MAXDNN_F32) store_float8<MAXDNN_F32>(static_cast<float*>(args.c) + at + n0 + c, v, 8, true);
-              else if (args.c_type == MAXDNN_BF16) store_float8<MAXDNN_BF16>(static_cast<__nv_bfloat16*>(args.c) + at + n0 + c, v, 8, true);
-              else store_float8<MAXDNN_F16>(static_cast<__half*>(args.c) + at + n0 + c, v, 8, true);
+              if (args.c_type == MAXDNN_F32) store_float8<MAXDNN_F32, false>(static_cast<float*>(args.c) + at + n0 + c, v, 8);
+              else if (args.c_type == MAXDNN_BF16) store_float8<MAXDNN_BF16, false>(static_cast<__nv_bfloat16*>(args.c) + at + n0 + c, v, 8);
+              else store_float8<MAXDNN_F16, false>(static_cast<__half*>(args.c) + at + n0 + c, v, 8);
             }
           } else {
 #pragma unroll

@@ -29,7 +29,7 @@ struct LayerNormArgs {
   float* partial;              // [grid][2][cols] sums of a CTA's rows: dy xh, dy
   int64_t ldx, ldy, ldq;
   int32_t rows, cols, w_type;
-  int32_t vec_x, vec_y, vec_w; // rows (weights) allow the wide loads
+  int32_t whole;               // vectors of eight columns are whole and aligned (the host's choice of instance)
   int32_t q_e5m2;
   float eps, inv_cols;
 };
@@ -52,8 +52,8 @@ __device__ __forceinline__ void norm_pack_as(const F2 (&v)[4], const F2 (&w)[4],
     bv = exact_byte<QT>(v, &fv);
     bw = exact_byte<QT>(w, &fw);
   }
-  store_bytes8<EDGE>(qv, pack8<QT>(v, inv_scale_of(bv), fv), nv, true);
-  store_bytes8<EDGE>(qw, pack8<QT>(w, inv_scale_of(bw), fw), nw, true);
+  store_bytes8<EDGE>(qv, pack8<QT>(v, inv_scale_of(bv), fv), nv);
+  store_bytes8<EDGE>(qw, pack8<QT>(w, inv_scale_of(bw), fw), nw);
   if ((lane & 15) == 0) {
     if (nv > 0) *sv = (uint8_t)bv;
     if (nw > 0) *sw = (uint8_t)bw;
@@ -72,16 +72,16 @@ __device__ __forceinline__ void norm_pack(const F2 (&v)[4], const F2 (&w)[4], bo
 
 // Eight neighbouring weights.
 template <bool EDGE>
-__device__ __forceinline__ void load_weights8(const void* p, int c, int n, int type, bool vec, float none, F2 (&w)[4]) {
+__device__ __forceinline__ void load_weights8(const void* p, int c, int n, int type, float none, F2 (&w)[4]) {
   if (!p || n == 0) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = f2(none);
   } else if (type == MAXDNN_F32) {
-    to_pairs<MAXDNN_F32>(load_raw8<MAXDNN_F32, EDGE>(static_cast<const float*>(p) + c, n, vec), w);
+    to_pairs<MAXDNN_F32>(load_raw8<MAXDNN_F32, EDGE>(static_cast<const float*>(p) + c, n), w);
   } else if (type == MAXDNN_BF16) {
-    to_pairs<MAXDNN_BF16>(load_raw8<MAXDNN_BF16, EDGE>(static_cast<const __nv_bfloat16*>(p) + c, n, vec), w);
+    to_pairs<MAXDNN_BF16>(load_raw8<MAXDNN_BF16, EDGE>(static_cast<const __nv_bfloat16*>(p) + c, n), w);
   } else {
-    to_pairs<MAXDNN_F16>(load_raw8<MAXDNN_F16, EDGE>(static_cast<const __half*>(p) + c, n, vec), w);
+    to_pairs<MAXDNN_F16>(load_raw8<MAXDNN_F16, EDGE>(static_cast<const __half*>(p) + c, n), w);
   }
 }
 
@@ -145,10 +145,10 @@ layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
       for (int c = 8 * (int)threadIdx.x; c < padded; c += 8 * kNormThreads) {
         const int n = vector_cols<EDGE>(args.cols, c);
         F2 w[4];
-        load_weights8<EDGE>(args.gamma, c, n, args.w_type, true, 1.f, w);
+        load_weights8<EDGE>(args.gamma, c, n, args.w_type, 1.f, w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) *reinterpret_cast<F2*>(&weights[c + 2 * i]) = w[i];
-        load_weights8<EDGE>(args.beta, c, n, args.w_type, true, 0.f, w);
+        load_weights8<EDGE>(args.beta, c, n, args.w_type, 0.f, w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) *reinterpret_cast<F2*>(&weights[padded + c + 2 * i]) = w[i];
       }
@@ -172,7 +172,7 @@ layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int c = 8 * (t + 32 * WR * j);
-      raw[j] = load_raw8<XT, EDGE>(x + r * args.ldx + c, vector_cols<EDGE>(args.cols, c), args.vec_x != 0);
+      raw[j] = load_raw8<XT, EDGE>(x + r * args.ldx + c, vector_cols<EDGE>(args.cols, c));
     }
     F2 sum = 0;
 #pragma unroll
@@ -232,11 +232,11 @@ layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
             b[e] = bb.x; b[e + 1] = bb.y;
           }
         } else {
-          load_weights8<EDGE>(args.gamma, c, n[i], args.w_type, args.vec_w != 0, 1.f, g);
-          load_weights8<EDGE>(args.beta, c, n[i], args.w_type, args.vec_w != 0, 0.f, b);
+          load_weights8<EDGE>(args.gamma, c, n[i], args.w_type, 1.f, g);
+          load_weights8<EDGE>(args.beta, c, n[i], args.w_type, 0.f, b);
         }
         normalise8<EDGE>(v[i], minus_mean, f2(rstd), g, b, n[i]);
-        if (args.y) store_pairs<XT, EDGE>(yp + kStep * (j + i), v[i], n[i], args.vec_y != 0);
+        if (args.y) store_pairs<XT, EDGE>(yp + kStep * (j + i), v[i], n[i]);
       }
       if (args.q)
         norm_pack<QT, EDGE>(v[0], v[1], args.q_e5m2, qp + kStep * j, qp + kStep * (j + 1), sqp + scale_step * j,
@@ -310,7 +310,7 @@ layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     const int c = 8 * (t + threads * j);
-    load_weights8<true>(args.gamma, c, min(max(args.cols - c, 0), 8), args.w_type, args.vec_w != 0, 1.f, g[j]);
+    load_weights8<true>(args.gamma, c, min(max(args.cols - c, 0), 8), args.w_type, 1.f, g[j]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) dg[j][i] = db[j][i] = 0;
   }
@@ -325,8 +325,8 @@ layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
     for (int j = 0; j < J; ++j) {
       const int c = 8 * (t + threads * j);
       const int n = min(max(args.cols - c, 0), 8);
-      rx[j] = load_raw8<XT, EDGE>(x + r * args.ldx + c, n, args.vec_x != 0);
-      rdy[j] = load_raw8<YT, EDGE>(dy + r * args.ldy + c, n, args.vec_y != 0);
+      rx[j] = load_raw8<XT, EDGE>(x + r * args.ldx + c, n);
+      rdy[j] = load_raw8<YT, EDGE>(dy + r * args.ldy + c, n);
       scale[j] = 1.f;
       if constexpr (is_fp8(XT)) scale[j] = n > 0 ? e8m0_value(args.x_scale[(int64_t)(c >> 7) * args.rows + r]) : 0.f;
     }
@@ -355,7 +355,7 @@ layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
       const int c = 8 * (t + threads * j);
       F2 o[4];
       norm_dx8(xh[j], e[j], rstd, s1, s2, o);
-      store_pairs<YT, EDGE>(dx + r * args.ldy + c, o, min(max(args.cols - c, 0), 8), args.vec_y != 0);
+      store_pairs<YT, EDGE>(dx + r * args.ldy + c, o, min(max(args.cols - c, 0), 8));
     }
   }
   if (!args.partial) return;
@@ -462,7 +462,7 @@ layer_norm_bprop_ring_kernel(const __grid_constant__ LayerNormArgs args, int dep
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     const int c = 8 * (t + threads * j);
-    load_weights8<true>(args.gamma, c, c < args.cols ? 8 : 0, args.w_type, args.vec_w != 0, 1.f, g[j]);
+    load_weights8<true>(args.gamma, c, c < args.cols ? 8 : 0, args.w_type, 1.f, g[j]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) dg[j][i] = db[j][i] = 0;
   }
@@ -530,7 +530,7 @@ layer_norm_bprop_ring_kernel(const __grid_constant__ LayerNormArgs args, int dep
         const int c = 8 * (t + threads * j);
         F2 o[4];
         norm_dx8(xh[j], e[j], rstd, s1, s2, o);
-        store_pairs<YT, false>(dx + r * args.ldy + c, o, c < args.cols ? 8 : 0, true);
+        store_pairs<YT, false>(dx + r * args.ldy + c, o, c < args.cols ? 8 : 0);
       }
       slot = slot + 1 == depth ? 0 : slot + 1;
     }
@@ -598,7 +598,7 @@ __global__ void __launch_bounds__(1024) layer_norm_fprop_long_kernel(const __gri
         const int c = 8 * t + 8192 * j;
         const int n = min(max(args.cols - c, 0), 8);
         F2 v[4], none[4] = {};
-        to_pairs<XT>(load_raw8<XT, true>(x + r * args.ldx + c, n, args.vec_x != 0), v);
+        to_pairs<XT>(load_raw8<XT, true>(x + r * args.ldx + c, n), v);
         if (pass == 0) {
           acc += sum2(add2(add2(v[0], v[1]), add2(v[2], v[3])));
         } else if (pass == 1) {
@@ -608,10 +608,10 @@ __global__ void __launch_bounds__(1024) layer_norm_fprop_long_kernel(const __gri
             norm_pack<kEitherFp8, true>(v, none, args.q_e5m2, args.c + r * args.ldq + c, nullptr,
                                         args.sc + (int64_t)(c >> 7) * args.rows + r, nullptr, n, 0, lane);
           F2 g[4], b[4];
-          load_weights8<true>(args.gamma, c, n, args.w_type, args.vec_w != 0, 1.f, g);
-          load_weights8<true>(args.beta, c, n, args.w_type, args.vec_w != 0, 0.f, b);
+          load_weights8<true>(args.gamma, c, n, args.w_type, 1.f, g);
+          load_weights8<true>(args.beta, c, n, args.w_type, 0.f, b);
           normalise8<true>(v, f2(-mean), f2(rstd), g, b, n);
-          if (args.y) store_pairs<XT, true>(y + r * args.ldy + c, v, n, args.vec_y != 0);
+          if (args.y) store_pairs<XT, true>(y + r * args.ldy + c, v, n);
           if (args.q)
             norm_pack<kEitherFp8, true>(v, none, args.q_e5m2, args.q + r * args.ldq + c, nullptr,
                                         args.s + (int64_t)(c >> 7) * args.rows + r, nullptr, n, 0, lane);
@@ -653,16 +653,19 @@ __global__ void __launch_bounds__(1024) layer_norm_bprop_long_kernel(const __gri
         const int c = 8 * t + 8192 * j;
         const int n = min(max(args.cols - c, 0), 8);
         float xh[8], e[8];
-        to_float8<XT>(load_raw8<XT, EDGE>(x + r * args.ldx + c, n, args.vec_x != 0), xh);
-        to_float8<YT>(load_raw8<YT, EDGE>(dy + r * args.ldy + c, n, args.vec_y != 0), e);
+        to_float8<XT>(load_raw8<XT, EDGE>(x + r * args.ldx + c, n), xh);
+        to_float8<YT>(load_raw8<YT, EDGE>(dy + r * args.ldy + c, n), e);
         float scale = 1.f;
         if constexpr (is_fp8(XT)) scale = n > 0 ? e8m0_value(args.x_scale[(int64_t)(c >> 7) * args.rows + r]) : 0.f;
-        float o[8];
+        F2 g2[4];
+        float g8[8], o[8];
+        load_weights8<true>(args.gamma, c, n, args.w_type, 1.f, g2);
+        to_floats(g2, g8);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           if constexpr (is_fp8(XT)) xh[i] *= scale;
           xh[i] = i < n ? (xh[i] - mean) * rstd : 0.f;
-          const float g = (args.gamma && i < n) ? load_weight(args.gamma, c + i, args.w_type) : 1.f;
+          const float g = g8[i];
           if (pass == 0) {
             if (out && i < n) {
               float* pg = out + c + i;
@@ -676,7 +679,7 @@ __global__ void __launch_bounds__(1024) layer_norm_bprop_long_kernel(const __gri
             o[i] = rstd * (e[i] * g - s1 - xh[i] * s2);
           }
         }
-        if (pass == 1) store_float8<YT, EDGE>(static_cast<TY*>(args.dx) + r * args.ldy + c, o, n, args.vec_y != 0);
+        if (pass == 1) store_float8<YT, EDGE>(static_cast<TY*>(args.dx) + r * args.ldy + c, o, n);
       }
       if (pass == 1) break;
       s1 = warp_sum(s1);

@@ -49,7 +49,7 @@ maxdnn_status launch_norm_rows(const LayerNormArgs& a, int sm_count, cudaStream_
   const int64_t units = ((int64_t)a.rows + 8 / WR - 1) / (8 / WR);
   const int64_t most = (int64_t)sm_count * 4;
   const unsigned grid = (unsigned)(units < most ? units : most);
-  if (!(a.vec_x && a.vec_y && a.vec_w && a.cols % 8 == 0)) {
+  if (!a.whole) {
     layer_norm_fprop_kernel<XT, kEitherFp8, J, WR, true><<<grid, kNormThreads, 0, stream>>>(a);
     return launched();
   }
@@ -115,11 +115,9 @@ maxdnn_status layer_norm_fprop(const maxdnn_layer_norm_desc* d, const void* x, c
   a.rows = d->rows;
   a.cols = d->cols;
   a.w_type = d->w_type;
-  a.vec_x = vec_ok(d->x_type, d->ldx);
-  a.vec_y = vec_ok(d->y_type, d->ldy);
+  a.whole = vec_ok(d->x_type, d->ldx) && vec_ok(d->y_type, d->ldy) && aligned16(gamma) && aligned16(beta) && d->cols % 8 == 0;
   a.eps = d->eps;
   a.inv_cols = 1.f / (float)d->cols;
-  a.vec_w = aligned16(gamma) && aligned16(beta);
   a.q_e5m2 = (q || c) && d->q_type == MAXDNN_E5M2;
   return by_wide(d->x_type, [&](auto xt) { return launch_norm_fprop<decltype(xt)::value>(a, dev.sm_count, stream); });
 }
@@ -174,9 +172,7 @@ maxdnn_status layer_norm_bprop(const maxdnn_layer_norm_desc* d, const void* dy, 
   a.rows = d->rows;
   a.cols = d->cols;
   a.w_type = d->w_type;
-  a.vec_x = vec_ok(d->x_type, d->ldx);
-  a.vec_y = vec_ok(d->y_type, d->ldy);
-  a.vec_w = aligned16(gamma);
+  a.whole = vec_ok(d->x_type, d->ldx) && vec_ok(d->y_type, d->ldy) && aligned16(gamma) && d->cols % 8 == 0;
   a.inv_cols = 1.f / (float)d->cols;
   auto run = [&](auto xt, auto yt) {
     constexpr int X = decltype(xt)::value, Y = decltype(yt)::value;
@@ -201,7 +197,7 @@ maxdnn_status layer_norm_bprop(const maxdnn_layer_norm_desc* d, const void* dy, 
       kern<<<grid, sh.threads, smem, stream>>>(a, sh.depth);
       return launched();
     }
-    return by_edge(a.vec_x && a.vec_y && d->cols % 8 == 0, [&](auto edge) {
+    return by_edge(a.whole, [&](auto edge) {
       constexpr bool E = decltype(edge)::value != 0;
       if (sh.threads == 32 && sh.j == 1) layer_norm_bprop_kernel<X, Y, 1, true, E><<<grid, 128, 0, stream>>>(a);
       else if (sh.threads == 32 && sh.j == 2) layer_norm_bprop_kernel<X, Y, 2, true, E><<<grid, 128, 0, stream>>>(a);

@@ -22,7 +22,6 @@ struct Quant8Args {
   int64_t ldx, ldq;
   int32_t rows, cols;
   int32_t col_blocks;          // blocks of 128 columns
-  int32_t vec_x;               // rows of x allow the wide load
 };
 
 template <int XT, int QT, bool EDGE>
@@ -44,7 +43,7 @@ __global__ void __launch_bounds__(kQuantThreads, XT == MAXDNN_F32 ? 2 : 3) quant
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const int r = r0 + rg + 16 * k;
-    raw[k] = load_raw8<XT, EDGE>(x + (int64_t)r * args.ldx + c0, r < args.rows ? n : 0, args.vec_x != 0);
+    raw[k] = load_raw8<XT, EDGE>(x + (int64_t)r * args.ldx + c0, r < args.rows ? n : 0);
     if constexpr (is_fp8(XT))
       xs[k] = r < args.rows ? e8m0_value(args.x_scale[(int64_t)cb * args.rows + r]) : 0.f;
   }
@@ -89,7 +88,7 @@ __global__ void __launch_bounds__(kQuantThreads, XT == MAXDNN_F32 ? 2 : 3) quant
       // one row at a time, from memory again: registers cannot be indexed
       const int r = r0 + rg + 16 * k;
       float f[8];
-      to_float8<XT>(load_raw8<XT, true>(x + (int64_t)r * args.ldx + c0, r < args.rows ? n : 0, args.vec_x != 0), f);
+      to_float8<XT>(load_raw8<XT, true>(x + (int64_t)r * args.ldx + c0, r < args.rows ? n : 0), f);
       float scale = 1.f, m = 0.f;
       if constexpr (is_fp8(XT)) scale = r < args.rows ? e8m0_value(args.x_scale[(int64_t)cb * args.rows + r]) : 0.f;
 #pragma unroll
@@ -109,7 +108,7 @@ __global__ void __launch_bounds__(kQuantThreads, XT == MAXDNN_F32 ? 2 : 3) quant
     if (r >= args.rows) return;
     F2 v[4];
     values(k, v);
-    store_bytes8<EDGE>(q + (int64_t)r * args.ldq + c0, pack8<QT>(v, inv, fix), n, true);
+    store_bytes8<EDGE>(q + (int64_t)r * args.ldq + c0, pack8<QT>(v, inv, fix), n);
   };
 
   if (args.q_row) {
@@ -181,7 +180,6 @@ struct Dequant8Args {
   int32_t rows, cols;
   int32_t col_blocks;
   int32_t block;               // maxdnn_block
-  int32_t vec_x, vec_q;
 };
 
 // The same tile and the same eight columns x eight rows in each thread.
@@ -199,7 +197,7 @@ __global__ void __launch_bounds__(kQuantThreads) dequant8_kernel(const __grid_co
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const int r = r0 + 16 * k;
-    raw[k] = load_raw8<QT, EDGE>(args.q + (int64_t)r * args.ldq + c0, r < args.rows ? n : 0, args.vec_q != 0);
+    raw[k] = load_raw8<QT, EDGE>(args.q + (int64_t)r * args.ldq + c0, r < args.rows ? n : 0);
     byte[k] = 127;
     if (args.block == MAXDNN_BLOCK_ROW && r < args.rows) byte[k] = args.s[(int64_t)cb * args.rows + r];
   }
@@ -224,7 +222,7 @@ __global__ void __launch_bounds__(kQuantThreads) dequant8_kernel(const __grid_co
     const float m = e8m0_value(byte[k]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = args.block == MAXDNN_BLOCK_ROW ? v[i] * m : v[i] * s[i];
-    store_float8<XT, EDGE>(static_cast<T*>(args.x) + (int64_t)r * args.ldx + c0, v, n, args.vec_x != 0);
+    store_float8<XT, EDGE>(static_cast<T*>(args.x) + (int64_t)r * args.ldx + c0, v, n);
   }
 }
 

@@ -42,11 +42,10 @@ maxdnn_status quant8(const maxdnn_quant8_desc* d, const void* x, const void* x_s
   a.rows = d->rows;
   a.cols = d->cols;
   a.col_blocks = (int32_t)blocks_of(d->cols);
-  a.vec_x = vec_ok(d->x_type, d->ldx);
   const unsigned grid = (unsigned)(blocks_of(d->rows) * blocks_of(d->cols));
   return by_any(d->x_type, [&](auto xt) {
     return by_fp8(d->q_type, [&](auto qt) {
-      return by_edge(a.vec_x && d->cols % 8 == 0, [&](auto edge) {
+      return by_edge(vec_ok(d->x_type, d->ldx) && d->cols % 8 == 0, [&](auto edge) {
         quant8_kernel<decltype(xt)::value, decltype(qt)::value, decltype(edge)::value != 0>
             <<<grid, kQuantThreads, 0, stream>>>(a);
         return launched();
@@ -75,12 +74,10 @@ maxdnn_status dequant8(const maxdnn_quant8_desc* d, int block, const void* q, co
   a.cols = d->cols;
   a.col_blocks = (int32_t)blocks_of(d->cols);
   a.block = block;
-  a.vec_x = vec_ok(d->x_type, d->ldx);
-  a.vec_q = vec_ok(d->q_type, d->ldq);
   const unsigned grid = (unsigned)(blocks_of(d->rows) * blocks_of(d->cols));
   return by_wide(d->x_type, [&](auto xt) {
     return by_fp8(d->q_type, [&](auto qt) {
-      return by_edge(a.vec_x && a.vec_q && d->cols % 8 == 0, [&](auto edge) {
+      return by_edge(vec_ok(d->x_type, d->ldx) && vec_ok(d->q_type, d->ldq) && d->cols % 8 == 0, [&](auto edge) {
         dequant8_kernel<decltype(xt)::value, decltype(qt)::value, decltype(edge)::value != 0>
             <<<grid, kQuantThreads, 0, stream>>>(a);
         return launched();
@@ -140,12 +137,12 @@ maxdnn_status act8_fprop(const maxdnn_act8_desc* d, const void* h, void* a_out, 
   a.rows = d->rows;
   a.cols = d->cols;
   a.col_blocks = (int32_t)blocks_of(d->cols);
-  a.vec_h = vec_ok(d->x_type, d->ldh);
-  a.vec_u = vec_ok(d->x_type, d->ldh, d->cols);
-  a.vec_a = vec_ok(d->x_type, d->lda);
-  a.vec_cu = d->cols % 8 == 0;
+  const bool vec_h = vec_ok(d->x_type, d->ldh);
+  const bool vec_u = vec_ok(d->x_type, d->ldh, d->cols);
+  const bool vec_a = vec_ok(d->x_type, d->lda);
+  const bool vec_cu = d->cols % 8 == 0;
   const unsigned grid = (unsigned)(((int64_t)d->rows + kActRows - 1) / kActRows * a.col_blocks);
-  const bool whole = a.vec_h && (!d->gated || (a.vec_u && a.vec_cu)) && a.vec_a && d->cols % 8 == 0;
+  const bool whole = vec_h && (!d->gated || (vec_u && vec_cu)) && vec_a && d->cols % 8 == 0;
   const int qt_code = (q || c) ? d->q_type : MAXDNN_E4M3;
   return by_wide(d->x_type, [&](auto xt) {
     return by_fp8(qt_code, [&](auto qt) {
@@ -184,13 +181,13 @@ maxdnn_status act8_bprop(const maxdnn_act8_desc* d, const void* da, const void* 
   a.cols = d->cols;
   a.col_blocks = (int32_t)blocks_of(d->cols);
   const int64_t ldh = packed ? d->ldc : d->ldh;
-  a.vec_h = vec_ok(d->h_type, ldh);
-  a.vec_u = vec_ok(d->h_type, ldh, d->cols);
-  a.vec_a = vec_ok(d->x_type, d->lda);
-  a.vec_dh = vec_ok(d->x_type, d->ldh);
-  a.vec_du = vec_ok(d->x_type, d->ldh, d->cols);
+  const bool vec_h = vec_ok(d->h_type, ldh);
+  const bool vec_u = vec_ok(d->h_type, ldh, d->cols);
+  const bool vec_a = vec_ok(d->x_type, d->lda);
+  const bool vec_dh = vec_ok(d->x_type, d->ldh);
+  const bool vec_du = vec_ok(d->x_type, d->ldh, d->cols);
   const unsigned grid = (unsigned)(((int64_t)d->rows + kActRows - 1) / kActRows * a.col_blocks);
-  const bool whole = a.vec_h && a.vec_a && a.vec_dh && (!d->gated || (a.vec_u && a.vec_du)) && d->cols % 8 == 0;
+  const bool whole = vec_h && vec_a && vec_dh && (!d->gated || (vec_u && vec_du)) && d->cols % 8 == 0;
   return by_wide(d->x_type, [&](auto xt) {
     auto run = [&](auto ht) {
       return by_act(d, [&](auto act, auto gated) {
