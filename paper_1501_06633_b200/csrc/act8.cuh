@@ -88,6 +88,8 @@ __device__ __forceinline__ void pack_rows8(const F2 (&v)[4], const F2 (&w)[4], u
 
 template <int XT, int QT, int ACT, bool GATED, bool EDGE>
 __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_constant__ Act8Args args) {
+  let_next_start();
+  wait_for_previous();
   typedef typename ElemOf<XT>::T T;
   __shared__ uint8_t bytes[3][kActRows];
   const int t = threadIdx.x;
@@ -166,6 +168,8 @@ __global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_co
 // HT: the type of h (wide, or packed); XT: of da and dh.
 template <int HT, int XT, int ACT, bool GATED, bool EDGE>
 __global__ void __launch_bounds__(kActThreads) act8_bprop_kernel(const __grid_constant__ Act8Args args) {
+  let_next_start();
+  wait_for_previous();
   typedef typename ElemOf<HT>::T TH;
   typedef typename ElemOf<XT>::T T;
   const int t = threadIdx.x;

@@ -16,8 +16,30 @@ inline int vec_ok(int dt, int64_t ld, int64_t off = 0) {
   return (ld * elem_bytes(dt)) % unit == 0 && (off * elem_bytes(dt)) % unit == 0;
 }
 
-inline maxdnn_status launched() {
-  if (cudaGetLastError() != cudaSuccess) return MAXDNN_CUDA_ERROR;
+// A launch that may start while the kernel before it in the stream still runs (the kernels wait for
+// its end themselves: wait_for_previous).  Two calls in a row of a few microseconds each overlap
+// their starts: 1.5 to 2 us less for the second.
+template <class... P, class... A>
+maxdnn_status launch_early(void (*kern)(P...), unsigned grid, unsigned threads, size_t smem, int cluster,
+                           cudaStream_t stream, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid, 1, 1);
+  cfg.blockDim = dim3(threads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  if (cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...) != cudaSuccess) {
+    cudaGetLastError();
+    return MAXDNN_CUDA_ERROR;
+  }
   runtime_count_launch();
   return MAXDNN_OK;
 }

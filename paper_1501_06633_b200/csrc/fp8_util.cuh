@@ -22,6 +22,12 @@ namespace maxdnn {
 constexpr int kBlock8 = 128;       // values along a block
 constexpr int kLanesPerBlock = 16; // lanes of eight values that cover a block
 
+// Every kernel of these operators is launched so that it may start while the kernel before it in
+// the stream still runs (programmatic dependent launch): it lets the next one do the same at once and, before
+// it touches memory, waits until the one before has finished and its writes are visible.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 template <int DT> struct ElemOf;
 template <> struct ElemOf<MAXDNN_F32> { typedef float T; };
 template <> struct ElemOf<MAXDNN_BF16> { typedef __nv_bfloat16 T; };

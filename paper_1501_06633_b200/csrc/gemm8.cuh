@@ -202,6 +202,10 @@ gemm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
   __syncthreads();
   tcgen05_fence_after();
   const uint32_t tmem_base = *tmem_slot_ptr;
+  // Only now: a CTA of the next kernel that shares this SM takes its tensor memory after this one has
+  // its own (it holds it while it waits for this kernel's end).
+  let_next_start();
+  wait_for_previous();
 
   if (warp == 0) {
     // ------------------------------------------------------------ copies

@@ -53,36 +53,14 @@ maxdnn_status raise_smem(const RuntimeDevice& dev, std::atomic<bool> (&done)[64]
   return MAXDNN_OK;
 }
 
-template <class Kern, class... Args>
-maxdnn_status launch_clusters(Kern kern, const Gemm8Plan& p, int threads, int cluster, cudaStream_t stream,
-                              const Args&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)p.grid, 1, 1);
-  cfg.blockDim = dim3((unsigned)threads, 1, 1);
-  cfg.dynamicSmemBytes = (size_t)p.smem_bytes;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)cluster;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = cluster > 1 ? 1 : 0;
-  if (cudaLaunchKernelEx(&cfg, kern, args...) != cudaSuccess) {
-    cudaGetLastError();
-    return MAXDNN_CUDA_ERROR;
-  }
-  runtime_count_launch();
-  return MAXDNN_OK;
-}
-
 template <int NT, bool SBV>
 maxdnn_status launch_gemm8(const RuntimeDevice& dev, const Gemm8Plan& p, const CUtensorMap& ma, const CUtensorMap& mb,
                            const Gemm8Args& args, cudaStream_t stream) {
   static std::atomic<bool> done[64];
   const maxdnn_status st = raise_smem(dev, done, gemm8_kernel<NT, SBV>);
   if (st != MAXDNN_OK) return st;
-  return launch_clusters(gemm8_kernel<NT, SBV>, p, gemm8_threads(NT), p.split, stream, ma, mb, args);
+  return launch_early(gemm8_kernel<NT, SBV>, (unsigned)p.grid, gemm8_threads(NT), (size_t)p.smem_bytes, p.split, stream, ma, mb,
+                      args);
 }
 
 template <int NT, bool PAIR>
@@ -92,7 +70,8 @@ maxdnn_status launch_gemm8_mx(const RuntimeDevice& dev, const Gemm8Plan& p, cons
   static std::atomic<bool> done[64];
   const maxdnn_status st = raise_smem(dev, done, gemm8_mx_kernel<NT, PAIR>);
   if (st != MAXDNN_OK) return st;
-  return launch_clusters(gemm8_mx_kernel<NT, PAIR>, p, kMxThreads, PAIR ? 2 : p.split, stream, ma, mb, mc, args);
+  return launch_early(gemm8_mx_kernel<NT, PAIR>, (unsigned)p.grid, kMxThreads, (size_t)p.smem_bytes, PAIR ? 2 : p.split, stream,
+                      ma, mb, mc, args);
 }
 
 maxdnn_status gemm8_mx(const RuntimeDevice& dev, const maxdnn_gemm8_desc& d, const Gemm8Plan& p, const Operand& oa,

@@ -128,6 +128,8 @@ __host__ __device__ constexpr bool norm_shared_weights(int j, int wr) { return j
 template <int XT, int QT, int J, int WR, bool EDGE>
 __global__ void __launch_bounds__(kNormThreads, J > 4 ? 2 : XT == MAXDNN_F32 || EDGE ? 3 : 4)
 layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
+  let_next_start();
+  wait_for_previous();
   typedef typename ElemOf<XT>::T T;
   __shared__ float slots[8 / WR][2][WR];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -295,6 +297,8 @@ __device__ __forceinline__ void norm_dx8(const F2 (&xh)[4], const F2 (&e)[4], fl
 template <int XT, int YT, int J, bool WARP_ROW, bool EDGE>
 __global__ void __launch_bounds__(WARP_ROW ? 128 : 512)
 layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
+  let_next_start();
+  wait_for_previous();
   typedef typename ElemOf<XT>::T TX;
   typedef typename ElemOf<YT>::T TY;
   __shared__ float slots[2][2][kNormMaxWarps];
@@ -424,6 +428,8 @@ __host__ __device__ constexpr int norm_ring_row(int x_bytes, int y_bytes, int th
 template <int XT, int YT, int J, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS)
 layer_norm_bprop_ring_kernel(const __grid_constant__ LayerNormArgs args, int depth) {
+  let_next_start();
+  wait_for_previous();
   typedef typename ElemOf<XT>::T TX;
   typedef typename ElemOf<YT>::T TY;
   constexpr int XB = 8 * (int)sizeof(TX), YB = 8 * (int)sizeof(TY);
@@ -557,11 +563,12 @@ layer_norm_bprop_ring_kernel(const __grid_constant__ LayerNormArgs args, int dep
 // 16 warps takes every sixteenth sum, four at a time, and the warps' results are added in warp order.
 __global__ void __launch_bounds__(512) layer_norm_fold_kernel(const float* partial, int parts, int cols,
                                                               float* dgamma, float* dbeta) {
+  let_next_start();
+  wait_for_previous();
   __shared__ float part[16][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t c = (int64_t)blockIdx.x * 32 + lane, pitch = 2 * (int64_t)cols;
   float s[4] = {0.f, 0.f, 0.f, 0.f};
-  asm volatile("griddepcontrol.wait;" ::: "memory");     // launched while the sums' kernel still runs
   if (c < pitch) {
     const float* at = partial + c;
     int p = warp;
@@ -585,6 +592,8 @@ __global__ void __launch_bounds__(512) layer_norm_fold_kernel(const float* parti
 // comes from the second-level cache).  One CTA of 1024 threads per row, 8192 columns at a time.
 template <int XT>
 __global__ void __launch_bounds__(1024) layer_norm_fprop_long_kernel(const __grid_constant__ LayerNormArgs args) {
+  let_next_start();
+  wait_for_previous();
   typedef typename ElemOf<XT>::T T;
   __shared__ float slots[2][kNormMaxWarps];
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -634,6 +643,8 @@ __global__ void __launch_bounds__(1024) layer_norm_fprop_long_kernel(const __gri
 // (this CTA alone writes them, each thread always the same columns).
 template <int XT, int YT>
 __global__ void __launch_bounds__(1024) layer_norm_bprop_long_kernel(const __grid_constant__ LayerNormArgs args) {
+  let_next_start();
+  wait_for_previous();
   constexpr bool EDGE = true;
   typedef typename ElemOf<XT>::T TX;
   typedef typename ElemOf<YT>::T TY;

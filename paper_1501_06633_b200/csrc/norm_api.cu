@@ -50,13 +50,12 @@ maxdnn_status launch_norm_rows(const LayerNormArgs& a, int sm_count, cudaStream_
   const int64_t most = (int64_t)sm_count * 4;
   const unsigned grid = (unsigned)(units < most ? units : most);
   if (!a.whole) {
-    layer_norm_fprop_kernel<XT, kEitherFp8, J, WR, true><<<grid, kNormThreads, 0, stream>>>(a);
-    return launched();
+    return launch_early(layer_norm_fprop_kernel<XT, kEitherFp8, J, WR, true>, grid, kNormThreads, 0, 1, stream, a);
   }
   const size_t smem = norm_shared_weights(J, WR) ? 2 * 256 * WR * J * sizeof(float) : 0;     // at most 32 KB
-  if (a.q_e5m2) layer_norm_fprop_kernel<XT, MAXDNN_E5M2, J, WR, false><<<grid, kNormThreads, smem, stream>>>(a);
-  else layer_norm_fprop_kernel<XT, MAXDNN_E4M3, J, WR, false><<<grid, kNormThreads, smem, stream>>>(a);
-  return launched();
+  return launch_early(a.q_e5m2 ? layer_norm_fprop_kernel<XT, MAXDNN_E5M2, J, WR, false>
+                               : layer_norm_fprop_kernel<XT, MAXDNN_E4M3, J, WR, false>,
+                      grid, kNormThreads, smem, 1, stream, a);
 }
 
 // Vectors of eight columns per thread (J) and warps per row (WR).  Few rows (fewer than the SMs
@@ -78,8 +77,7 @@ maxdnn_status launch_norm_fprop(const LayerNormArgs& a, int sm_count, cudaStream
   if (vecs <= 1024) return launch_norm_rows<XT, 4, 8>(a, sm_count, stream);
   if (vecs <= 2048) return launch_norm_rows<XT, 8, 8>(a, sm_count, stream);
   const int64_t most = 2 * (int64_t)sm_count;
-  layer_norm_fprop_long_kernel<XT><<<(unsigned)(a.rows < most ? a.rows : most), 1024, 0, stream>>>(a);
-  return launched();
+  return launch_early(layer_norm_fprop_long_kernel<XT>, (unsigned)(a.rows < most ? a.rows : most), 1024, 0, 1, stream, a);
 }
 
 maxdnn_status layer_norm_fprop(const maxdnn_layer_norm_desc* d, const void* x, const void* gamma, const void* beta,
@@ -177,8 +175,7 @@ maxdnn_status layer_norm_bprop(const maxdnn_layer_norm_desc* d, const void* dy, 
   auto run = [&](auto xt, auto yt) {
     constexpr int X = decltype(xt)::value, Y = decltype(yt)::value;
     if (sh.threads == 0) {
-      layer_norm_bprop_long_kernel<X, Y><<<grid, 1024, 0, stream>>>(a);
-      return launched();
+      return launch_early(layer_norm_bprop_long_kernel<X, Y>, grid, 1024, 0, 1, stream, a);
     }
     if (sh.ring) {
       const int smem = sh.depth * norm_ring_row(elem_bytes(X), elem_bytes(Y), sh.threads, sh.j) +
@@ -194,16 +191,15 @@ maxdnn_status layer_norm_bprop(const maxdnn_layer_norm_desc* d, const void* dy, 
         }
         done[slot][dev.index].store(true, std::memory_order_release);
       }
-      kern<<<grid, sh.threads, smem, stream>>>(a, sh.depth);
-      return launched();
+      return launch_early(kern, grid, sh.threads, smem, 1, stream, a, sh.depth);
     }
     return by_edge(a.whole, [&](auto edge) {
       constexpr bool E = decltype(edge)::value != 0;
-      if (sh.threads == 32 && sh.j == 1) layer_norm_bprop_kernel<X, Y, 1, true, E><<<grid, 128, 0, stream>>>(a);
-      else if (sh.threads == 32 && sh.j == 2) layer_norm_bprop_kernel<X, Y, 2, true, E><<<grid, 128, 0, stream>>>(a);
-      else if (sh.threads == 32) layer_norm_bprop_kernel<X, Y, 4, true, E><<<grid, 128, 0, stream>>>(a);
-      else layer_norm_bprop_kernel<X, Y, 2, false, true><<<grid, sh.threads, 0, stream>>>(a);   // (whole vectors: the ring)
-      return launched();
+      if (sh.threads != 32)      // (whole vectors: the ring)
+        return launch_early(layer_norm_bprop_kernel<X, Y, 2, false, true>, grid, sh.threads, 0, 1, stream, a);
+      return launch_early(sh.j == 1 ? layer_norm_bprop_kernel<X, Y, 1, true, E>
+                          : sh.j == 2 ? layer_norm_bprop_kernel<X, Y, 2, true, E> : layer_norm_bprop_kernel<X, Y, 4, true, E>,
+                          grid, 128, 0, 1, stream, a);
     });
   };
   st = by_wide(d->y_type, [&](auto yt) {
@@ -211,21 +207,8 @@ maxdnn_status layer_norm_bprop(const maxdnn_layer_norm_desc* d, const void* dy, 
     return run(yt, yt);
   });
   if (st != MAXDNN_OK || !sums) return st;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((2 * (int64_t)d->cols + 31) / 32), 1, 1);
-  cfg.blockDim = dim3(512, 1, 1);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, layer_norm_fold_kernel, (const float*)a.partial, grid, (int)d->cols, dgamma, dbeta) !=
-      cudaSuccess) {
-    cudaGetLastError();
-    return MAXDNN_CUDA_ERROR;
-  }
-  return launched();
+  return launch_early(layer_norm_fold_kernel, (unsigned)((2 * (int64_t)d->cols + 31) / 32), 512, 0, 1, stream, a.partial, grid,
+                      d->cols, dgamma, dbeta);
 }
 
 }  // namespace

@@ -26,6 +26,8 @@ struct Quant8Args {
 
 template <int XT, int QT, bool EDGE>
 __global__ void __launch_bounds__(kQuantThreads, XT == MAXDNN_F32 ? 2 : 3) quant8_kernel(const __grid_constant__ Quant8Args args) {
+  let_next_start();
+  wait_for_previous();
   typedef typename ElemOf<XT>::T T;
   __shared__ float col_part[kQuantThreads / 32][kBlock8];   // per warp: maxima of its rows
   __shared__ float col_inv[kBlock8];
@@ -185,6 +187,8 @@ struct Dequant8Args {
 // The same tile and the same eight columns x eight rows in each thread.
 template <int XT, int QT, bool EDGE>
 __global__ void __launch_bounds__(kQuantThreads) dequant8_kernel(const __grid_constant__ Dequant8Args args) {
+  let_next_start();
+  wait_for_previous();
   typedef typename ElemOf<XT>::T T;
   const int t = threadIdx.x;
   const int cb = blockIdx.x % args.col_blocks;

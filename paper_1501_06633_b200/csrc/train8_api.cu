@@ -46,9 +46,7 @@ maxdnn_status quant8(const maxdnn_quant8_desc* d, const void* x, const void* x_s
   return by_any(d->x_type, [&](auto xt) {
     return by_fp8(d->q_type, [&](auto qt) {
       return by_edge(vec_ok(d->x_type, d->ldx) && d->cols % 8 == 0, [&](auto edge) {
-        quant8_kernel<decltype(xt)::value, decltype(qt)::value, decltype(edge)::value != 0>
-            <<<grid, kQuantThreads, 0, stream>>>(a);
-        return launched();
+        return launch_early(quant8_kernel<decltype(xt)::value, decltype(qt)::value, decltype(edge)::value != 0>, grid, kQuantThreads, 0, 1, stream, a);
       });
     });
   });
@@ -78,9 +76,7 @@ maxdnn_status dequant8(const maxdnn_quant8_desc* d, int block, const void* q, co
   return by_wide(d->x_type, [&](auto xt) {
     return by_fp8(d->q_type, [&](auto qt) {
       return by_edge(vec_ok(d->x_type, d->ldx) && vec_ok(d->q_type, d->ldq) && d->cols % 8 == 0, [&](auto edge) {
-        dequant8_kernel<decltype(xt)::value, decltype(qt)::value, decltype(edge)::value != 0>
-            <<<grid, kQuantThreads, 0, stream>>>(a);
-        return launched();
+        return launch_early(dequant8_kernel<decltype(xt)::value, decltype(qt)::value, decltype(edge)::value != 0>, grid, kQuantThreads, 0, 1, stream, a);
       });
     });
   });
@@ -148,9 +144,7 @@ maxdnn_status act8_fprop(const maxdnn_act8_desc* d, const void* h, void* a_out, 
     return by_fp8(qt_code, [&](auto qt) {
       return by_act(d, [&](auto act, auto gated) {
         return by_edge(whole, [&](auto edge) {
-          act8_fprop_kernel<decltype(xt)::value, decltype(qt)::value, decltype(act)::value, decltype(gated)::value != 0,
-                            decltype(edge)::value != 0><<<grid, kActThreads, 0, stream>>>(a);
-          return launched();
+          return launch_early(act8_fprop_kernel<decltype(xt)::value, decltype(qt)::value, decltype(act)::value, decltype(gated)::value != 0, decltype(edge)::value != 0>, grid, kActThreads, 0, 1, stream, a);
         });
       });
     });
@@ -192,9 +186,7 @@ maxdnn_status act8_bprop(const maxdnn_act8_desc* d, const void* da, const void* 
     auto run = [&](auto ht) {
       return by_act(d, [&](auto act, auto gated) {
         return by_edge(whole, [&](auto edge) {
-          act8_bprop_kernel<decltype(ht)::value, decltype(xt)::value, decltype(act)::value, decltype(gated)::value != 0,
-                            decltype(edge)::value != 0><<<grid, kActThreads, 0, stream>>>(a);
-          return launched();
+          return launch_early(act8_bprop_kernel<decltype(ht)::value, decltype(xt)::value, decltype(act)::value, decltype(gated)::value != 0, decltype(edge)::value != 0>, grid, kActThreads, 0, 1, stream, a);
         });
       });
     };
