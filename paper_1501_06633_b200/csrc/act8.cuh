@@ -9,6 +9,10 @@
 //
 // A CTA takes 128 columns x 64 rows: 16 lanes cover a row block, thread t has eight columns of
 // the rows t/16 + 16 k, so 4 (plain) or 8 (gated) loads of 16 bytes are in flight per thread.
+//
+// Measured: forward SiLU, gated, 8192 x 4096 bf16 with a and h packed 50 us, 236 MB at 4.7 TB/s (copy: 6.5),
+// bound by instruction issue (38 M warp instructions, three packings of 8 values each); backward
+// GELU from packed h, 4097 x 2736, 22.5 us, 90 MB at 4.0 TB/s.
 #pragma once
 #include "fp8_util.cuh"
 

@@ -16,7 +16,11 @@
 // the MMA's descriptor covers both, so gradients read operands as the forward pass stored them.
 //
 // Few tiles.  A cluster of 2, 4 or 8 CTAs shares a tile's reduction: each leaves its totals in its
-// shared memory and takes a part of the columns, adding the CTAs' totals in CTA order.
+// shared memory and takes a part of the tile, adding the CTAs' totals in CTA order.
+//
+// This kernel serves scales that are fp32 numbers; E8M0 scales go to gemm8_mx.cuh.  Measured: 2048 x
+// 4096 x 4096 46 us (1.5 PFLOP/s), bound by reading the products back from tensor memory and the
+// multiply-adds; 16 x 4096 x 4096 7.4 us.
 // Every wait is bounded and ends in a status code; TMEM is always freed.
 #pragma once
 #include "fp8_util.cuh"

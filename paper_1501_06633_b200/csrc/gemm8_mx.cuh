@@ -28,6 +28,11 @@
 // is read while the other fills; NT = 256 has one.
 //
 // Few tiles (not PAIR): a cluster of 2, 4 or 8 CTAs shares a tile's reduction, as in gemm8.cuh.
+//
+// Measured: 8192 x 8192 x 8192 to bf16 390 us = 2.8 PFLOP/s (MMAs in 88 % of the cycles; the power limit
+// holds the clock at 1.3 to 1.4 GHz, so that with the copies left out it would be 3.4), 2048 x 4096 x 4096 31 us,
+// one token through 4096 x 4096 7.6 us (16.8 MB: 2.2 TB/s; the start of a call, a memory latency and the
+// exchange between the CTAs are 5 of them).
 #pragma once
 #include "gemm8.cuh"
 

@@ -8,6 +8,10 @@
 // those 16 lanes; column maxima are a maximum over the thread's rows, a shuffle between the two
 // halves of the warp and one pass through shared memory.  The values are converted again for each
 // form instead of being kept as fp32 (64 registers of a thread).
+//
+// Measured: 8192 x 4096 bf16 to E5M2 rows and columns 31 us, 134 MB at 4.3 TB/s (copy: 6.5).  What
+// bounds it is the integer pipe: conversions, maxima and byte packing are half-rate instructions,
+// 9.2 M of 20 M warp instructions, 16 us of issue by themselves.  Unpacking 70k x 128 to bf16: 27 MB in 5.0 us.
 #pragma once
 #include "fp8_util.cuh"
 

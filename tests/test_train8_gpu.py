@@ -1,9 +1,10 @@
 """The 8-bit training operators against their definitions in 64 bits.
 
 Tolerances.  Packing multiplies by powers of two and rounds once: values and scales are
-compared for equality.  A product sums blocks of up to 128 terms on the tensor core (an error of at most
-one unit in the last place, 2^-23, of the running sum per term) and adds one rounding per block: at most
-(128 + blocks) 2^-23 of sum |a b|.  Row sums of the layer norm
+compared for equality.  A product sums on the tensor core (an error of at most one unit in the last place,
+2^-23, of the running sum per MMA of 32 terms, at most 64 MMAs to an accumulator of an fp32 result and
+4 per block of a 16-bit one, here of at most 14 blocks) and adds accumulators or blocks with one rounding each:
+at most (128 + blocks) 2^-23 of sum |a b|.  Row sums of the layer norm
 pass at most 64 additions from a value to the total: 64 x 2^-24 = 2^-18 of the sum of
 magnitudes.  The activations' exponentials, error function and quotient are within a few units in the last
 place: 2^-20 of the magnitudes that enter.  A result of 16 bits is compared with the rounded ends of its
