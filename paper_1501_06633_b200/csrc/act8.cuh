@@ -10,9 +10,9 @@
 // A CTA takes 128 columns x 64 rows: 16 lanes cover a row block, thread t has eight columns of
 // the rows t/16 + 16 k, so 4 (plain) or 8 (gated) loads of 16 bytes are in flight per thread.
 //
-// Measured: forward SiLU, gated, 8192 x 4096 bf16 with a and h packed 50 us, 236 MB at 4.7 TB/s (copy: 6.5),
-// bound by instruction issue (38 M warp instructions, three packings of 8 values each); backward
-// GELU from packed h, 4097 x 2736, 22.5 us, 90 MB at 4.0 TB/s.
+// Measured: forward SiLU, gated, 8192 x 4096 bf16 with a and h packed 46 us, 236 MB at 5.1 TB/s (copy: 6.5),
+// bound by instruction issue (38 M warp instructions, three packings of 8 values each; 50 us with
+// three CTAs of an SM instead of four); backward GELU from packed h, 4097 x 2736, 22 us, 90 MB at 4.0 TB/s.
 #pragma once
 #include "fp8_util.cuh"
 
@@ -91,7 +91,7 @@ __device__ __forceinline__ void pack_rows8(const F2 (&v)[4], const F2 (&w)[4], u
 }
 
 template <int XT, int QT, int ACT, bool GATED, bool EDGE>
-__global__ void __launch_bounds__(kActThreads) act8_fprop_kernel(const __grid_constant__ Act8Args args) {
+__global__ void __launch_bounds__(kActThreads, XT == MAXDNN_F32 ? 2 : 4) act8_fprop_kernel(const __grid_constant__ Act8Args args) {
   let_next_start();
   wait_for_previous();
   typedef typename ElemOf<XT>::T T;

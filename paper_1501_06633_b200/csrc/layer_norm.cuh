@@ -12,11 +12,11 @@
 // in 32 bits.  Sixteen neighbouring lanes hold a block of 128 columns, so the packed forms take
 // four shuffles for two blocks.
 //
-// Measured at 8192 x 4096 bf16 (copy: 6.5 TB/s): statistics alone 15 us (4.5 TB/s), y 33 us (4.1), y and x packed
-// 45 us (3.0: two packings, 28 M warp instructions at 0.65 a cycle and scheduler), backward from packed x
-// 51 us with the sums over rows (3.3).  Tried and slower: two rows at a time to share the weights
-// (50 us: half the warps), the next row prefetched in registers (51 us) or in a ring in shared memory (72 us,
-// the weights then fall out of the first-level cache), 48 registers and five CTAs (50 us).
+// Measured at 8192 x 4096 bf16 (copy: 6.5 TB/s): statistics alone 15 us (4.5 TB/s), y 27.5 us (4.9), y and x packed
+// 40 us (3.4: two packings, 28 M warp instructions), backward from packed x 50 us with the sums over
+// rows (3.4).  Tried when the packed forward pass took 45 us, and slower: two rows at a time to share
+// the weights (50 us: half the warps), the next row prefetched in registers (51 us) or in a ring in shared
+// memory (72 us, the weights then fall out of the first-level cache), 48 registers and five CTAs (50 us).
 #pragma once
 #include "fp8_util.cuh"
 #include "ptx_util.cuh"
@@ -130,7 +130,9 @@ __device__ __forceinline__ float squares8(const F2 (&v)[4], F2 minus_mean, int n
 // unrolled code no longer fits the instruction cache (8192 x 4096 with packed y and x: a third of
 // the stalls were for instructions, 89 us).
 constexpr int kNormThreads = 256;
-__host__ __device__ constexpr bool norm_shared_weights(int j, int wr) { return j == 4 && wr <= 4; }
+__host__ __device__ constexpr bool norm_shared_weights(int j, int wr) {
+  return (j == 4 && wr <= 4) || (j == 2 && wr == 1);
+}
 template <int XT, int QT, int J, int WR, bool EDGE>
 __global__ void __launch_bounds__(kNormThreads, J > 4 ? 2 : XT == MAXDNN_F32 || EDGE ? 3 : 4)
 layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
@@ -143,8 +145,9 @@ layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
   const T* x = static_cast<const T*>(args.x);
   T* y = static_cast<T*>(args.y);
   // The weights as fp32 in shared memory, for every row of the CTA: whatever their type, and where
-  // there are none (up to 4096 columns, 32 KB; 16384 x 1024: 25.8 -> 21.6 us with packed results.  With
-  // 64 KB for 8192 columns fewer CTAs fit an SM: 92 us become 125).
+  // there are none (up to 4096 columns, 32 KB; 16384 x 1024 with packed results: 25.8 us with the
+  // weights from the first-level cache, 19.9 from here.  With 64 KB for 8192 columns fewer CTAs fit an SM:
+  // 92 us became 125).
   constexpr bool kShared = norm_shared_weights(J, WR) && !EDGE;
   extern __shared__ __align__(16) float weights[];
   const int padded = 256 * WR * J;
