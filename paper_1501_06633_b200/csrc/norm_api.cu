@@ -36,11 +36,20 @@ maxdnn_status check_layer_norm(const maxdnn_layer_norm_desc* d) {
   return MAXDNN_OK;
 }
 
-// CTAs of the backward pass: each leaves one row of sums.
+// CTAs of the backward pass: each leaves one row of sums, which the fold reads again.  Where the CTAs
+// of a whole device would have fewer than four rows each, the sums cost more than the CTAs save, so
+// there are fewer of them, down to 64 (packed bf16, four rows a CTA against a full device: 512 x 4096
+// 17.8 against 19.5 us, 300 x 2048 14.0 against 15.7, 256 x 1280 8.1 against 11.1; with 32 CTAs
+// 128 x 8192 takes 20.0 against 18.3).  Rows that a warp takes alone leave a quarter of the sums
+// and stay on all SMs (1000 x 300: 9.7 against 13.4 us).
 int norm_bprop_grid(const maxdnn_layer_norm_desc& d, int sm_count, const NormShape& s) {
   const int64_t units = s.threads == 32 ? ((int64_t)d.rows + 3) / 4 : d.rows;
   const int per_sm = s.threads == 0 ? 1 : s.threads == 32 ? 4 : s.ring ? 512 / s.threads : s.threads >= 512 ? 1 : 512 / s.threads;
-  const int64_t most = (int64_t)sm_count * per_sm;
+  int64_t most = (int64_t)sm_count * per_sm;
+  if (s.ring) {
+    const int64_t few = d.rows / 4 < 64 ? 64 : d.rows / 4;
+    if (few < most) most = few;
+  }
   return (int)(units < most ? units : most);
 }
 
