@@ -568,10 +568,11 @@ layer_norm_bprop_ring_kernel(const __grid_constant__ LayerNormArgs args, int dep
     float a[8], b[8];
     to_floats(dg[j], a);
     to_floats(db[j], b);
+    // (whole vectors: cols is a multiple of 8, and so every part starts on 16 bytes)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      out[c + i] = a[i];
-      out[(int64_t)args.cols + c + i] = b[i];
+    for (int i = 0; i < 8; i += 4) {
+      *reinterpret_cast<float4*>(out + c + i) = make_float4(a[i], a[i + 1], a[i + 2], a[i + 3]);
+      *reinterpret_cast<float4*>(out + args.cols + c + i) = make_float4(b[i], b[i + 1], b[i + 2], b[i + 3]);
     }
   }
 }
