@@ -13,8 +13,8 @@
 // four shuffles for two blocks.
 //
 // Measured at 8192 x 4096 bf16 (copy: 6.5 TB/s): statistics alone 15 us (4.5 TB/s), y 27.5 us (4.9), y and x packed
-// 40 us (3.4: two packings, 28 M warp instructions), backward from packed x 50 us with the sums over
-// rows (3.4).  Tried when the packed forward pass took 45 us, and slower: two rows at a time to share
+// 40 us (3.4: two packings, 28 M warp instructions), backward from packed x 41.6 us with the sums over
+// rows (4.0).  Tried when the packed forward pass took 45 us, and slower: two rows at a time to share
 // the weights (50 us: half the warps), the next row prefetched in registers (51 us) or in a ring in shared
 // memory (72 us, the weights then fall out of the first-level cache), 48 registers and five CTAs (50 us).
 #pragma once
@@ -32,7 +32,7 @@ struct LayerNormArgs {
   uint8_t *q, *s, *c, *sc;     // fprop: packed y, packed x
   const void* dy;              // bprop
   void* dx;
-  float* partial;              // [grid][2][cols] sums of a CTA's rows: dy xh, dy
+  float* partial;              // [grid][2][norm_sums_pitch(cols)] sums of a CTA's rows: dy xh, dy
   int64_t ldx, ldy, ldq;
   int32_t rows, cols, w_type;
   int32_t whole;               // vectors of eight columns are whole and aligned (the host's choice of instance)
@@ -41,6 +41,20 @@ struct LayerNormArgs {
 };
 
 constexpr int kNormMaxWarps = 32;
+
+// Columns of a row of sums: whole vectors of eight, so that a thread's eight go in two 16-byte pieces
+// whatever the width (one by one, 32 bytes from lane to lane, the stores of 296 CTAs took 8 us of the 50 of
+// 8192 x 4096, and as much of the 18 of 128 x 8192).
+__host__ __device__ inline int64_t norm_sums_pitch(int cols) { return ((int64_t)cols + 7) / 8 * 8; }
+__device__ __forceinline__ void load_sums8(const float* p, float (&v)[8]) {    // (plain loads: the kernel wrote them)
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+  v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void store_sums8(float* p, const float (&v)[8]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -381,7 +395,8 @@ layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
   }
   if (!args.partial) return;
   // this CTA's sums over its rows; a CTA of several rows adds them warp by warp
-  float* out = args.partial + (int64_t)blockIdx.x * 2 * args.cols;
+  const int64_t pitch = norm_sums_pitch(args.cols);
+  float* out = args.partial + (int64_t)blockIdx.x * 2 * pitch;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     float a[J][8];
@@ -402,17 +417,15 @@ layer_norm_bprop_kernel(const __grid_constant__ LayerNormArgs args) {
       }
       for (int c = threadIdx.x; c < args.cols; c += blockDim.x) {
         const int vecj = c >> 8, l = (c >> 3) & 31, i = c & 7;
-        out[(int64_t)which * args.cols + c] = fold[(i * J + vecj) * 32 + l];
+        out[which * pitch + c] = fold[(i * J + vecj) * 32 + l];
       }
       __syncthreads();
     } else {
 #pragma unroll
-      for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int c = 8 * (t + threads * j) + i;
-          if (c < args.cols) out[(int64_t)which * args.cols + c] = a[j][i];
-        }
+      for (int j = 0; j < J; ++j) {
+        const int c = 8 * (t + threads * j);
+        if (c < args.cols) store_sums8(out + which * pitch + c, a[j]);
+      }
     }
   }
 }
@@ -560,7 +573,8 @@ layer_norm_bprop_ring_kernel(const __grid_constant__ LayerNormArgs args, int dep
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
   if (!args.partial) return;
-  float* out = args.partial + (int64_t)blockIdx.x * 2 * args.cols;
+  const int64_t pitch = norm_sums_pitch(args.cols);
+  float* out = args.partial + (int64_t)blockIdx.x * 2 * pitch;
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     const int c = 8 * (t + threads * j);
@@ -568,16 +582,12 @@ layer_norm_bprop_ring_kernel(const __grid_constant__ LayerNormArgs args, int dep
     float a[8], b[8];
     to_floats(dg[j], a);
     to_floats(db[j], b);
-    // (whole vectors: cols is a multiple of 8, and so every part starts on 16 bytes)
-#pragma unroll
-    for (int i = 0; i < 8; i += 4) {
-      *reinterpret_cast<float4*>(out + c + i) = make_float4(a[i], a[i + 1], a[i + 2], a[i + 3]);
-      *reinterpret_cast<float4*>(out + args.cols + c + i) = make_float4(b[i], b[i + 1], b[i + 2], b[i + 3]);
-    }
+    store_sums8(out + c, a);
+    store_sums8(out + pitch + c, b);
   }
 }
 
-// dg and db from the CTAs' sums, in CTA order.  A CTA takes 32 of the 2 x cols columns; each of its
+// dg and db from the CTAs' sums, in CTA order.  A CTA takes 32 of the 2 x pitch columns; each of its
 // 16 warps takes every sixteenth sum, four at a time, and the warps' results are added in warp order.
 __global__ void __launch_bounds__(512) layer_norm_fold_kernel(const float* partial, int parts, int cols,
                                                               float* dgamma, float* dbeta) {
@@ -585,7 +595,7 @@ __global__ void __launch_bounds__(512) layer_norm_fold_kernel(const float* parti
   wait_for_previous();
   __shared__ float part[16][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t c = (int64_t)blockIdx.x * 32 + lane, pitch = 2 * (int64_t)cols;
+  const int64_t c = (int64_t)blockIdx.x * 32 + lane, half = norm_sums_pitch(cols), pitch = 2 * half;
   float s[4] = {0.f, 0.f, 0.f, 0.f};
   if (c < pitch) {
     const float* at = partial + c;
@@ -602,8 +612,9 @@ __global__ void __launch_bounds__(512) layer_norm_fold_kernel(const float* parti
   float total = 0.f;
 #pragma unroll
   for (int w = 0; w < 16; ++w) total += part[w][lane];
-  if (c < cols) { if (dgamma) dgamma[c] = total; }
-  else if (dbeta) dbeta[c - cols] = total;
+  const int64_t col = c < half ? c : c - half;
+  float* to = c < half ? dgamma : dbeta;
+  if (to && col < cols) to[col] = total;
 }
 
 // Rows too long for the registers of a CTA: the same sums with the row read again for each (it
@@ -671,7 +682,8 @@ __global__ void __launch_bounds__(1024) layer_norm_bprop_long_kernel(const __gri
   const int steps = (args.cols + 8191) / 8192;
   const TX* x = static_cast<const TX*>(args.x);
   const TY* dy = static_cast<const TY*>(args.dy);
-  float* out = args.partial ? args.partial + (int64_t)blockIdx.x * 2 * args.cols : nullptr;
+  const int64_t pitch = norm_sums_pitch(args.cols);
+  float* out = args.partial ? args.partial + (int64_t)blockIdx.x * 2 * pitch : nullptr;
   bool first = true;
   int flip = 0;
   for (int64_t r = blockIdx.x; r < args.rows; r += gridDim.x, flip ^= 1) {
@@ -687,7 +699,12 @@ __global__ void __launch_bounds__(1024) layer_norm_bprop_long_kernel(const __gri
         float scale = 1.f;
         if constexpr (is_fp8(XT)) scale = n > 0 ? e8m0_value(args.x_scale[(int64_t)(c >> 7) * args.rows + r]) : 0.f;
         F2 g2[4];
-        float g8[8], o[8];
+        float g8[8], o[8], pg[8] = {}, pb[8] = {};
+        const bool add = pass == 0 && out && n > 0;
+        if (add && !first) {
+          load_sums8(out + c, pg);
+          load_sums8(out + pitch + c, pb);
+        }
         load_weights8<true>(args.gamma, c, n, args.w_type, 1.f, g2);
         to_floats(g2, g8);
 #pragma unroll
@@ -696,17 +713,17 @@ __global__ void __launch_bounds__(1024) layer_norm_bprop_long_kernel(const __gri
           xh[i] = i < n ? (xh[i] - mean) * rstd : 0.f;
           const float g = g8[i];
           if (pass == 0) {
-            if (out && i < n) {
-              float* pg = out + c + i;
-              float* pb = pg + args.cols;
-              *pg = first ? e[i] * xh[i] : fmaf(e[i], xh[i], *pg);
-              *pb = first ? e[i] : *pb + e[i];
-            }
+            pg[i] = fmaf(e[i], xh[i], pg[i]);
+            pb[i] += e[i];
             s1 = fmaf(e[i], g, s1);
             s2 = fmaf(e[i] * g, xh[i], s2);
           } else {
             o[i] = rstd * (e[i] * g - s1 - xh[i] * s2);
           }
+        }
+        if (add) {
+          store_sums8(out + c, pg);
+          store_sums8(out + pitch + c, pb);
         }
         if (pass == 1) store_float8<YT, EDGE>(static_cast<TY*>(args.dx) + r * args.ldy + c, o, n);
       }

@@ -37,17 +37,15 @@ maxdnn_status check_layer_norm(const maxdnn_layer_norm_desc* d) {
 }
 
 // CTAs of the backward pass: each leaves one row of sums, which the fold reads again.  Where the CTAs
-// of a whole device would have fewer than four rows each, the sums cost more than the CTAs save, so
-// there are fewer of them, down to 64 (packed bf16, four rows a CTA against a full device: 512 x 4096
-// 17.8 against 19.5 us, 300 x 2048 14.0 against 15.7, 256 x 1280 8.1 against 11.1; with 32 CTAs
-// 128 x 8192 takes 20.0 against 18.3).  Rows that a warp takes alone leave a quarter of the sums
-// and stay on all SMs (1000 x 300: 9.7 against 13.4 us).
+// of a whole device would have fewer than four rows each there are fewer of them, down to one per
+// SM (packed bf16: 1024 x 4096 13.3 us with 256 CTAs, 14.7 with 296; 512 x 4096 9.7 with 148, 11.5 with
+// 296; 300 x 2048 8.9 against 8.4.  Fewer than the SMs lose: 128 x 4096 8.7 with 64, 7.5 with 128).
 int norm_bprop_grid(const maxdnn_layer_norm_desc& d, int sm_count, const NormShape& s) {
   const int64_t units = s.threads == 32 ? ((int64_t)d.rows + 3) / 4 : d.rows;
   const int per_sm = s.threads == 0 ? 1 : s.threads == 32 ? 4 : s.ring ? 512 / s.threads : s.threads >= 512 ? 1 : 512 / s.threads;
   int64_t most = (int64_t)sm_count * per_sm;
   if (s.ring) {
-    const int64_t few = d.rows / 4 < 64 ? 64 : d.rows / 4;
+    const int64_t few = d.rows / 4 < sm_count ? sm_count : d.rows / 4;
     if (few < most) most = few;
   }
   return (int)(units < most ? units : most);
@@ -138,7 +136,7 @@ maxdnn_status layer_norm_bprop_workspace(const maxdnn_layer_norm_desc* d, size_t
     if ((st = runtime_device(&dev)) != MAXDNN_OK) return st;
     sm_count = dev.sm_count;
   }
-  *bytes = (size_t)norm_bprop_grid(*d, sm_count, norm_shape(*d)) * 2 * (size_t)d->cols * 4;
+  *bytes = (size_t)norm_bprop_grid(*d, sm_count, norm_shape(*d)) * 2 * (size_t)norm_sums_pitch(d->cols) * 4;
   return MAXDNN_OK;
 }
 
@@ -163,7 +161,7 @@ maxdnn_status layer_norm_bprop(const maxdnn_layer_norm_desc* d, const void* dy, 
   const NormShape sh = norm_shape(*d);
   const int grid = norm_bprop_grid(*d, dev.sm_count, sh);
   const bool sums = dgamma || dbeta;
-  if (sums && (!workspace || !aligned16(workspace) || workspace_bytes < (size_t)grid * 2 * (size_t)d->cols * 4))
+  if (sums && (!workspace || !aligned16(workspace) || workspace_bytes < (size_t)grid * 2 * (size_t)norm_sums_pitch(d->cols) * 4))
     return MAXDNN_INVALID_VALUE;
   LayerNormArgs a = {};
   a.x = x;
@@ -216,7 +214,7 @@ maxdnn_status layer_norm_bprop(const maxdnn_layer_norm_desc* d, const void* dy, 
     return run(yt, yt);
   });
   if (st != MAXDNN_OK || !sums) return st;
-  return launch_early(layer_norm_fold_kernel, (unsigned)((2 * (int64_t)d->cols + 31) / 32), 512, 0, 1, stream, a.partial, grid,
+  return launch_early(layer_norm_fold_kernel, (unsigned)((2 * norm_sums_pitch(d->cols) + 31) / 32), 512, 0, 1, stream, a.partial, grid,
                       d->cols, dgamma, dbeta);
 }
 
