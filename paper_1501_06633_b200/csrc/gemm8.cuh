@@ -21,7 +21,10 @@
 // This kernel serves scales that are fp32 numbers; E8M0 scales go to gemm8_mx.cuh.  Measured: 2048 x
 // 4096 x 4096 46 us (1.5 PFLOP/s), bound by reading the products back from tensor memory and the
 // multiply-adds; 16 x 4096 x 4096 7.4 us.
-// Every wait is bounded and ends in a status code; TMEM is always freed.
+// Every wait on a barrier in shared memory is bounded and ends in a status code; TMEM is always freed.
+// The waits without a limit are those for tensor memory and, at a cluster's end, for its CTAs: the
+// first ends with the CTA before it on the SM (clusters whose CTAs could hold one another up do not
+// fit an SM together: cluster_smem_floor), the second when the peers' bounded waits have.
 #pragma once
 #include "fp8_util.cuh"
 #include "gemm8.h"
@@ -58,7 +61,6 @@ struct Gemm8Args {
 __host__ __device__ constexpr int gemm8_cols_per_warp(int nt) { return nt < 64 ? nt : 64; }
 __host__ __device__ constexpr int gemm8_epi_warps(int nt) { return 4 * (nt < 64 ? 1 : nt / 64); }
 __host__ __device__ constexpr int gemm8_threads(int nt) { return 64 + 32 * gemm8_epi_warps(nt); }
-__host__ __device__ constexpr int gemm8_tmem_cols(int nt) { return 2 * nt < 32 ? 32 : 2 * nt; }
 
 __device__ __forceinline__ void tcgen05_mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc,
                                                uint32_t idesc, uint32_t accumulate) {

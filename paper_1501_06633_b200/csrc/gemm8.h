@@ -4,12 +4,25 @@
 #include <stdint.h>
 
 #include "../../include/maxdnn.h"
+#include "plan.h"
 
 namespace maxdnn {
 
 constexpr int kGemm8TileM = 128;     // rows of a tile (TMEM lanes)
 constexpr int kGemm8BlockK = 128;    // reduction steps per stage: one scale block
 constexpr int kGemm8MaxSplit = 8;    // CTAs of a cluster that share one tile's reduction
+
+// Tensor memory of a CTA.  gemm8.cuh: two accumulators of nt columns.  gemm8_mx.cuh: two where they
+// fit (else one), and kMxScaleTmem groups of scale columns: four for 128 rows of A, four for each
+// 128 columns of B.
+constexpr int kMxScaleTmem = 4;
+MAXDNN_HD constexpr int gemm8_tmem_cols(int nt) { return 2 * nt < 32 ? 32 : 2 * nt; }
+MAXDNN_HD constexpr int mx_buffers(int nt) { return nt <= 224 ? 2 : 1; }
+MAXDNN_HD constexpr int mx_sf_cols(int nt) { return 4 + 4 * ((nt + 127) / 128); }
+MAXDNN_HD constexpr int mx_tmem_cols(int nt) {
+  const int need = mx_buffers(nt) * nt + kMxScaleTmem * mx_sf_cols(nt);
+  return need <= 64 ? 64 : need <= 128 ? 128 : need <= 256 ? 256 : 512;
+}
 
 struct Gemm8Plan {
   int32_t mx;          // 1: the tensor core applies the scales (both operands' are E8M0 bytes)

@@ -42,16 +42,9 @@ constexpr int kMxThreads = 384;
 constexpr int kMxEpiWarps = 8;
 constexpr int kMxScaleBatch = 4;                   // scale groups (four blocks each) gathered at a time
 constexpr int kMxScaleBufs = 2 * kMxScaleBatch;    // groups in shared memory
-constexpr int kMxScaleTmem = 4;                    // groups in tensor memory
 
-__host__ __device__ constexpr int mx_buffers(int nt) { return nt <= 224 ? 2 : 1; }
 __host__ __device__ constexpr int mx_units(int nt) { return (nt + 63) / 64; }           // 32 columns each, per warp
-__host__ __device__ constexpr int mx_sf_cols(int nt) { return 4 + 4 * ((nt + 127) / 128); }
 __host__ __device__ constexpr int mx_sf_bytes(int nt) { return 128 * mx_sf_cols(nt); }
-__host__ __device__ constexpr int mx_tmem_cols(int nt) {
-  const int need = mx_buffers(nt) * nt + kMxScaleTmem * mx_sf_cols(nt);
-  return need <= 64 ? 64 : need <= 128 ? 128 : need <= 256 ? 256 : 512;
-}
 
 struct Gemm8MxArgs {
   Gemm8Scale sa, sb;

@@ -3,8 +3,6 @@
 
 #include <algorithm>
 
-#include "plan.h"
-
 namespace maxdnn {
 
 namespace {
@@ -131,6 +129,9 @@ maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* pl
     plan->stages = std::max(plan->stages, (need + ring - 1) / ring);
   }
   plan->smem_bytes = fixed + plan->stages * per_stage;
+  if (plan->pair || plan->split > 1)
+    plan->smem_bytes = std::max(plan->smem_bytes,
+                                cluster_smem_floor(plan->mx ? mx_tmem_cols(plan->tile_n) : gemm8_tmem_cols(plan->tile_n)));
   return MAXDNN_OK;
 }
 

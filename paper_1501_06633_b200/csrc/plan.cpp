@@ -4,6 +4,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <atomic>
 #include <mutex>
 
@@ -615,6 +616,7 @@ static maxdnn_status plan_umma_as(const ConvDims& d, int elem_bytes, int sm_coun
   g->stages = stages;
   g->smem_bytes = stages * stage + fixed;
   if (pair) {
+    g->smem_bytes = std::max(g->smem_bytes, cluster_smem_floor(512));
     const int pairs = sm_count / 2;
     g->grid = 2 * (g->n_tiles < pairs ? g->n_tiles : pairs);
   } else {
@@ -801,6 +803,7 @@ maxdnn_status plan_wgrad(const ConvDims& d, int elem_bytes, int sm_count, int fo
   g->smem_bytes = g->stages * (128 + (g->pair ? 128 : max_rows)) * 128 + 1024 + 1024 +
                   (tensor ? 2048 : 0);   // ring, alignment slack, barriers, row table
   if (g->pair) {
+    g->smem_bytes = std::max(g->smem_bytes, cluster_smem_floor(512));
     const int pairs = sm_count / 2;
     g->grid = 2 * (g->n_items < pairs ? g->n_items : pairs);
   } else {

@@ -100,6 +100,15 @@ struct KStepTable {
 #define MAXDNN_HD inline
 #endif
 
+// Dynamic shared memory that a CTA of a cluster asks for at least, when it allocates `tmem_cols` columns of
+// tensor memory.  An allocation waits until the columns are free, and the CTAs of a cluster
+// wait for one another: two clusters on different streams could each hold the columns of one SM and
+// wait for the other's.  So shared memory, which the hardware assigns to a CTA before it starts, is asked
+// for in the same proportion: CTAs that ask for more than 512 columns between them (544 at
+// least: allocations are multiples of 32) do not fit one SM (228 KB, of which each CTA takes 1 KB besides).
+constexpr int kSmSharedBytes = 228 * 1024;
+constexpr int cluster_smem_floor(int tmem_cols) { return (tmem_cols * kSmSharedBytes + 543) / 544 + 1 - 1024; }
+
 // Work items of the fp32 kernel (see ffma_conv.cuh): a whole tile, a contribution of
 // partial sums to a tile of the split tail, or the piece that finishes such a tile.
 enum FfmaItemKind : int { kItemWhole = 0, kItemContribute = 1, kItemFinish = 2 };
