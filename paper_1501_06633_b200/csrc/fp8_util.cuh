@@ -28,6 +28,12 @@ constexpr int kLanesPerBlock = 16; // lanes of eight values that cover a block
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// What a kernel before this one may have written while this one was already resident is read by
+// plain loads: the read-only path (ld.global.nc) is for memory that nobody writes during the
+// kernel's life, which begins before that wait.
+template <class T>
+__device__ __forceinline__ T load_global(const T* p) { return *p; }
+
 template <int DT> struct ElemOf;
 template <> struct ElemOf<MAXDNN_F32> { typedef float T; };
 template <> struct ElemOf<MAXDNN_BF16> { typedef __nv_bfloat16 T; };
@@ -251,15 +257,15 @@ __device__ __forceinline__ Raw8<DT> load_raw8(const typename ElemOf<DT>::T* p, i
     if constexpr (DT == MAXDNN_F32) {
       r.a = r.b = make_uint4(0, 0, 0, 0);
       if (n) {
-        r.a = __ldg(reinterpret_cast<const uint4*>(p));
-        r.b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
+        r.a = load_global(reinterpret_cast<const uint4*>(p));
+        r.b = load_global(reinterpret_cast<const uint4*>(p) + 1);
       }
     } else if constexpr (is_fp8(DT)) {
       r.a = make_uint2(0, 0);
-      if (n) r.a = __ldg(reinterpret_cast<const uint2*>(p));
+      if (n) r.a = load_global(reinterpret_cast<const uint2*>(p));
     } else {
       r.a = make_uint4(0, 0, 0, 0);
-      if (n) r.a = __ldg(reinterpret_cast<const uint4*>(p));
+      if (n) r.a = load_global(reinterpret_cast<const uint4*>(p));
     }
   } else {
     const uintptr_t at = reinterpret_cast<uintptr_t>(p);
@@ -268,20 +274,20 @@ __device__ __forceinline__ Raw8<DT> load_raw8(const typename ElemOf<DT>::T* p, i
       const uint32_t s = (uint32_t)(at & 7u);
       const uint2* q = reinterpret_cast<const uint2*>(at - s);
       uint2 lo = make_uint2(0, 0), hi = make_uint2(0, 0);
-      if (bytes > 0) lo = __ldg(q);
-      if ((int)s + bytes > 8) hi = __ldg(q + 1);
+      if (bytes > 0) lo = load_global(q);
+      if ((int)s + bytes > 8) hi = load_global(q + 1);
       const uint4 v = words_at(make_uint4(lo.x, lo.y, hi.x, hi.y), make_uint4(0, 0, 0, 0), s);
       r.a = make_uint2(first_bytes(v.x, bytes), first_bytes(v.y, bytes - 4));
     } else {
       const uint32_t s = (uint32_t)(at & 15u);
       const uint4* q = reinterpret_cast<const uint4*>(at - s);
       uint4 c0 = make_uint4(0, 0, 0, 0), c1 = c0;
-      if (bytes > 0) c0 = __ldg(q);
-      if ((int)s + bytes > 16) c1 = __ldg(q + 1);
+      if (bytes > 0) c0 = load_global(q);
+      if ((int)s + bytes > 16) c1 = load_global(q + 1);
       r.a = first_bytes(words_at(c0, c1, s), bytes);
       if constexpr (DT == MAXDNN_F32) {
         uint4 c2 = make_uint4(0, 0, 0, 0);
-        if ((int)s + bytes > 32) c2 = __ldg(q + 2);
+        if ((int)s + bytes > 32) c2 = load_global(q + 2);
         r.b = first_bytes(words_at(c1, c2, s), bytes - 16);
       }
     }

@@ -89,8 +89,8 @@ __device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr) {
 
 __device__ __forceinline__ float gemm8_scale(const Gemm8Scale& s, int i, int kb) {
   const int64_t at = (int64_t)(min(i, s.count - 1) >> s.shift) * s.step + (int64_t)kb * s.kstep;
-  return s.is_float ? __ldg(static_cast<const float*>(s.p) + at)
-                    : e8m0_value(__ldg(static_cast<const uint8_t*>(s.p) + at));
+  return s.is_float ? load_global(static_cast<const float*>(s.p) + at)
+                    : e8m0_value(load_global(static_cast<const uint8_t*>(s.p) + at));
 }
 
 __device__ __forceinline__ void gemm8_store1(void* c, int c_type, int64_t at, float v) {

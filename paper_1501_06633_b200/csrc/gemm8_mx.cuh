@@ -117,19 +117,19 @@ __device__ __forceinline__ void mx_load_scales(const Gemm8Scale& s, int row0, in
   if (s.shift) {    // row0 is a multiple of 16: the four rows have one scale
     p += (int64_t)(min(r, s.count - 1) >> s.shift) * s.step;
 #pragma unroll
-    for (int b = 0; b < 4; ++b) raw[b] = 0x01010101u * __ldg(p + (int64_t)min(kb + b, last) * s.kstep);
+    for (int b = 0; b < 4; ++b) raw[b] = 0x01010101u * load_global(p + (int64_t)min(kb + b, last) * s.kstep);
   } else {
     if (s.words && r + 3 < s.count) {
 #pragma unroll
       for (int b = 0; b < 4; ++b)
-        raw[b] = __ldg(reinterpret_cast<const uint32_t*>(p + (int64_t)min(kb + b, last) * s.kstep + r));
+        raw[b] = load_global(reinterpret_cast<const uint32_t*>(p + (int64_t)min(kb + b, last) * s.kstep + r));
     } else {
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const uint8_t* q = p + (int64_t)min(kb + b, last) * s.kstep;
         raw[b] = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) raw[b] |= (uint32_t)__ldg(q + min(r + i, s.count - 1)) << (8 * i);
+        for (int i = 0; i < 4; ++i) raw[b] |= (uint32_t)load_global(q + min(r + i, s.count - 1)) << (8 * i);
       }
     }
   }
