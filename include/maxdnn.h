@@ -492,8 +492,8 @@ maxdnn_status maxdnn_dequant8(const maxdnn_quant8_desc* desc, maxdnn_block block
  * were packed elsewhere; the product of two scales must be a finite fp32 number).  C: F32, BF16
  * or F16, row-major with pitch ldc, overwritten.  K = 0 writes zeros.
  * With E8M0 scales on both sides the tensor core applies them, and sums in its fp32 accumulator:
- * the whole reduction for a 16-bit C, 2048 steps at a time for an fp32 C, whose partial sums are added with
- * one rounding each (measured 3e-7 of the result over 16384 steps).  With an fp32 scale on either
+ * 16384 steps at a time for a 16-bit C, 2048 for an fp32 C; the partial sums are added with one rounding
+ * each (measured 3e-7 of an fp32 result over 16384 steps).  With an fp32 scale on either
  * side every block of 128 is scaled and added in registers.  Results do not change from run to run.
  * NOT_SUPPORTED: lda or ldb not a multiple of 16, a size above 2^30.
  */

@@ -29,7 +29,7 @@ struct Gemm8Plan {
   int32_t pair;        // 1: tiles of 256 rows on two SMs
   int32_t swap;        // 1: the kernel's rows are the columns of C (few rows of C)
   int32_t tile_n;      // columns of a tile
-  int32_t chunk;       // mx: blocks of the reduction per accumulator
+  int32_t chunk;       // mx: blocks of the reduction per accumulator (a multiple of four)
   int32_t bulk_c;      // mx: C is stored by bulk tensor copies
   int32_t staged_c;    // mx: C goes through staging tiles in shared memory
   int32_t split;       // CTAs that share a tile's reduction: 1, 2, 4 or 8

@@ -5,12 +5,15 @@
 //   C[m, n] = sum_k (a[m, k] 2^ea) (b[n, k] 2^eb)
 //
 // Nothing is left to do between the blocks of the reduction, so an accumulator takes a whole
-// chunk of it.  The tensor core truncates its fp32 accumulator at every MMA (towards zero); a
-// 16-bit result does not notice, and its chunk is the whole reduction.  An fp32 result takes chunks of sixteen
-// blocks (64 MMAs), which are added in registers with round-to-nearest.  Measured on a weight
-// gradient over 16384 tokens (error against 64 bits, relative, and time at 8192 x 4096): chunks of
+// chunk of it.  The tensor core truncates its fp32 accumulator at every MMA (towards zero), so terms of
+// one sign lose about half a unit of the running sum each time, and the loss grows with the length.
+// Chunks are added in registers with round-to-nearest.  An fp32 result takes chunks of sixteen
+// blocks (64 MMAs).  Measured on a weight gradient over 16384 tokens (error against 64 bits, relative,
+// and time at 8192 x 4096 in short runs at a high clock; 543 to 555 us back to back): chunks of
 // 4 blocks 1.1e-7, 674 us; 8: 1.6e-7, 512 us; 16: 3.0e-7, 462 us; none 1.5e-6, 460 us (fp32
-// arithmetic throughout: 3.6e-7).
+// arithmetic throughout: 3.6e-7).  A 16-bit result takes chunks of 128 blocks (512 MMAs): at most 6.2e-5
+// of it for terms of one sign, against 2.4e-4 for the rounding to fp16; with one accumulator for 2^18
+// terms of one sign its bf16 values were off, for 2^20 its fp16 values.
 //
 // Roles.  Warp 0 copies A, warp 3 copies B, warp 1 issues the MMAs, warp 2 gathers the scales:
 // the bytes of four blocks and 128 rows, which lie [block][row] in memory, become 32 rows of 16
@@ -337,7 +340,7 @@ gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       const uint64_t desc_a = desc | (uint64_t)((base & 0x3FFFFu) >> 4);
       const uint64_t desc_b = desc | (uint64_t)(((base + b_off) & 0x3FFFFu) >> 4);
       const uint32_t b_stage = (uint32_t)args.b_stage_bytes >> 4;
-      const int chunk = args.chunk;             // a multiple of four, or the whole reduction
+      const int chunk = args.chunk;             // a multiple of four
       int stage = 0;
       uint32_t phase = 0, group = 0, acc_n = 0;
       bool ok = true, ready = false;

@@ -67,8 +67,8 @@ maxdnn_status plan_gemm8(const maxdnn_gemm8_desc& d, int sm_count, Gemm8Plan* pl
       const int64_t tiles = m_tiles * n_tiles;
       const int b_stage = b_major == MAXDNN_MAJOR_MN ? std::max(rows_b, 128) * 128 : rows_b * 128;
       const int slots = s.pair ? sm_count / 2 : mx && s.nt <= 32 ? 2 * sm_count : sm_count;   // tiles that run side by side
-      // an fp32 result is added up from accumulators of sixteen blocks (gemm8_mx.cuh)
-      const int chunk = mx ? (d.c_type == MAXDNN_F32 ? 16 : std::max(k_blocks, 1)) : 1;
+      // results are added up from accumulators of so many blocks (gemm8_mx.cuh)
+      const int chunk = mx ? (d.c_type == MAXDNN_F32 ? 16 : 128) : 1;
       for (int split : kSplit) {
         if (option_is_set(OPT_GEMM8_SPLIT) && option(OPT_GEMM8_SPLIT) != split) continue;
         if (split > k_blocks || (split > 1 && s.pair)) continue;
