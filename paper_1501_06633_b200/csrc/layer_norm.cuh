@@ -298,12 +298,13 @@ __device__ __forceinline__ void norm_back8(const Raw8<XT>& rx, const Raw8<YT>& r
                                            F2* s1, F2* s2) {
   to_pairs<XT>(rx, xh);
   to_pairs<YT>(rdy, e);
-  // (scale x - mean) rstd as one multiply-add; the rounding of mean rstd is of the size that the
-  // mean itself was rounded by
-  const F2 k = f2(is_fp8(XT) ? scale * rstd : rstd), mm = f2(-mean * rstd);
+  // The difference first: one multiply-add with -mean rstd would round that product, 2e-5 of xh
+  // for rows at 1000 with a spread of 1, and leaves the range where mean rstd does.
+  // (Vectors past the row's end: zeros, so that they stay out of the sums.)
+  const F2 mm = f2(EDGE || n > 0 ? -mean : 0.f), rs = f2(rstd), sc = f2(scale);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    xh[i] = fma2(xh[i], k, mm);
+    xh[i] = mul2(is_fp8(XT) ? fma2(xh[i], sc, mm) : add2(xh[i], mm), rs);
     if (EDGE) {
       const float2 t = unf2(xh[i]);
       xh[i] = f2(2 * i < n ? t.x : 0.f, 2 * i + 1 < n ? t.y : 0.f);
@@ -539,7 +540,7 @@ layer_norm_bprop_ring_kernel(const __grid_constant__ LayerNormArgs args, int dep
           if constexpr (is_fp8(XT)) scale = e8m0_value(scales[(c >> 7) * kNormChunk + k]);
         }
         // (columns past the end: dy = 0 keeps them out of every sum)
-        norm_back8<XT, YT, false>(rx, rdy, scale, mean, rstd, g[j], 8, xh[j], e[j], dg[j], db[j], &p1, &p2);
+        norm_back8<XT, YT, false>(rx, rdy, scale, mean, rstd, g[j], c < args.cols ? 8 : 0, xh[j], e[j], dg[j], db[j], &p1, &p2);
       }
       // both sums in six shuffles: the halves of the warp take one each
       float s1 = sum2(p1), s2 = sum2(p2);
