@@ -553,7 +553,7 @@ maxdnn_status maxdnn_layer_norm_bprop(const maxdnn_layer_norm_desc* desc, const 
  *   SILU g / (1 + exp(-g));  GELU g P(g), P the normal distribution function;
  *   GELU_TANH g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2
  * With x_type F32, f is within a few units of its last place; with 16-bit types the factors of g are within
- * 2e-7 before the result is rounded (P: within 5e-5 of itself down to g = -3).
+ * 1e-6 before the result is rounded (P: within 3e-5 of itself however small it is).
  * Forward: a (x_type, pitch lda; may be null), (q, s): a packed in row blocks, the next product's
  * operand (may be null, not both), and (c, sc): h packed for the backward pass (may be null),
  * each half in row blocks of its own (u's blocks start at its first column): c [rows] with pitch

@@ -11,7 +11,7 @@ import torch
 from scipy import special
 
 import paper_1501_06633_b200 as mx
-from test_train8_gpu import ACTS, down
+from test_train8_gpu import ACTS, WIDE, as_held, down, within
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +61,19 @@ def test_fp32_activations_to_a_few_units(act, gated):
     assert np.all(np.abs(got[:cols] - da * uu * (t1 + t2)) <= tol_d * np.abs(da * uu) * size + tiny)
     if gated:
         assert np.all(np.abs(got[cols:] - da * f) <= tol * np.abs(da * f) + tiny)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_gelu_of_16_bit_values_far_below_zero(kind):
+    """f = g P(g) where P is small: a few roundings of the exponential's argument (up to 72), 3 x 72 x 2^-24 of the
+    value, and of its own growing error, 1.2 x 72 x 2^-23: 2^-15.  The result is rounded once."""
+    g = as_held(-np.linspace(2.0, 12.0, 997), kind)
+    n = g.size
+    h = torch.from_numpy(np.concatenate([g, np.ones(n)])).to(WIDE[kind][1]).cuda().view(1, 2 * n)
+    d = mx.Act8Desc.make(1, n, act=mx.ACT_GELU, x_type=WIDE[kind][0])
+    a, dh = (torch.empty(1, m * n, dtype=WIDE[kind][1], device="cuda") for m in (1, 2))
+    mx.act8_fprop(d, h, a=a)
+    mx.act8_bprop(d, torch.ones(1, n, dtype=WIDE[kind][1], device="cuda"), h, dh)
+    want = g * special.ndtr(g)
+    for got in (down(a)[0], down(dh)[0, n:]):
+        within(got, want, 2.0 ** -15 * np.abs(want), kind)
