@@ -522,7 +522,7 @@ maxdnn_status maxdnn_gemm8(const maxdnn_gemm8_desc* desc, const void* a, const v
  * reads), (q, s): y packed in row blocks, the next product's operand, and (c, sc): x packed in
  * row blocks, which the backward pass takes in place of x (both q_type, pitch ldq; y is packed
  * from its 32-bit value).  NOT_SUPPORTED: x_type other than y_type (forward; backward unless x
- * is packed).
+ * is packed), more than 2^30 columns.
  */
 typedef struct maxdnn_layer_norm_desc {
   int32_t rows, cols;

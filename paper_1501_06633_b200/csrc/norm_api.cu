@@ -33,6 +33,7 @@ maxdnn_status check_layer_norm(const maxdnn_layer_norm_desc* d) {
   if (d->ldx < d->cols || d->ldy < d->cols) return MAXDNN_INVALID_VALUE;
   if (!(d->eps >= 0.f) || d->eps > 3.0e38f) return MAXDNN_INVALID_VALUE;
   if (is_wide(d->x_type) && d->x_type != d->y_type) return MAXDNN_NOT_SUPPORTED;
+  if (d->cols > (1 << 30)) return MAXDNN_NOT_SUPPORTED;    // column numbers are 32 bits
   return MAXDNN_OK;
 }
 
