@@ -109,6 +109,16 @@ struct Call {
 
 PyObject* not_plain() { return PyLong_FromLong(-1); }
 
+// The library's call with the interpreter's lock released: a launch may wait (a full queue, a device's first
+// call), and other threads run meanwhile.  (The descriptor was copied before: it is a Python object's memory.)
+template <class F> PyObject* unlocked(F call) {
+  maxdnn_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = call();
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
 #define MAXDNN_TRY try {
 #define MAXDNN_CATCH } catch (...) { PyErr_Clear(); return not_plain(); }
 
@@ -116,7 +126,7 @@ PyObject* quant8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MAXDNN_TRY
   Call c(a, n, 10, sizeof(maxdnn_quant8_desc));
   if (!c.ok) return not_plain();
-  const auto& d = c.as<maxdnn_quant8_desc>();
+  const auto d = c.as<maxdnn_quant8_desc>();
   const int64_t r = d.rows, k = d.cols, rs = blocks(k) * r;
   void* x = c.mat(1, d.x_type, r, k, d.ldx);
   void* xs = d.x_type >= MAXDNN_E4M3 ? c.vec(2, MAXDNN_E8M0, rs) : nullptr;
@@ -126,7 +136,7 @@ PyObject* quant8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   c.pair(7, d.q_type, r, k, d.ldq, blocks(r) * blocks(k), &q[2], &s[2]);
   void* stream = c.stream(9);
   if (!c.ok) return not_plain();
-  return PyLong_FromLong(f_quant8(&d, x, xs, q[0], s[0], q[1], s[1], q[2], s[2], stream));
+  return unlocked([&] { return f_quant8(&d, x, xs, q[0], s[0], q[1], s[1], q[2], s[2], stream); });
   MAXDNN_CATCH
 }
 
@@ -134,7 +144,7 @@ PyObject* dequant8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MAXDNN_TRY
   Call c(a, n, 6, sizeof(maxdnn_quant8_desc));
   if (!c.ok) return not_plain();
-  const auto& d = c.as<maxdnn_quant8_desc>();
+  const auto d = c.as<maxdnn_quant8_desc>();
   const long block = PyLong_AsLong(a[1]);
   if (PyErr_Occurred() || block < 0 || block > 2) { PyErr_Clear(); return not_plain(); }
   const int64_t r = d.rows, k = d.cols;
@@ -143,7 +153,7 @@ PyObject* dequant8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* x = c.mat(4, d.x_type, r, k, d.ldx);
   void* stream = c.stream(5);
   if (!c.ok) return not_plain();
-  return PyLong_FromLong(f_dequant8(&d, (maxdnn_block)block, q, s, x, stream));
+  return unlocked([&] { return f_dequant8(&d, (maxdnn_block)block, q, s, x, stream); });
   MAXDNN_CATCH
 }
 
@@ -151,7 +161,7 @@ PyObject* gemm8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MAXDNN_TRY
   Call c(a, n, 7, sizeof(maxdnn_gemm8_desc));
   if (!c.ok) return not_plain();
-  const auto& d = c.as<maxdnn_gemm8_desc>();
+  const auto d = c.as<maxdnn_gemm8_desc>();
   auto side = [&](int i, int type, int major, int block, int scale_type, int64_t mn, int64_t ld, void** q, void** s) {
     const int64_t rows = major == MAXDNN_MAJOR_K ? mn : d.K, cols = major == MAXDNN_MAJOR_K ? d.K : mn;
     *q = c.mat(i, type, rows, cols, ld);
@@ -164,7 +174,7 @@ PyObject* gemm8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* out = c.mat(5, d.c_type, d.M, d.N, d.ldc);
   void* stream = c.stream(6);
   if (!c.ok) return not_plain();
-  return PyLong_FromLong(f_gemm8(&d, qa, sa, qb, sb, out, stream));
+  return unlocked([&] { return f_gemm8(&d, qa, sa, qb, sb, out, stream); });
   MAXDNN_CATCH
 }
 
@@ -172,7 +182,7 @@ PyObject* layer_norm_fprop(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MAXDNN_TRY
   Call c(a, n, 12, sizeof(maxdnn_layer_norm_desc));
   if (!c.ok) return not_plain();
-  const auto& d = c.as<maxdnn_layer_norm_desc>();
+  const auto d = c.as<maxdnn_layer_norm_desc>();
   const int64_t r = d.rows, k = d.cols, rs = blocks(k) * r;
   void* x = c.mat(1, d.x_type, r, k, d.ldx);
   void* gamma = c.vec(2, d.w_type, k, true);
@@ -185,7 +195,7 @@ PyObject* layer_norm_fprop(PyObject*, PyObject* const* a, Py_ssize_t n) {
   c.pair(9, d.q_type, r, k, d.ldq, rs, &ck, &sc);
   void* stream = c.stream(11);
   if (!c.ok) return not_plain();
-  return PyLong_FromLong(f_layer_norm_fprop(&d, x, gamma, beta, y, (float*)mean, (float*)rstd, q, s, ck, sc, stream));
+  return unlocked([&] { return f_layer_norm_fprop(&d, x, gamma, beta, y, (float*)mean, (float*)rstd, q, s, ck, sc, stream); });
   MAXDNN_CATCH
 }
 
@@ -193,7 +203,7 @@ PyObject* layer_norm_bprop(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MAXDNN_TRY
   Call c(a, n, 12, sizeof(maxdnn_layer_norm_desc));
   if (!c.ok) return not_plain();
-  const auto& d = c.as<maxdnn_layer_norm_desc>();
+  const auto d = c.as<maxdnn_layer_norm_desc>();
   const int64_t r = d.rows, k = d.cols;
   void* dy = c.mat(1, d.y_type, r, k, d.ldy);
   void* x = c.mat(2, d.x_type, r, k, d.ldx);
@@ -217,8 +227,8 @@ PyObject* layer_norm_bprop(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   void* stream = c.stream(11);
   if (!c.ok) return not_plain();
-  return PyLong_FromLong(f_layer_norm_bprop(&d, dy, x, xs, gamma, (float*)mean, (float*)rstd, dx, (float*)dg, (float*)db,
-                                            ws, ws_bytes, stream));
+  return unlocked([&] { return f_layer_norm_bprop(&d, dy, x, xs, gamma, (float*)mean, (float*)rstd, dx, (float*)dg, (float*)db,
+                                            ws, ws_bytes, stream); });
   MAXDNN_CATCH
 }
 
@@ -226,7 +236,7 @@ PyObject* act8_fprop(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MAXDNN_TRY
   Call c(a, n, 8, sizeof(maxdnn_act8_desc));
   if (!c.ok) return not_plain();
-  const auto& d = c.as<maxdnn_act8_desc>();
+  const auto d = c.as<maxdnn_act8_desc>();
   const int64_t r = d.rows, k = d.cols, many = 1 + d.gated, rs = blocks(k) * r;
   void* h = c.mat(1, d.x_type, r, many * k, d.ldh);
   void* out = c.mat(2, d.x_type, r, k, d.lda, true);
@@ -235,7 +245,7 @@ PyObject* act8_fprop(PyObject*, PyObject* const* a, Py_ssize_t n) {
   c.pair(5, d.q_type, r, many * k, d.ldc, many * rs, &ck, &sc);
   void* stream = c.stream(7);
   if (!c.ok) return not_plain();
-  return PyLong_FromLong(f_act8_fprop(&d, h, out, q, s, ck, sc, stream));
+  return unlocked([&] { return f_act8_fprop(&d, h, out, q, s, ck, sc, stream); });
   MAXDNN_CATCH
 }
 
@@ -243,7 +253,7 @@ PyObject* act8_bprop(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MAXDNN_TRY
   Call c(a, n, 6, sizeof(maxdnn_act8_desc));
   if (!c.ok) return not_plain();
-  const auto& d = c.as<maxdnn_act8_desc>();
+  const auto d = c.as<maxdnn_act8_desc>();
   const int64_t r = d.rows, k = d.cols, many = 1 + d.gated;
   const bool packed = d.h_type >= MAXDNN_E4M3;
   void* da = c.mat(1, d.x_type, r, k, d.lda);
@@ -252,7 +262,7 @@ PyObject* act8_bprop(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* dh = c.mat(4, d.x_type, r, many * k, d.ldh);
   void* stream = c.stream(5);
   if (!c.ok) return not_plain();
-  return PyLong_FromLong(f_act8_bprop(&d, da, h, hs, dh, stream));
+  return unlocked([&] { return f_act8_bprop(&d, da, h, hs, dh, stream); });
   MAXDNN_CATCH
 }
 
