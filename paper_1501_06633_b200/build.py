@@ -8,8 +8,10 @@ from __future__ import annotations
 
 import glob
 import os
+import shutil
 import subprocess
 import sys
+import warnings
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -51,22 +53,47 @@ BINDING = os.path.join(HERE, "_train8.so")
 BINDING_SOURCE = os.path.join(CSRC, "train8_binding.cpp")
 
 
-def build_binding(force: bool = False) -> str:
-    """Compile the marshalling module of the 8-bit training operators (host C++ against the
-    installed torch's headers) if it is missing or older than its sources; return its path."""
+def _binding_marker(torch_version: str) -> bytes:
+    return b"built for torch " + torch_version.encode()
+
+
+def binding_stale(torch_version: str) -> bool:
+    """Whether the marshalling module is missing, older than its sources, or built against another
+    torch (it reads tensors through torch's headers)."""
     deps = (BINDING_SOURCE, os.path.join(HERE, "..", "include", "maxdnn.h"), os.path.abspath(__file__))
-    if not force and os.path.exists(BINDING) and all(os.path.getmtime(p) <= os.path.getmtime(BINDING) for p in deps):
-        return BINDING
+    if not os.path.exists(BINDING) or any(os.path.getmtime(p) > os.path.getmtime(BINDING) for p in deps):
+        return True
+    with open(BINDING, "rb") as f:
+        return _binding_marker(torch_version) + b"\0" not in f.read()
+
+
+def build_binding(force: bool = False):
+    """Compile the marshalling module of the 8-bit training operators (host C++ against the
+    installed torch's headers) if it is stale; return its path.  The operators work without it (their calls
+    then take a few microseconds more): None, with a warning, where a compiler or headers are missing."""
     import sysconfig
 
     import torch
     from torch.utils import cpp_extension
+    if not force and not binding_stale(torch.__version__):
+        return BINDING
+    cxx, python_include = os.environ.get("CXX", "g++"), sysconfig.get_paths()["include"]
+    includes = cpp_extension.include_paths()
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    missing = [] if shutil.which(cxx) else [cxx]
+    for header, dirs in (("Python.h", [python_include]), ("torch/csrc/autograd/python_variable.h", includes),
+                         ("cuda_runtime_api.h", [os.path.join(cuda, "include")])):
+        if not any(os.path.exists(os.path.join(d, header)) for d in dirs):
+            missing.append(header)
+    if missing:
+        warnings.warn("the marshalling module of the 8-bit operators is not built: no " + ", ".join(missing))
+        return None
     tmp = BINDING + ".tmp.%d" % os.getpid()
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
-    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
-    cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-fPIC", "-shared", "-w",
-           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), "-I" + sysconfig.get_paths()["include"],
-           "-I" + os.path.join(cuda, "include")] + ["-I" + p for p in cpp_extension.include_paths()] + \
+    cmd = [cxx, "-std=c++17", "-O2", "-fPIC", "-shared", "-w",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), "-I" + python_include,
+           "-DMAXDNN_BUILT_FOR=\"%s\"" % _binding_marker(torch.__version__).decode(),
+           "-I" + os.path.join(cuda, "include")] + ["-I" + p for p in includes] + \
           ["-o", tmp, BINDING_SOURCE, "-L" + libs, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
@@ -79,4 +106,4 @@ def build_binding(force: bool = False) -> str:
 
 if __name__ == "__main__":
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))
-    print(build_binding(force="--force" in sys.argv))
+    print(build_binding(force="--force" in sys.argv) or "(no marshalling module)")

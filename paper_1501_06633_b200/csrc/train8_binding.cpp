@@ -307,4 +307,13 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train8", nullptr, -1, methods, nu
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__train8() { return PyModule_Create(&module); }
+// The torch whose headers this was compiled with, after a fixed prefix (build.py looks for it).
+PyMODINIT_FUNC PyInit__train8() {
+  static const char built_for[] = MAXDNN_BUILT_FOR;
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "torch_version", built_for + sizeof("built for torch ") - 1) != 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}

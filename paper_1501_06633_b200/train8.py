@@ -5,6 +5,7 @@ views with a row pitch (``stride(0)``) that matches the descriptor.  8-bit value
 from __future__ import annotations
 
 import ctypes
+import warnings
 
 from .binding import OK, MaxdnnError, load_library
 
@@ -110,6 +111,15 @@ class _NoPlain:
 _plain = _NoPlain
 
 
+def _usable(module):
+    """Whether the module was built for this torch, whose tensors it reads by the layout of its headers."""
+    built = getattr(module, "torch_version", "(unknown)")
+    if built != torch.__version__:
+        warnings.warn("_train8 was built for torch %s, this is %s: its calls are marshalled in Python; "
+                      "python -m paper_1501_06633_b200.build renews it" % (built, torch.__version__))
+    return built == torch.__version__
+
+
 def _load_plain(lib):
     """The module that checks and passes on the arguments of plain calls (csrc/train8_binding.cpp)."""
     if not torch.cuda.is_available():
@@ -117,6 +127,8 @@ def _load_plain(lib):
     try:
         from . import _train8
     except ImportError:
+        return _NoPlain
+    if not _usable(_train8):
         return _NoPlain
     _train8.bind(*(ctypes.cast(getattr(lib, "maxdnn_" + n), ctypes.c_void_p).value for n in (
         "quant8", "dequant8", "gemm8", "layer_norm_fprop", "layer_norm_bprop", "act8_fprop", "act8_bprop")))
