@@ -118,3 +118,18 @@ def test_no_two_clusters_fit_an_sm_with_more_than_its_tensor_memory(planners):
             if sum(group) > COLUMNS:
                 assert sum(least[c] + CTA_BYTES for c in group) > SM_BYTES, (group, least)
     assert max(s for _, s in found) <= 227 * 1024
+
+
+def test_which_products_store_by_bulk_copies(planners):
+    """Whole 16 bytes at both ends of every row, tiles of 32 columns or more, neither split nor exchanged roles."""
+    so = planners
+    for ct, bytes_ in ((mx.DTYPE_F32, 4), (mx.DTYPE_BF16, 2), (mx.DTYPE_F16, 2)):
+        for n, ldc in ((328, 328), (328, 344), (330, 336), (331, 344), (328, 330)):
+            for pair, cols in ((-1, 32), (-1, 64), (-1, 128), (1, 128), (1, 192), (1, 224), (1, 256)):
+                so.reset_opts()
+                for name, v in ((b"GEMM8_PAIR", pair), (b"GEMM8_COLS", cols), (b"GEMM8_SPLIT", 1), (b"GEMM8_SWAP", 0)):
+                    so.set_opt(name, v)
+                p = gemm8_plan(so, 150, n, 300, c_type=ct, ldc=ldc)
+                whole = n * bytes_ % 16 == 0 and ldc * bytes_ % 16 == 0
+                assert (p["tile_n"], p["pair"]) == (cols, int(pair > 0)) and bool(p["bulk_c"]) == whole and p["staged_c"]
+    so.reset_opts()
