@@ -203,10 +203,10 @@ def _on_device(t, what):
         raise ValueError("%s is not on the current device" % what)
 
 
-def _vec(t, dtypes, n, what):
+def _vec(t, dtype, n, what):
     """Address of a contiguous tensor of n elements."""
     _on_device(t, what)
-    if t.dtype not in dtypes:
+    if not 0 <= dtype < len(_TYPES) or t.dtype not in _TYPES[dtype]:
         raise TypeError("%s has dtype %s, which is not what the descriptor says" % (what, t.dtype))
     if t.numel() != n or not t.is_contiguous():
         raise ValueError("%s has shape %s, expected %d contiguous elements" % (what, tuple(t.shape), n))
@@ -222,7 +222,7 @@ def _n_scales(block, rows, cols):
 
 
 def _scales(t, n, what):
-    return _vec(t, _TYPES[DTYPE_E8M0], n, what)
+    return _vec(t, DTYPE_E8M0, n, what)
 
 
 def _stream(stream):
@@ -286,7 +286,7 @@ def _operand(t, s, dtype, major, block, scale_type, mn, k, ld, what):
     rows, cols = (mn, k) if major == MAJOR_K else (k, mn)
     p = _mat(t, dtype, rows, cols, ld, what)
     n = _n_scales(block, rows, cols) if 0 <= block <= 2 else -1
-    return p, _vec(s, _TYPES[scale_type], n, "scales of " + what)
+    return p, _vec(s, scale_type, n, "scales of " + what)
 
 
 def gemm8(desc: Gemm8Desc, a, a_scale, b, b_scale, c, stream=None) -> None:
@@ -313,7 +313,7 @@ def layer_norm_fprop(desc: LayerNormDesc, x, gamma=None, beta=None, y=None, mean
     if status >= 0:
         return _raise(status, "maxdnn_layer_norm_fprop")
     r, c = desc.rows, desc.cols
-    f32, w, n = _TYPES[DTYPE_F32], _TYPES[desc.w_type], _n_scales(BLOCK_ROW, r, c)
+    f32, w, n = DTYPE_F32, desc.w_type, _n_scales(BLOCK_ROW, r, c)
     q, s = _pair(packed, desc.q_type, r, c, desc.ldq, n, "packed")
     k, sk = _pair(checkpoint, desc.q_type, r, c, desc.ldq, n, "checkpoint")
     _raise(lib.maxdnn_layer_norm_fprop(
@@ -339,7 +339,7 @@ def layer_norm_bprop(desc: LayerNormDesc, dy, x, gamma, mean, rstd, dx, dgamma=N
                            None if stream is None else stream.cuda_stream)
     if status >= 0:
         return _raise(status, "maxdnn_layer_norm_bprop")
-    r, c, f32 = desc.rows, desc.cols, _TYPES[DTYPE_F32]
+    r, c, f32 = desc.rows, desc.cols, DTYPE_F32
     if workspace is not None:
         _on_device(workspace, "workspace")
         if not workspace.is_contiguous():
@@ -347,7 +347,7 @@ def layer_norm_bprop(desc: LayerNormDesc, dy, x, gamma, mean, rstd, dx, dgamma=N
     _raise(lib.maxdnn_layer_norm_bprop(
         ctypes.byref(desc), _mat(dy, desc.y_type, r, c, desc.ldy, "dy"), _mat(x, desc.x_type, r, c, desc.ldx, "x"),
         None if desc.x_type < DTYPE_E4M3 else _scales(x_scale, _n_scales(BLOCK_ROW, r, c), "x_scale"),
-        None if gamma is None else _vec(gamma, _TYPES[desc.w_type], c, "gamma"), _vec(mean, f32, r, "mean"), _vec(rstd, f32, r, "rstd"),
+        None if gamma is None else _vec(gamma, desc.w_type, c, "gamma"), _vec(mean, f32, r, "mean"), _vec(rstd, f32, r, "rstd"),
         _mat(dx, desc.y_type, r, c, desc.ldy, "dx"), None if dgamma is None else _vec(dgamma, f32, c, "dgamma"),
         None if dbeta is None else _vec(dbeta, f32, c, "dbeta"), None if workspace is None else workspace.data_ptr(),
         0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)),
