@@ -41,3 +41,22 @@ def test_other_threads_run_during_a_call():
     assert got == {n: 0 for n in CALLS}          # (1: held, -1: the call was not plain)
     mx.quant8(calls["quant8"][0], x, row=(q, s))
     assert bool((s == 127).all())
+
+
+def test_both_ways_of_marshalling_make_the_same_calls(monkeypatch):
+    """The example's forward and backward pass with the module, and with every call checked in Python."""
+    import importlib.util
+    import os
+    at = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "feed_forward8.py")
+    spec = importlib.util.spec_from_file_location("feed_forward8", at)
+    ff = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ff)
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    x, dout = (torch.randn(70, 200, device="cuda", generator=gen).to(torch.bfloat16) for _ in range(2))
+    got = []
+    for plain in (train8._library() and train8._plain, train8._NoPlain):
+        monkeypatch.setattr(train8, "_plain", plain)
+        block, before = ff.FeedForward8(200, 150, seed=1), mx.launch_count()
+        got.append([block.forward(x), block.backward(dout), mx.launch_count() - before])
+    (out, grads, n), (out2, grads2, n2) = got
+    assert n == n2 and torch.equal(out, out2) and all(torch.equal(grads[k], grads2[k]) for k in grads)
