@@ -33,6 +33,23 @@ __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontr
 // kernel's life, which begins before that wait.
 template <class T>
 __device__ __forceinline__ T load_global(const T* p) { return *p; }
+// The same loads (16 or 8 bytes), which stay behind that wait but which the compiler may move across this
+// kernel's own stores: inputs and outputs do not overlap.
+__device__ __forceinline__ uint4 load_global_free(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint2 load_global_free(const uint2* p) {
+  uint2 v;
+  asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+  return v;
+}
+template <bool FREE, class T>
+__device__ __forceinline__ T load_as(const T* p) {
+  if constexpr (FREE) return load_global_free(p);
+  else return load_global(p);
+}
 
 template <int DT> struct ElemOf;
 template <> struct ElemOf<MAXDNN_F32> { typedef float T; };
@@ -250,22 +267,22 @@ __device__ __forceinline__ uint4 first_bytes(uint4 v, int n) {
 // turn (a layer norm with 16 loads a lane took 9.7 us a row that way).
 // EDGE = true: the aligned 16 (8-bit types: 8) bytes that hold the first and the last value are
 // loaded and shifted; no load touches an aligned unit that holds none of the n values.
-template <int DT, bool EDGE>
+template <int DT, bool EDGE, bool FREE = false>
 __device__ __forceinline__ Raw8<DT> load_raw8(const typename ElemOf<DT>::T* p, int n) {
   Raw8<DT> r;
   if constexpr (!EDGE) {
     if constexpr (DT == MAXDNN_F32) {
       r.a = r.b = make_uint4(0, 0, 0, 0);
       if (n) {
-        r.a = load_global(reinterpret_cast<const uint4*>(p));
-        r.b = load_global(reinterpret_cast<const uint4*>(p) + 1);
+        r.a = load_as<FREE>(reinterpret_cast<const uint4*>(p));
+        r.b = load_as<FREE>(reinterpret_cast<const uint4*>(p) + 1);
       }
     } else if constexpr (is_fp8(DT)) {
       r.a = make_uint2(0, 0);
-      if (n) r.a = load_global(reinterpret_cast<const uint2*>(p));
+      if (n) r.a = load_as<FREE>(reinterpret_cast<const uint2*>(p));
     } else {
       r.a = make_uint4(0, 0, 0, 0);
-      if (n) r.a = load_global(reinterpret_cast<const uint4*>(p));
+      if (n) r.a = load_as<FREE>(reinterpret_cast<const uint4*>(p));
     }
   } else {
     const uintptr_t at = reinterpret_cast<uintptr_t>(p);
@@ -274,20 +291,20 @@ __device__ __forceinline__ Raw8<DT> load_raw8(const typename ElemOf<DT>::T* p, i
       const uint32_t s = (uint32_t)(at & 7u);
       const uint2* q = reinterpret_cast<const uint2*>(at - s);
       uint2 lo = make_uint2(0, 0), hi = make_uint2(0, 0);
-      if (bytes > 0) lo = load_global(q);
-      if ((int)s + bytes > 8) hi = load_global(q + 1);
+      if (bytes > 0) lo = load_as<FREE>(q);
+      if ((int)s + bytes > 8) hi = load_as<FREE>(q + 1);
       const uint4 v = words_at(make_uint4(lo.x, lo.y, hi.x, hi.y), make_uint4(0, 0, 0, 0), s);
       r.a = make_uint2(first_bytes(v.x, bytes), first_bytes(v.y, bytes - 4));
     } else {
       const uint32_t s = (uint32_t)(at & 15u);
       const uint4* q = reinterpret_cast<const uint4*>(at - s);
       uint4 c0 = make_uint4(0, 0, 0, 0), c1 = c0;
-      if (bytes > 0) c0 = load_global(q);
-      if ((int)s + bytes > 16) c1 = load_global(q + 1);
+      if (bytes > 0) c0 = load_as<FREE>(q);
+      if ((int)s + bytes > 16) c1 = load_as<FREE>(q + 1);
       r.a = first_bytes(words_at(c0, c1, s), bytes);
       if constexpr (DT == MAXDNN_F32) {
         uint4 c2 = make_uint4(0, 0, 0, 0);
-        if ((int)s + bytes > 32) c2 = load_global(q + 2);
+        if ((int)s + bytes > 32) c2 = load_as<FREE>(q + 2);
         r.b = first_bytes(words_at(c1, c2, s), bytes - 16);
       }
     }

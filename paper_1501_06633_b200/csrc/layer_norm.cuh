@@ -91,17 +91,17 @@ __device__ __forceinline__ void norm_pack(const F2 (&v)[4], const F2 (&w)[4], bo
 }
 
 // Eight neighbouring weights.
-template <bool EDGE>
+template <bool EDGE, bool FREE = false>
 __device__ __forceinline__ void load_weights8(const void* p, int c, int n, int type, float none, F2 (&w)[4]) {
   if (!p || n == 0) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = f2(none);
   } else if (type == MAXDNN_F32) {
-    to_pairs<MAXDNN_F32>(load_raw8<MAXDNN_F32, EDGE>(static_cast<const float*>(p) + c, n), w);
+    to_pairs<MAXDNN_F32>(load_raw8<MAXDNN_F32, EDGE, FREE>(static_cast<const float*>(p) + c, n), w);
   } else if (type == MAXDNN_BF16) {
-    to_pairs<MAXDNN_BF16>(load_raw8<MAXDNN_BF16, EDGE>(static_cast<const __nv_bfloat16*>(p) + c, n), w);
+    to_pairs<MAXDNN_BF16>(load_raw8<MAXDNN_BF16, EDGE, FREE>(static_cast<const __nv_bfloat16*>(p) + c, n), w);
   } else {
-    to_pairs<MAXDNN_F16>(load_raw8<MAXDNN_F16, EDGE>(static_cast<const __half*>(p) + c, n), w);
+    to_pairs<MAXDNN_F16>(load_raw8<MAXDNN_F16, EDGE, FREE>(static_cast<const __half*>(p) + c, n), w);
   }
 }
 
@@ -265,8 +265,8 @@ layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
             b[e] = bb.x; b[e + 1] = bb.y;
           }
         } else {
-          load_weights8<EDGE>(args.gamma, c, n[i], args.w_type, 1.f, g);
-          load_weights8<EDGE>(args.beta, c, n[i], args.w_type, 0.f, b);
+          load_weights8<EDGE, true>(args.gamma, c, n[i], args.w_type, 1.f, g);
+          load_weights8<EDGE, true>(args.beta, c, n[i], args.w_type, 0.f, b);
         }
         normalise8<EDGE>(v[i], minus_mean, f2(rstd), g, b, n[i]);
         if (args.y) store_pairs<XT, EDGE>(yp + kStep * (j + i), v[i], n[i]);
@@ -647,8 +647,8 @@ __global__ void __launch_bounds__(1024) layer_norm_fprop_long_kernel(const __gri
             norm_pack<kEitherFp8, true>(v, none, args.q_e5m2, args.c + r * args.ldq + c, nullptr,
                                         args.sc + (int64_t)(c >> 7) * args.rows + r, nullptr, n, 0, lane);
           F2 g[4], b[4];
-          load_weights8<true>(args.gamma, c, n, args.w_type, 1.f, g);
-          load_weights8<true>(args.beta, c, n, args.w_type, 0.f, b);
+          load_weights8<true, true>(args.gamma, c, n, args.w_type, 1.f, g);
+          load_weights8<true, true>(args.beta, c, n, args.w_type, 0.f, b);
           normalise8<true>(v, f2(-mean), f2(rstd), g, b, n);
           if (args.y) store_pairs<XT, true>(y + r * args.ldy + c, v, n);
           if (args.q)

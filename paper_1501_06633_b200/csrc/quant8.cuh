@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(kQuantThreads, XT == MAXDNN_F32 ? 2 : 3) quant
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const int r = r0 + rg + 16 * k;
-    raw[k] = load_raw8<XT, EDGE>(x + (int64_t)r * args.ldx + c0, r < args.rows ? n : 0);
+    raw[k] = load_raw8<XT, EDGE, true>(x + (int64_t)r * args.ldx + c0, r < args.rows ? n : 0);
     if constexpr (is_fp8(XT))
       xs[k] = r < args.rows ? e8m0_value(args.x_scale[(int64_t)cb * args.rows + r]) : 0.f;
   }
