@@ -10,9 +10,10 @@
 // A CTA takes 128 columns x 64 rows: 16 lanes cover a row block, thread t has eight columns of
 // the rows t/16 + 16 k, so 4 (plain) or 8 (gated) loads of 16 bytes are in flight per thread.
 //
-// Measured: forward SiLU, gated, 8192 x 4096 bf16 with a and h packed 46 us, 236 MB at 5.1 TB/s (copy: 6.5),
-// bound by instruction issue (38 M warp instructions, three packings of 8 values each; 50 us with
-// three CTAs of an SM instead of four); backward GELU from packed h, 4097 x 2736, 22 us, 90 MB at 4.0 TB/s.
+// Measured: forward SiLU, gated, 8192 x 4096 bf16 with a and h packed 47 to 50 us (on different boards), 236 MB at
+// 4.7 to 5.0 TB/s (copy: 6.5): 40 M warp instructions at 0.78 a cycle (three packings of 8 values each; three CTAs
+// of an SM instead of four were 4 us slower, at the price of 16 bytes a thread spilled);
+// backward GELU from packed h, 4097 x 2736, 23.3 us, 90 MB at 3.9 TB/s.
 #pragma once
 #include "fp8_util.cuh"
 

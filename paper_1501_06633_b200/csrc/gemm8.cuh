@@ -19,7 +19,7 @@
 // shared memory and takes a part of the tile, adding the CTAs' totals in CTA order.
 //
 // This kernel serves scales that are fp32 numbers; E8M0 scales go to gemm8_mx.cuh.  Measured: 2048 x
-// 4096 x 4096 46 us (1.5 PFLOP/s), bound by reading the products back from tensor memory and the
+// 4096 x 4096 45 us (1.5 PFLOP/s), bound by reading the products back from tensor memory and the
 // multiply-adds; 16 x 4096 x 4096 7.4 us.
 // Every wait on a barrier in shared memory is bounded and ends in a status code; TMEM is always freed.
 // The waits without a limit are those for tensor memory and, at a cluster's end, for its CTAs: the

@@ -8,12 +8,12 @@
 // chunk of it.  The tensor core truncates its fp32 accumulator at every MMA (towards zero), so terms of
 // one sign lose about half a unit of the running sum each time, and the loss grows with the length.
 // Chunks are added in registers with round-to-nearest.  An fp32 result takes chunks of sixteen
-// blocks (64 MMAs).  Measured on a weight gradient over 16384 tokens (error against 64 bits, relative,
-// and time at 8192 x 4096 in short runs at a high clock; 543 to 555 us back to back): chunks of
-// 4 blocks 1.1e-7, 674 us; 8: 1.6e-7, 512 us; 16: 3.0e-7, 462 us; none 1.5e-6, 460 us (fp32
-// arithmetic throughout: 3.6e-7).  A 16-bit result takes chunks of 128 blocks (512 MMAs): at most 6.2e-5
-// of it for terms of one sign, against 2.4e-4 for the rounding to fp16; with one accumulator for 2^18
-// terms of one sign its bf16 values were off, for 2^20 its fp16 values.
+// blocks (64 MMAs).  Measured on a weight gradient over 16384 tokens, 8192 x 4096 (error against 64 bits, relative;
+// time of a short run at a high clock / back to back): chunks of 4 blocks 1.1e-7, 674 us; 8: 1.6e-7, 512; 16:
+// 3.0e-7, 462 / 540; 32: 428 / 498; one accumulator 1.5e-6, 396 / 460 (fp32 arithmetic throughout: 3.6e-7).
+// A 16-bit result takes chunks of 128 blocks (512 MMAs): at most 6.2e-5 of it for terms of one sign, against 2.4e-4
+// for the rounding to fp16; with one accumulator for 2^18 terms of one sign its bf16 values were off, for 2^20
+// its fp16 values.
 //
 // Roles.  Warp 0 copies A, warp 3 copies B, warp 1 issues the MMAs, warp 2 gathers the scales:
 // the bytes of four blocks and 128 rows, which lie [block][row] in memory, become 32 rows of 16
@@ -28,14 +28,15 @@
 // of all columns.  Both CTAs' copies report to the leader's barriers; its commits reach both.
 //
 // Accumulators.  Two where tensor memory holds them next to the scales (NT <= 224), so that one
-// is read while the other fills; NT = 256 has one.
+// is read while the other fills; NT = 256 has one, and the MMAs wait while it is read: the tensor pipe is busy in
+// 82 % of that weight gradient's cycles with a 16-bit C, 61 % with an fp32 C (either major).
 //
 // Few tiles (not PAIR): a cluster of 2, 4 or 8 CTAs shares a tile's reduction, as in gemm8.cuh.
 //
-// Measured: 8192 x 8192 x 8192 to bf16 390 us = 2.8 PFLOP/s (MMAs in 88 % of the cycles; the power limit
-// holds the clock at 1.3 to 1.4 GHz, so that with the copies left out it would be 3.4), 2048 x 4096 x 4096 31 us,
-// one token through 4096 x 4096 7.6 us (16.8 MB: 2.2 TB/s; the start of a call, a memory latency and the
-// exchange between the CTAs are 5 of them).
+// Measured: 8192 x 8192 x 8192 to bf16 390 to 396 us in short runs = 2.8 PFLOP/s (MMAs in 88 % of the cycles; the
+// power limit holds the clock at 1.2 to 1.4 GHz, so that with the copies left out it would be 3.4), 2048 x 4096 x 4096
+// 31 us in short runs, 36 back to back, one token through 4096 x 4096 7.4 us (16.8 MB: 2.3 TB/s; the start of a call, a
+// memory latency and the exchange between the CTAs are 5 of them).
 #pragma once
 #include "gemm8.cuh"
 

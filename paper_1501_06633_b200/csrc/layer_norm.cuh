@@ -12,9 +12,10 @@
 // in 32 bits.  Sixteen neighbouring lanes hold a block of 128 columns, so the packed forms take
 // four shuffles for two blocks.
 //
-// Measured at 8192 x 4096 bf16 (copy: 6.5 TB/s): statistics alone 15 us (4.5 TB/s), y 27.5 us (4.9), y and x packed
-// 40 us (3.4: two packings, 28 M warp instructions), backward from packed x 41.6 us with the sums over
-// rows (4.0).  Tried when the packed forward pass took 45 us, and slower: two rows at a time to share
+// Measured at 8192 x 4096 bf16 (copy: 6.5 TB/s): statistics alone 15 us (4.5 TB/s), y 27.7 us (4.9), y and x packed
+// 40 us (3.4: two packings, 27 M warp instructions at 0.64 a cycle: one row after the other, no load of the next
+// under way), backward from packed x 43.6 us with the sums over rows (3.9).  Widths that are no multiple of 8 take 3
+// to 4 times that (4095 columns: 96, 117 and 140 us).  Tried when the packed forward pass took 45 us, and slower: two rows at a time to share
 // the weights (50 us: half the warps), the next row prefetched in registers (51 us) or in a ring in shared
 // memory (72 us, the weights then fall out of the first-level cache), 48 registers and five CTAs (50 us).
 #pragma once
@@ -161,7 +162,7 @@ layer_norm_fprop_kernel(const __grid_constant__ LayerNormArgs args) {
   // The weights as fp32 in shared memory, for every row of the CTA: whatever their type, and where
   // there are none (up to 4096 columns, 32 KB; 16384 x 1024 with packed results: 25.8 us with the
   // weights from the first-level cache, 19.9 from here.  With 64 KB for 8192 columns fewer CTAs fit an SM:
-  // 92 us became 125).
+  // 92 us became 125; now 100 without).
   constexpr bool kShared = norm_shared_weights(J, WR) && !EDGE;
   extern __shared__ __align__(16) float weights[];
   const int padded = 256 * WR * J;

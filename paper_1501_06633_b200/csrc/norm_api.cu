@@ -39,8 +39,8 @@ maxdnn_status check_layer_norm(const maxdnn_layer_norm_desc* d) {
 
 // CTAs of the backward pass: each leaves one row of sums, which the fold reads again.  Where the CTAs
 // of a whole device would have fewer than four rows each there are fewer of them, down to one per
-// SM (packed bf16: 1024 x 4096 13.3 us with 256 CTAs, 14.7 with 296; 512 x 4096 9.7 with 148, 11.5 with
-// 296; 300 x 2048 8.9 against 8.4.  Fewer than the SMs lose: 128 x 4096 8.7 with 64, 7.5 with 128).
+// SM (packed bf16: 1024 x 4096 13.8 us with 256 CTAs, 1.4 more with 296; 512 x 4096 9.7 with 148, 1.8 more with
+// 296; 300 x 2048 9.1, 0.5 less with all.  Fewer than the SMs lose: 128 x 4096 8.7 with 64, 7.5 with 128).
 int norm_bprop_grid(const maxdnn_layer_norm_desc& d, int sm_count, const NormShape& s) {
   const int64_t units = s.threads == 32 ? ((int64_t)d.rows + 3) / 4 : d.rows;
   const int per_sm = s.threads == 0 ? 1 : s.threads == 32 ? 4 : s.ring ? 512 / s.threads : s.threads >= 512 ? 1 : 512 / s.threads;
@@ -66,8 +66,8 @@ maxdnn_status launch_norm_rows(const LayerNormArgs& a, int sm_count, cudaStream_
                       grid, kNormThreads, smem, 1, stream, a);
 }
 
-// Vectors of eight columns per thread (J) and warps per row (WR).  Few rows (fewer than the SMs
-// hold warps): eight warps share a row, for the latency (three rows of 2048: 2.1 us against 2.5
+// Vectors of eight columns per thread (J) and warps per row (WR).  Few rows (fewer than four for each
+// SM): eight warps share a row, for the latency (three rows of 2048: 2.1 us against 2.5
 // with a warp each).  Else as few warps as hold the row with J <= 4.  Rows beyond 16384 columns are read again
 // for each sum.
 template <int XT>
