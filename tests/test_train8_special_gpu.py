@@ -198,3 +198,22 @@ def test_activation_of_values_that_are_not_finite(cols, kind, act, gated):
     both = np.concatenate([touched] * many, 1)
     same(dh[~both], dh0[~both])
     assert np.isnan(dh[4, 100]) and np.isnan(dh[6, cols - 1]) and not np.isfinite(dh8[both]).all()
+
+
+@pytest.mark.parametrize("to", ["e4m3", "e5m2"])
+def test_repacking_values_that_are_not_finite(to):
+    """Infinities and NaN of packed E5M2 values, and a scale byte 255, in every form of the new packing."""
+    rows, cols = 140, 300
+    rng = np.random.default_rng(4)
+    q, s = ref.pack(data(rng, rows, cols), "row", "e5m2")
+    q[3, 5], q[3, 200], q[131, 7], q[9, 290] = INF, -INF, NAN, INF
+    s[0, 20] = 255
+    x = q * ref.spread(ref.value_of(s), "row", rows, cols)
+    t, ts = packed_up(q, s, "e5m2")
+    d = mx.Quant8Desc.make(rows, cols, x_type=mx.DTYPE_E5M2, q_type=PACKED[to][0], ldx=t.stride(0))
+    out = {f: (mx.empty_packed(rows, cols, PACKED[to][0]), mx.empty_scales(FORM[f], rows, cols)) for f in FORM}
+    mx.quant8(d, t, x_scale=ts, **out)
+    for f in FORM:
+        want, ws = ref.pack(x, f, to)
+        same(down(out[f][0]), want)
+        np.testing.assert_array_equal(bytes_of(out[f][1]), ws)
