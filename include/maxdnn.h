@@ -580,6 +580,102 @@ maxdnn_status maxdnn_act8_fprop(const maxdnn_act8_desc* desc, const void* h, voi
 maxdnn_status maxdnn_act8_bprop(const maxdnn_act8_desc* desc, const void* da, const void* h,
                                 const void* h_scale, void* dh, void* cuda_stream);
 
+/*
+ * Root-mean-square norm over the columns, with the residual's addition:
+ *
+ *   h = x + residual,  rstd = 1 / sqrt(sum h^2 / cols + eps),  y = h rstd gamma
+ *
+ * h is held in 32 bits: y, rstd and the packed forms come from it before it is rounded.  residual may be null (h = x).
+ * gamma: [cols] in w_type, null for 1.  Forward, any of the results may be null: sum (h rounded to x_type,
+ * the residual of the next addition), y (y_type = x_type), rstd (fp32 [rows], what the backward pass reads),
+ * (q, s): y packed in row blocks, the next product's operand, and (c, sc): h packed in row blocks, which the
+ * backward pass takes in place of h (both q_type, pitch ldq).  sum may be the residual's own memory or x's (same pitch);
+ * no other result may overlap an input.  NOT_SUPPORTED: x_type other than y_type (forward; backward unless h is packed),
+ * more than 2^30 columns, ldq no multiple of 16.
+ */
+typedef struct maxdnn_rms_norm_desc {
+  int32_t rows, cols;
+  int64_t ldx, ldr, ldy, ldq; /* pitch of x (backward: h); of residual, sum and dsum; of y, dy and dx; of q and c */
+  int32_t x_type, y_type, w_type, q_type;
+  float eps;
+} maxdnn_rms_norm_desc;
+
+maxdnn_status maxdnn_rms_norm_fprop(const maxdnn_rms_norm_desc* desc, const void* x, const void* residual,
+                                    const void* gamma, void* sum, void* y, float* rstd, void* q, void* s,
+                                    void* c, void* sc, void* cuda_stream);
+/* dx (y_type) and dgamma (fp32 [cols], null: not wanted), with hh = h rstd and g = gamma dy:
+ *   dx = rstd (g - hh mean(g hh)) + dsum,  dgamma = sum over rows of dy hh
+ * dx is the gradient of x and of the residual.  dsum (y_type, may be null): the gradient that reaches `sum` from where
+ * it was added next.  h: wide (x_type = y_type), or packed in row blocks (x_type E4M3 / E5M2, h_scale).
+ * dx may be dsum's own memory or dy's (same pitch).  The sums over rows go through the workspace and are added in a
+ * fixed order. */
+maxdnn_status maxdnn_rms_norm_bprop_workspace(const maxdnn_rms_norm_desc* desc, size_t* bytes);
+maxdnn_status maxdnn_rms_norm_bprop(const maxdnn_rms_norm_desc* desc, const void* dy, const void* h,
+                                    const void* h_scale, const void* gamma, const float* rstd,
+                                    const void* dsum, void* dx, float* dgamma, void* workspace,
+                                    size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Log probabilities of given tokens from logits x [rows][cols] (x_type, pitch ldx), in 32 bits:
+ *
+ *   z = scale x,  lse = log sum exp z,  logprob = z[target] - lse,  entropy = -sum p log p,  p = exp(z - lse)
+ *
+ * target: [rows] of int32 or int64 (target_type); a number outside [0, cols) stands for no token: its logprob is 0
+ * and it has no gradient.  Null: logprob is not wanted.  lse, entropy: fp32 [rows], may be null.  top (0 to 32): the
+ * `top` largest x of each row in falling order, equal ones by rising index, as top_logprob (fp32) and top_index (int32),
+ * both [rows][top]; a place for which no logit above -inf is left holds -inf and index -1.  A NaN counts as
+ * larger than every number.  A row without any logit above -inf (all masked) has lse = -inf, logprob = -inf
+ * (0 without a token), entropy = 0 and a gradient of zeros.  A row with a NaN or +inf has lse, logprob, entropy and
+ * top_logprob NaN.  scale: positive and finite.  NOT_SUPPORTED: top above 32, more than 2^30 columns.
+ */
+typedef enum maxdnn_index { MAXDNN_INDEX_I32 = 0, MAXDNN_INDEX_I64 = 1 } maxdnn_index;
+
+typedef struct maxdnn_logprob_desc {
+  int32_t rows, cols;
+  int64_t ldx, ldd, ldq;            /* pitch of x; of dx; of packed gradients */
+  int32_t x_type, q_type, target_type, top;
+  float scale;
+} maxdnn_logprob_desc;
+
+maxdnn_status maxdnn_logprob_fprop(const maxdnn_logprob_desc* desc, const void* x, const void* target,
+                                   float* logprob, float* lse, float* entropy, float* top_logprob,
+                                   int32_t* top_index, void* cuda_stream);
+/* The gradient of sum(dlogprob logprob) + sum(dentropy entropy), from x and what the forward pass gave:
+ *   dx_j = scale (dlogprob ([j = target] - p_j) - dentropy p_j (log p_j + entropy))
+ * dlogprob (with target) or dentropy (with entropy), fp32 [rows], may be null.  Results, any of them: dx (x_type, pitch
+ * ldd; may be x's own memory where ldd = ldx and nothing is packed in the same call), (q_row, s_row) and (q_col, s_col): dx
+ * packed in row and column blocks (q_type, pitch ldq) from its 32-bit value, the operands of the two products behind it. */
+maxdnn_status maxdnn_logprob_bprop(const maxdnn_logprob_desc* desc, const void* x, const void* target,
+                                   const float* lse, const float* dlogprob, const float* entropy,
+                                   const float* dentropy, void* dx, void* q_row, void* s_row, void* q_col,
+                                   void* s_col, void* cuda_stream);
+
+/*
+ * Orthogonalised update of weights by Newton-Schulz products, for each of `batch` matrices G [rows][cols]:
+ *
+ *   X = G / (|G| + eps)  (|G|: root of the sum of squares)
+ *   steps times:  A = X X^T,  X = a X + (b A + c A A) X     (X^T X and products from the right where rows > cols)
+ *   out = X
+ *
+ * x: x_type F32, BF16 or F16, pitch ldx, matrices stride_x apart; out: BF16, pitch ldo, stride_o.  coefficients: HOST
+ * memory, [steps][3] numbers a, b, c (read during the call); null: 3.4445, -4.7750, 2.0315 for every step.  The products
+ * run on the tensor cores on operands rounded to FP16 with 32-bit sums; X itself is kept in 22 bits, the diagonals of A and
+ * of the polynomial in 32, so that the result is about 1e-3 (of its norm) from the formula's, whatever the spectrum: less
+ * than its rounding to BF16.  A matrix of zeros gives zeros, one with a NaN or infinity gives NaN.  The coefficients
+ * have to keep every singular value of X below 100 (the default ones: below 1.3).  workspace: 16-byte
+ * aligned, its contents do not matter.  NOT_SUPPORTED: rows or cols above 65536, steps above 32.
+ */
+typedef struct maxdnn_ortho_desc {
+  int32_t batch, rows, cols, steps;
+  int64_t ldx, ldo, stride_x, stride_o;
+  int32_t x_type;
+  float eps;
+} maxdnn_ortho_desc;
+
+maxdnn_status maxdnn_orthogonalise_workspace(const maxdnn_ortho_desc* desc, size_t* bytes);
+maxdnn_status maxdnn_orthogonalise(const maxdnn_ortho_desc* desc, const void* x, const float* coefficients,
+                                   void* out, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* Synchronises `cuda_stream`, then reads and clears the current device's
  * status word.  MAXDNN_OK, MAXDNN_DEVICE_TIMEOUT (a bounded wait inside some
  * kernel launched since the last query ran out; that kernel's output is not

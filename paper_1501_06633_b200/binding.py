@@ -52,6 +52,8 @@ EXPORTED_SYMBOLS = [
     "maxdnn_quant8", "maxdnn_dequant8", "maxdnn_gemm8", "maxdnn_layer_norm_fprop",
     "maxdnn_layer_norm_bprop_workspace", "maxdnn_layer_norm_bprop", "maxdnn_act8_fprop",
     "maxdnn_act8_bprop",
+    "maxdnn_rms_norm_fprop", "maxdnn_rms_norm_bprop_workspace", "maxdnn_rms_norm_bprop",
+    "maxdnn_logprob_fprop", "maxdnn_logprob_bprop",
 ]
 
 

@@ -591,7 +591,7 @@ layer_norm_bprop_ring_kernel(const __grid_constant__ LayerNormArgs args, int dep
 
 // dg and db from the CTAs' sums, in CTA order.  A CTA takes 32 of the 2 x pitch columns; each of its
 // 16 warps takes every sixteenth sum, four at a time, and the warps' results are added in warp order.
-__global__ void __launch_bounds__(512) layer_norm_fold_kernel(const float* partial, int parts, int cols,
+static __global__ void __launch_bounds__(512) layer_norm_fold_kernel(const float* partial, int parts, int cols,
                                                               float* dgamma, float* dbeta) {
   let_next_start();
   wait_for_previous();

@@ -1,0 +1,505 @@
+// Root-mean-square norm over the last axis with the residual's addition, forward and backward, with the
+// packed forms that the 8-bit training step reads next.
+//
+//   h = x + residual,  rstd = 1 / sqrt(sum h^2 / C + eps),  hh = h rstd,  y = hh g
+//   dx = rstd (g dy - hh s) + dsum,  s = sum(g dy hh) / C,  dg = sum over rows of dy hh
+//
+// A group of WR warps has a row: thread t holds the eight columns at 8 t and the eight at 8 (t + 32 WR), as
+// 32-bit values, and the weights of the same columns for all of the group's rows.  Rows come through a ring in
+// shared memory: one thread of the group fetches the row `depth` ahead with a bulk copy per input, whatever the
+// row's alignment (the copy starts at the 16 bytes that hold the row's first value), so a row's loads cost no
+// registers and no issue slots while the row before is packed.  The exchange of the row's one sum is also what
+// tells that a stage has been read.  Few rows are read directly: a ring would only add its start.
+// Sums are in 32 bits; sixteen neighbouring lanes hold a block of 128 columns, so packing takes four shuffles
+// for two blocks.
+#pragma once
+#include "layer_norm.cuh"
+
+namespace maxdnn {
+
+struct RmsNormArgs {
+  const void *x, *res;         // fprop: x and residual; bprop: h (wide or packed) and dsum
+  const uint8_t* x_scale;
+  const void* gamma;           // null: 1
+  void *sum, *y;               // fprop
+  float* rstd;
+  uint8_t *q, *s, *c, *sc;     // fprop: packed y, packed h
+  const void* dy;              // bprop
+  void* dx;
+  float* partial;              // [grid][norm_sums_pitch(cols)] sums of a CTA's rows: dy hh
+  int64_t ldx, ldr, ldy, ldq;
+  int32_t rows, cols, w_type;
+  int32_t q_e5m2;
+  int32_t depth;               // stages of the ring
+  float eps, inv_cols;
+  WaitCtx wc;
+};
+
+constexpr int kRmsMaxDepth = 4;
+constexpr int kRmsRegCols = 16384;       // the longest row that a group's registers hold
+__host__ __device__ constexpr int rms_threads(int wr) { return wr > 8 ? 32 * wr : 256; }
+__host__ __device__ constexpr int rms_groups(int wr) { return wr > 8 ? 1 : 8 / wr; }
+// Bytes of a row in a stage: the 16-byte units that hold it, wherever its first value lies in one.
+__host__ __device__ constexpr int64_t rms_stage_row(int64_t cols, int bytes) { return (cols * bytes + 15) / 16 * 16 + 16; }
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+// One input of a ring stage: the units around `cols` values at `row`.
+struct RmsRow {
+  const void* from;
+  uint32_t bytes, shift;
+};
+__device__ __forceinline__ RmsRow rms_row(const void* base, int64_t first, int cols, int elem) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(base) + (uintptr_t)(first * elem);
+  RmsRow r;
+  r.shift = (uint32_t)(at & 15u);
+  r.from = reinterpret_cast<const void*>(at - r.shift);
+  r.bytes = (r.shift + (uint32_t)cols * (uint32_t)elem + 15u) & ~15u;
+  return r;
+}
+
+// Sum over the WR warps of a row's group.
+template <int WR>
+__device__ __forceinline__ float rms_total(float v, float (&slots)[2][WR], int flip, int group, int lane, int in_row) {
+  v = warp_sum(v);
+  if constexpr (WR > 1) {
+    if (lane == 0) slots[flip][in_row] = v;
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(WR * 32) : "memory");
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < WR; ++w) v += slots[flip][w];
+  } else {
+    __syncwarp();
+  }
+  return v;
+}
+
+template <int XT, int WR, bool EDGE, bool RING>
+__global__ void __launch_bounds__(rms_threads(WR), WR > 8 ? 1 : 3)
+rms_norm_fprop_kernel(const __grid_constant__ RmsNormArgs args) {
+  typedef typename ElemOf<XT>::T T;
+  constexpr int kGroups = rms_groups(WR), kStep = 256 * WR;      // columns from a thread's first vector to its second
+  __shared__ float slots[kGroups][2][WR];
+  __shared__ __align__(8) uint64_t full[kGroups][kRmsMaxDepth];
+  extern __shared__ __align__(16) uint8_t ring[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int group = warp / WR, in_row = warp % WR, t = in_row * 32 + lane;
+  const uint32_t bars = smem_u32(full[group]);
+  if (RING && t == 0) {
+    for (int i = 0; i < kRmsMaxDepth; ++i) mbar_init(bars + 8u * i, 1);
+    fence_mbar_init();
+    fence_proxy_async_smem();
+  }
+  if (RING) __syncthreads();
+  let_next_start();
+  wait_for_previous();
+  const T* x = static_cast<const T*>(args.x);
+  const T* res = static_cast<const T*>(args.res);
+  const int64_t step = (int64_t)gridDim.x * kGroups, first = (int64_t)blockIdx.x * kGroups + group;
+  const uint32_t part = (uint32_t)rms_stage_row(args.cols, sizeof(T)), stage = res ? 2 * part : part;
+  uint8_t* mine = ring + (size_t)group * args.depth * stage;
+  auto fetch = [&](int64_t r, int slot) {       // (one thread of the group)
+    if (r >= args.rows) return;
+    const RmsRow a = rms_row(x, r * args.ldx, args.cols, sizeof(T));
+    const RmsRow b = rms_row(res, r * args.ldr, args.cols, sizeof(T));
+    mbar_arrive_expect_tx(bars + 8u * slot, a.bytes + (res ? b.bytes : 0u));
+    const uint32_t dst = smem_u32(mine) + (uint32_t)slot * stage;
+    bulk_load(dst, a.from, a.bytes, bars + 8u * slot);
+    if (res) bulk_load(dst + part, b.from, b.bytes, bars + 8u * slot);
+  };
+  if (RING && t == 0)
+    for (int d = 0; d < args.depth; ++d) fetch(first + d * step, d);
+  int n[2];
+  F2 g[2][4];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int c = 8 * t + kStep * j;
+    n[j] = vector_cols<EDGE>(args.cols, c);
+    load_weights8<EDGE>(args.gamma, c, n[j], args.w_type, 1.f, g[j]);
+  }
+  int slot = 0, flip = 0;
+  uint32_t phase = 0;
+  bool ok = true;
+  for (int64_t r = first; r < args.rows; r += step, flip ^= 1) {
+    Raw8<XT> rx[2], rr[2];
+    if constexpr (RING) {
+      // (a wait that ran out ends the launch's other waits too; its rows are then not valid)
+      ok &= mbar_wait(bars + 8u * slot, phase, args.wc, kDevTimeoutFull);
+      const uint32_t sx = (uint32_t)((uintptr_t)(r * args.ldx) * sizeof(T)) & 15u, sr = (uint32_t)((uintptr_t)(r * args.ldr) * sizeof(T)) & 15u;
+      const uint8_t* at = mine + (size_t)slot * stage;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        rx[j] = load_raw8<XT, EDGE>(reinterpret_cast<const T*>(at + (EDGE ? sx : 0u)) + 8 * t + kStep * j, n[j]);
+        if (res) rr[j] = load_raw8<XT, EDGE>(reinterpret_cast<const T*>(at + part + (EDGE ? sr : 0u)) + 8 * t + kStep * j, n[j]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        rx[j] = load_raw8<XT, EDGE>(x + r * args.ldx + 8 * t + kStep * j, n[j]);
+        if (res) rr[j] = load_raw8<XT, EDGE>(res + r * args.ldr + 8 * t + kStep * j, n[j]);
+      }
+    }
+    F2 h[2][4], sq = 0;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      to_pairs<XT>(rx[j], h[j]);
+      if (res) {
+        F2 b[4];
+        to_pairs<XT>(rr[j], b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[j][i] = add2(h[j][i], b[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sq = fma2(h[j][i], h[j][i], sq);
+    }
+    const float rstd = 1.f / sqrtf(rms_total<WR>(sum2(sq), slots[group], flip, group, lane, in_row) * args.inv_cols + args.eps);
+    if constexpr (RING) {
+      // every thread of the group has read this stage: the sum above needed its values
+      if (t == 0) fetch(r + args.depth * step, slot);
+      if (++slot == args.depth) { slot = 0; phase ^= 1u; }
+    }
+    if (t == 0 && args.rstd) args.rstd[r] = rstd;
+    if (args.sum) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) store_pairs<XT, EDGE>(static_cast<T*>(args.sum) + r * args.ldr + 8 * t + kStep * j, h[j], n[j]);
+    }
+    const int64_t at = r * args.ldq + 8 * t, scale_at = (int64_t)(t >> 4) * args.rows + r, scale_step = (int64_t)(kStep / kBlock8) * args.rows;
+    if (args.c)
+      norm_pack<kEitherFp8, EDGE>(h[0], h[1], args.q_e5m2, args.c + at, args.c + at + kStep, args.sc + scale_at, args.sc + scale_at + scale_step,
+                                  n[0], n[1], lane);
+    if (!args.y && !args.q) continue;
+    const F2 rs = f2(rstd);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        h[j][i] = mul2(mul2(h[j][i], rs), g[j][i]);
+        // columns past the end take part in the block's maximum: zeros (0 x infinity is none)
+        if (EDGE) {
+          const float2 u = unf2(h[j][i]);
+          h[j][i] = f2(2 * i < n[j] ? u.x : 0.f, 2 * i + 1 < n[j] ? u.y : 0.f);
+        } else if (n[j] == 0) {
+          h[j][i] = 0;
+        }
+      }
+      if (args.y) store_pairs<XT, EDGE>(static_cast<T*>(args.y) + r * args.ldy + 8 * t + kStep * j, h[j], n[j]);
+    }
+    if (args.q)
+      norm_pack<kEitherFp8, EDGE>(h[0], h[1], args.q_e5m2, args.q + at, args.q + at + kStep, args.s + scale_at, args.s + scale_at + scale_step,
+                                  n[0], n[1], lane);
+  }
+  if (RING && !ok && t == 0)      // leaving early: give copies already issued time to land
+    for (int i = 0; i < args.depth; ++i) mbar_wait_grace(bars + 8u * i, i < slot ? phase ^ 1u : phase);
+}
+
+// Rows too long for the registers of a CTA: read once for the sum, and again (from the second-level cache) for
+// the results.  `sum` is written in the second reading, so that it may be the residual's own memory.
+template <int XT>
+__global__ void __launch_bounds__(1024) rms_norm_fprop_long_kernel(const __grid_constant__ RmsNormArgs args) {
+  let_next_start();
+  wait_for_previous();
+  typedef typename ElemOf<XT>::T T;
+  __shared__ float slots[2][kNormMaxWarps];
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int steps = (int)(((int64_t)args.cols + 8191) / 8192);
+  const T* x = static_cast<const T*>(args.x);
+  const T* res = static_cast<const T*>(args.res);
+  int flip = 0;
+  for (int64_t r = blockIdx.x; r < args.rows; r += gridDim.x, flip ^= 1) {
+    float acc = 0.f, rstd = 0.f;
+    for (int pass = 0; pass < 2; ++pass) {
+      for (int i = 0; i < steps; ++i) {
+        const int c = 8 * t + 8192 * i;
+        const int n = min(max(args.cols - c, 0), 8);
+        F2 h[4], none[4] = {};
+        to_pairs<XT>(load_raw8<XT, true>(x + r * args.ldx + c, n), h);
+        if (res) {
+          F2 b[4];
+          to_pairs<XT>(load_raw8<XT, true>(res + r * args.ldr + c, n), b);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) h[k] = add2(h[k], b[k]);
+        }
+        if (pass == 0) {
+          F2 sq = 0;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) sq = fma2(h[k], h[k], sq);
+          acc += sum2(sq);
+          continue;
+        }
+        if (args.sum) store_pairs<XT, true>(static_cast<T*>(args.sum) + r * args.ldr + c, h, n);
+        const int64_t scale_at = (int64_t)(c >> 7) * args.rows + r;
+        if (args.c)
+          norm_pack<kEitherFp8, true>(h, none, args.q_e5m2, args.c + r * args.ldq + c, nullptr, args.sc + scale_at, nullptr, n, 0, lane);
+        if (!args.y && !args.q) continue;
+        F2 g[4];
+        load_weights8<true>(args.gamma, c, n, args.w_type, 1.f, g);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 u = unf2(mul2(mul2(h[k], f2(rstd)), g[k]));
+          h[k] = f2(2 * k < n ? u.x : 0.f, 2 * k + 1 < n ? u.y : 0.f);
+        }
+        if (args.y) store_pairs<XT, true>(static_cast<T*>(args.y) + r * args.ldy + c, h, n);
+        if (args.q)
+          norm_pack<kEitherFp8, true>(h, none, args.q_e5m2, args.q + r * args.ldq + c, nullptr, args.s + scale_at, nullptr, n, 0, lane);
+      }
+      if (pass == 1) break;
+      rstd = 1.f / sqrtf(cta_sum(acc, slots[flip], lane, warp) * args.inv_cols + args.eps);
+    }
+    if (t == 0 && args.rstd) args.rstd[r] = rstd;
+  }
+}
+
+// Backward.  A group has neighbouring rows (so that a packed row's scale bytes, which lie rows apart, come from
+// the first-level cache); its threads keep dg of their columns for all of them.  With 32 warps to a row there are
+// 64 registers to a thread: the row is then read from the stage again for dx, and released after that.
+template <int XT, int YT, int WR, bool EDGE>
+__global__ void __launch_bounds__(rms_threads(WR), WR > 8 ? 1 : 2)
+rms_norm_bprop_kernel(const __grid_constant__ RmsNormArgs args) {
+  typedef typename ElemOf<XT>::T TX;
+  typedef typename ElemOf<YT>::T TY;
+  constexpr int kGroups = rms_groups(WR), kStep = 256 * WR;
+  constexpr bool kAgain = WR > 16;
+  __shared__ float slots[kGroups][2][WR];
+  __shared__ __align__(8) uint64_t full[kGroups][kRmsMaxDepth];
+  __shared__ float fold[kGroups > 1 ? 512 * WR : 1];
+  extern __shared__ __align__(16) uint8_t ring[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int group = warp / WR, in_row = warp % WR, t = in_row * 32 + lane;
+  const uint32_t bars = smem_u32(full[group]);
+  if (t == 0) {
+    for (int i = 0; i < kRmsMaxDepth; ++i) mbar_init(bars + 8u * i, 1);
+    fence_mbar_init();
+    fence_proxy_async_smem();
+  }
+  __syncthreads();
+  let_next_start();
+  wait_for_previous();
+  const TX* x = static_cast<const TX*>(args.x);
+  const TY* dy = static_cast<const TY*>(args.dy);
+  const TY* ds = static_cast<const TY*>(args.res);
+  const int64_t groups = (int64_t)gridDim.x * kGroups, me = (int64_t)blockIdx.x * kGroups + group;
+  const int64_t r0 = args.rows * me / groups, r1 = args.rows * (me + 1) / groups;
+  const uint32_t part_x = (uint32_t)rms_stage_row(args.cols, sizeof(TX)), part_y = (uint32_t)rms_stage_row(args.cols, sizeof(TY));
+  const uint32_t stage = part_x + (ds ? 2 : 1) * part_y;
+  uint8_t* mine = ring + (size_t)group * args.depth * stage;
+  auto fetch = [&](int64_t r, int slot) {
+    if (r >= r1) return;
+    const RmsRow a = rms_row(x, r * args.ldx, args.cols, sizeof(TX));
+    const RmsRow b = rms_row(dy, r * args.ldy, args.cols, sizeof(TY));
+    const RmsRow d = rms_row(ds, r * args.ldr, args.cols, sizeof(TY));
+    mbar_arrive_expect_tx(bars + 8u * slot, a.bytes + b.bytes + (ds ? d.bytes : 0u));
+    const uint32_t dst = smem_u32(mine) + (uint32_t)slot * stage;
+    bulk_load(dst, a.from, a.bytes, bars + 8u * slot);
+    bulk_load(dst + part_x, b.from, b.bytes, bars + 8u * slot);
+    if (ds) bulk_load(dst + part_x + part_y, d.from, d.bytes, bars + 8u * slot);
+  };
+  if (t == 0)
+    for (int d = 0; d < args.depth; ++d) fetch(r0 + d, d);
+  int n[2];
+  F2 g[2][4], dg[2][4];
+  const uint8_t* scales[2];
+  float rstd_next = r0 < r1 ? args.rstd[r0] : 0.f;
+  uint32_t byte_next[2] = {0, 0};
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int c = 8 * t + kStep * j;
+    n[j] = vector_cols<EDGE>(args.cols, c);
+    load_weights8<EDGE>(args.gamma, c, n[j], args.w_type, 1.f, g[j]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dg[j][i] = 0;
+    scales[j] = args.x_scale + (int64_t)(c >> 7) * args.rows;
+    if (is_fp8(XT) && n[j] > 0 && r0 < r1) byte_next[j] = scales[j][r0];
+  }
+  int slot = 0, flip = 0;
+  uint32_t phase = 0;
+  bool ok = true;
+  for (int64_t r = r0; r < r1; ++r, flip ^= 1) {
+    const float rstd = rstd_next;
+    F2 k[2];               // what a value of h is multiplied by to give hh
+#pragma unroll
+    for (int j = 0; j < 2; ++j) k[j] = f2(is_fp8(XT) ? (n[j] > 0 ? e8m0_value(byte_next[j]) : 0.f) : rstd);
+    if (r + 1 < r1) {      // the next row's, on their way during this one
+      rstd_next = args.rstd[r + 1];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (is_fp8(XT) && n[j] > 0) byte_next[j] = scales[j][r + 1];
+    }
+    ok &= mbar_wait(bars + 8u * slot, phase, args.wc, kDevTimeoutFull);
+    const uint8_t* at = mine + (size_t)slot * stage;
+    const uint32_t sx = EDGE ? (uint32_t)((uintptr_t)(r * args.ldx) * sizeof(TX)) & 15u : 0u;
+    const uint32_t sy = EDGE ? (uint32_t)((uintptr_t)(r * args.ldy) * sizeof(TY)) & 15u : 0u;
+    const uint32_t sd = EDGE ? (uint32_t)((uintptr_t)(r * args.ldr) * sizeof(TY)) & 15u : 0u;
+    // hh and dy of eight columns
+    auto values = [&](int j, F2 (&hh)[4], F2 (&e)[4]) {
+      to_pairs<XT>(load_raw8<XT, EDGE>(reinterpret_cast<const TX*>(at + sx) + 8 * t + kStep * j, n[j]), hh);
+      to_pairs<YT>(load_raw8<YT, EDGE>(reinterpret_cast<const TY*>(at + part_x + sy) + 8 * t + kStep * j, n[j]), e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        hh[i] = mul2(hh[i], k[j]);
+        if (is_fp8(XT)) hh[i] = mul2(hh[i], f2(rstd));
+      }
+    };
+    F2 hh[2][4], e[2][4], part = 0;
+    Raw8<YT> rd[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      values(j, hh[j], e[j]);
+      if (!kAgain && ds) rd[j] = load_raw8<YT, EDGE>(reinterpret_cast<const TY*>(at + part_x + part_y + sd) + 8 * t + kStep * j, n[j]);
+      if (n[j] > 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          dg[j][i] = fma2(e[j][i], hh[j][i], dg[j][i]);
+          e[j][i] = mul2(e[j][i], g[j][i]);
+          part = fma2(e[j][i], hh[j][i], part);
+        }
+      }
+    }
+    const float s = rms_total<WR>(sum2(part), slots[group], flip, group, lane, in_row) * args.inv_cols;
+    if (!kAgain && t == 0) fetch(r + args.depth, slot);
+    const F2 rs = f2(rstd), ms = f2(-s * rstd);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (kAgain) {
+        values(j, hh[j], e[j]);
+        if (ds) rd[j] = load_raw8<YT, EDGE>(reinterpret_cast<const TY*>(at + part_x + part_y + sd) + 8 * t + kStep * j, n[j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[j][i] = mul2(e[j][i], g[j][i]);
+      }
+      F2 o[4];
+      if (ds) {
+        to_pairs<YT>(rd[j], o);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = add2(fma2(hh[j][i], ms, mul2(e[j][i], rs)), o[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fma2(hh[j][i], ms, mul2(e[j][i], rs));
+      }
+      store_pairs<YT, EDGE>(static_cast<TY*>(args.dx) + r * args.ldy + 8 * t + kStep * j, o, n[j]);
+    }
+    if (kAgain) {
+      __syncthreads();
+      if (t == 0) fetch(r + args.depth, slot);
+    }
+    if (++slot == args.depth) { slot = 0; phase ^= 1u; }
+  }
+  if (!ok && t == 0)
+    for (int i = 0; i < args.depth; ++i) mbar_wait_grace(bars + 8u * i, i < slot ? phase ^ 1u : phase);
+  if (!args.partial) return;
+  float* out = args.partial + (int64_t)blockIdx.x * norm_sums_pitch(args.cols);
+  // the CTA's sum over its groups, in their order
+  if constexpr (kGroups > 1) {
+    for (int w = 0; w < kGroups; ++w) {
+      if (group == w) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float a[8];
+          to_floats(dg[j], a);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {      // place i of vector (t, j)
+            float& f = fold[(8 * j + i) * 32 * WR + t];
+            f = w == 0 ? a[i] : f + a[i];
+          }
+        }
+      }
+      __syncthreads();
+    }
+    for (int c = threadIdx.x; c < args.cols; c += rms_threads(WR)) {
+      const int j = c / kStep, in = c - kStep * j;
+      out[c] = fold[(8 * j + (in & 7)) * 32 * WR + (in >> 3)];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int c = 8 * t + kStep * j;
+      float a[8];
+      to_floats(dg[j], a);
+      if (c < args.cols) store_sums8(out + c, a);
+    }
+  }
+}
+
+// Long rows backward: the row's sum, then dx from a second reading; dg goes to the CTA's sums in memory (this CTA
+// alone writes them, each thread always the same columns).
+template <int XT, int YT>
+__global__ void __launch_bounds__(1024) rms_norm_bprop_long_kernel(const __grid_constant__ RmsNormArgs args) {
+  let_next_start();
+  wait_for_previous();
+  typedef typename ElemOf<XT>::T TX;
+  typedef typename ElemOf<YT>::T TY;
+  __shared__ float slots[2][kNormMaxWarps];
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int steps = (int)(((int64_t)args.cols + 8191) / 8192);
+  float* out = args.partial ? args.partial + (int64_t)blockIdx.x * norm_sums_pitch(args.cols) : nullptr;
+  bool first = true;
+  int flip = 0;
+  for (int64_t r = blockIdx.x; r < args.rows; r += gridDim.x, flip ^= 1) {
+    const float rstd = args.rstd[r];
+    float s = 0.f;
+    for (int pass = 0; pass < 2; ++pass) {
+      for (int i = 0; i < steps; ++i) {
+        const int c = 8 * t + 8192 * i;
+        const int n = min(max(args.cols - c, 0), 8);
+        F2 hh[4], e[4], g[4];
+        to_pairs<XT>(load_raw8<XT, true>(static_cast<const TX*>(args.x) + r * args.ldx + c, n), hh);
+        to_pairs<YT>(load_raw8<YT, true>(static_cast<const TY*>(args.dy) + r * args.ldy + c, n), e);
+        load_weights8<true>(args.gamma, c, n, args.w_type, 1.f, g);
+        float scale = 1.f;
+        if (is_fp8(XT)) scale = n > 0 ? e8m0_value(args.x_scale[(int64_t)(c >> 7) * args.rows + r]) : 0.f;
+        float pg[8] = {};
+        const bool add = pass == 0 && out && n > 0;
+        if (add && !first) load_sums8(out + c, pg);
+        F2 part = 0, o[4] = {};
+        if (pass == 1 && args.res) to_pairs<YT>(load_raw8<YT, true>(static_cast<const TY*>(args.res) + r * args.ldr + c, n), o);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (is_fp8(XT)) hh[k] = mul2(hh[k], f2(scale));
+          hh[k] = mul2(hh[k], f2(rstd));
+          const float2 u = unf2(mul2(e[k], hh[k]));
+          pg[2 * k] += u.x;
+          pg[2 * k + 1] += u.y;
+          e[k] = mul2(e[k], g[k]);
+          part = fma2(e[k], hh[k], part);
+          o[k] = add2(fma2(hh[k], f2(-s * rstd), mul2(e[k], f2(rstd))), o[k]);
+        }
+        if (add) store_sums8(out + c, pg);
+        if (pass == 0 && n > 0) s += sum2(part);
+        if (pass == 1) store_pairs<YT, true>(static_cast<TY*>(args.dx) + r * args.ldy + c, o, n);
+      }
+      if (pass == 0) s = cta_sum(s, slots[flip], lane, warp) * args.inv_cols;
+    }
+    first = false;
+  }
+}
+
+// dg from the CTAs' sums, in CTA order.  A CTA takes 32 columns; each of its 16 warps takes every sixteenth sum, four at a
+// time, and the warps' results are added in warp order.
+__global__ void __launch_bounds__(512) rms_norm_fold_kernel(const float* partial, int parts, int cols, float* dgamma) {
+  let_next_start();
+  wait_for_previous();
+  __shared__ float part[16][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t c = (int64_t)blockIdx.x * 32 + lane, pitch = norm_sums_pitch(cols);
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (c < cols) {
+    const float* at = partial + c;
+    int p = warp;
+    for (; p + 48 < parts; p += 64) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] += at[(int64_t)(p + 16 * i) * pitch];
+    }
+    for (; p < parts; p += 16) s[0] += at[(int64_t)p * pitch];
+  }
+  part[warp][lane] = (s[0] + s[1]) + (s[2] + s[3]);
+  __syncthreads();
+  if (warp != 0 || c >= cols) return;
+  float total = 0.f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) total += part[w][lane];
+  dgamma[c] = total;
+}
+
+}  // namespace maxdnn

@@ -23,6 +23,10 @@ decltype(&maxdnn_layer_norm_fprop) f_layer_norm_fprop;
 decltype(&maxdnn_layer_norm_bprop) f_layer_norm_bprop;
 decltype(&maxdnn_act8_fprop) f_act8_fprop;
 decltype(&maxdnn_act8_bprop) f_act8_bprop;
+decltype(&maxdnn_rms_norm_fprop) f_rms_norm_fprop;
+decltype(&maxdnn_rms_norm_bprop) f_rms_norm_bprop;
+decltype(&maxdnn_logprob_fprop) f_logprob_fprop;
+decltype(&maxdnn_logprob_bprop) f_logprob_bprop;
 
 int64_t blocks(int64_t n) { return (n + 127) / 128; }
 
@@ -98,6 +102,26 @@ struct Call {
       ok = false;
     }
     return reinterpret_cast<void*>(v);
+  }
+  // contiguous bytes of any type
+  void* scratch(int i, size_t* bytes) {
+    *bytes = 0;
+    if (!ok || args[i] == Py_None) return nullptr;
+    const at::Tensor* t = tensor(i);
+    if (!t || !t->is_contiguous()) { ok = false; return nullptr; }
+    *bytes = t->nbytes();
+    return t->data_ptr();
+  }
+  // contiguous numbers of tokens
+  void* index(int i, bool wide, int64_t count, bool optional) {
+    if (!ok || args[i] == Py_None) { ok = ok && optional; return nullptr; }
+    const at::Tensor* t = tensor(i);
+    if (!t) return nullptr;
+    if (t->scalar_type() != (wide ? at::kLong : at::kInt) || t->numel() != count || !t->is_contiguous()) {
+      ok = false;
+      return nullptr;
+    }
+    return t->data_ptr();
   }
   // values and scales of a packed matrix: both or neither
   void pair(int i, int dtype, int64_t rows, int64_t cols, int64_t ld, int64_t n_scales, void** q, void** s) {
@@ -266,6 +290,92 @@ PyObject* act8_bprop(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MAXDNN_CATCH
 }
 
+PyObject* rms_norm_fprop(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MAXDNN_TRY
+  Call c(a, n, 12, sizeof(maxdnn_rms_norm_desc));
+  if (!c.ok) return not_plain();
+  const auto d = c.as<maxdnn_rms_norm_desc>();
+  const int64_t r = d.rows, k = d.cols, rs = blocks(k) * r;
+  void* x = c.mat(1, d.x_type, r, k, d.ldx);
+  void* res = c.mat(2, d.x_type, r, k, d.ldr, true);
+  void* gamma = c.vec(3, d.w_type, k, true);
+  void* sum = c.mat(4, d.x_type, r, k, d.ldr, true);
+  void* y = c.mat(5, d.y_type, r, k, d.ldy, true);
+  void* rstd = c.vec(6, MAXDNN_F32, r, true);
+  void *q, *s, *ck, *sc;
+  c.pair(7, d.q_type, r, k, d.ldq, rs, &q, &s);
+  c.pair(9, d.q_type, r, k, d.ldq, rs, &ck, &sc);
+  void* stream = c.stream(11);
+  if (!c.ok) return not_plain();
+  return unlocked([&] { return f_rms_norm_fprop(&d, x, res, gamma, sum, y, (float*)rstd, q, s, ck, sc, stream); });
+  MAXDNN_CATCH
+}
+
+PyObject* rms_norm_bprop(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MAXDNN_TRY
+  Call c(a, n, 11, sizeof(maxdnn_rms_norm_desc));
+  if (!c.ok) return not_plain();
+  const auto d = c.as<maxdnn_rms_norm_desc>();
+  const int64_t r = d.rows, k = d.cols;
+  void* dy = c.mat(1, d.y_type, r, k, d.ldy);
+  void* h = c.mat(2, d.x_type, r, k, d.ldx);
+  void* hs = d.x_type >= MAXDNN_E4M3 ? c.vec(3, MAXDNN_E8M0, blocks(k) * r) : nullptr;
+  void* gamma = c.vec(4, d.w_type, k, true);
+  void* rstd = c.vec(5, MAXDNN_F32, r);
+  void* ds = c.mat(6, d.y_type, r, k, d.ldr, true);
+  void* dx = c.mat(7, d.y_type, r, k, d.ldy);
+  void* dg = c.vec(8, MAXDNN_F32, k, true);
+  size_t ws_bytes;
+  void* ws = c.scratch(9, &ws_bytes);
+  void* stream = c.stream(10);
+  if (!c.ok) return not_plain();
+  return unlocked([&] { return f_rms_norm_bprop(&d, dy, h, hs, gamma, (float*)rstd, ds, dx, (float*)dg, ws, ws_bytes, stream); });
+  MAXDNN_CATCH
+}
+
+PyObject* logprob_fprop(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MAXDNN_TRY
+  Call c(a, n, 9, sizeof(maxdnn_logprob_desc));
+  if (!c.ok) return not_plain();
+  const auto d = c.as<maxdnn_logprob_desc>();
+  const int64_t r = d.rows;
+  void* x = c.mat(1, d.x_type, r, d.cols, d.ldx);
+  void* target = c.index(2, d.target_type == MAXDNN_INDEX_I64, r, true);
+  void* logprob = c.vec(3, MAXDNN_F32, r, true);
+  void* lse = c.vec(4, MAXDNN_F32, r, true);
+  void* entropy = c.vec(5, MAXDNN_F32, r, true);
+  void* top = c.vec(6, MAXDNN_F32, r * d.top, true);
+  void* at = c.index(7, false, r * d.top, true);
+  void* stream = c.stream(8);
+  if (!c.ok) return not_plain();
+  return unlocked([&] { return f_logprob_fprop(&d, x, target, (float*)logprob, (float*)lse, (float*)entropy, (float*)top, (int32_t*)at,
+                                               stream); });
+  MAXDNN_CATCH
+}
+
+PyObject* logprob_bprop(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MAXDNN_TRY
+  Call c(a, n, 13, sizeof(maxdnn_logprob_desc));
+  if (!c.ok) return not_plain();
+  const auto d = c.as<maxdnn_logprob_desc>();
+  const int64_t r = d.rows, k = d.cols;
+  void* x = c.mat(1, d.x_type, r, k, d.ldx);
+  void* target = c.index(2, d.target_type == MAXDNN_INDEX_I64, r, true);
+  void* lse = c.vec(3, MAXDNN_F32, r);
+  void* dlp = c.vec(4, MAXDNN_F32, r, true);
+  void* entropy = c.vec(5, MAXDNN_F32, r, true);
+  void* dh = c.vec(6, MAXDNN_F32, r, true);
+  void* dx = c.mat(7, d.x_type, r, k, d.ldd, true);
+  void *q[2], *s[2];
+  c.pair(8, d.q_type, r, k, d.ldq, blocks(k) * r, &q[0], &s[0]);
+  c.pair(10, d.q_type, r, k, d.ldq, blocks(r) * k, &q[1], &s[1]);
+  void* stream = c.stream(12);
+  if (!c.ok) return not_plain();
+  return unlocked([&] { return f_logprob_bprop(&d, x, target, (float*)lse, (float*)dlp, (float*)entropy, (float*)dh, dx, q[0], s[0], q[1],
+                                               s[1], stream); });
+  MAXDNN_CATCH
+}
+
 // bind(addresses): where the loaded library has the seven functions, in the order below.
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* p[7];
@@ -290,6 +400,27 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// bind_more(addresses): the same for the functions behind those.
+PyObject* bind_more(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void* p[4];
+  if (n != 4) {
+    PyErr_SetString(PyExc_TypeError, "bind_more takes four addresses");
+    return nullptr;
+  }
+  for (int i = 0; i < 4; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (!p[i]) {
+      if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address");
+      return nullptr;
+    }
+  }
+  f_rms_norm_fprop = reinterpret_cast<decltype(f_rms_norm_fprop)>(p[0]);
+  f_rms_norm_bprop = reinterpret_cast<decltype(f_rms_norm_bprop)>(p[1]);
+  f_logprob_fprop = reinterpret_cast<decltype(f_logprob_fprop)>(p[2]);
+  f_logprob_bprop = reinterpret_cast<decltype(f_logprob_bprop)>(p[3]);
+  Py_RETURN_NONE;
+}
+
 template <class F> PyCFunction fast(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 
 PyMethodDef methods[] = {
@@ -301,6 +432,11 @@ PyMethodDef methods[] = {
     {"layer_norm_bprop", fast(layer_norm_bprop), METH_FASTCALL, nullptr},
     {"act8_fprop", fast(act8_fprop), METH_FASTCALL, nullptr},
     {"act8_bprop", fast(act8_bprop), METH_FASTCALL, nullptr},
+    {"bind_more", fast(bind_more), METH_FASTCALL, nullptr},
+    {"rms_norm_fprop", fast(rms_norm_fprop), METH_FASTCALL, nullptr},
+    {"rms_norm_bprop", fast(rms_norm_bprop), METH_FASTCALL, nullptr},
+    {"logprob_fprop", fast(logprob_fprop), METH_FASTCALL, nullptr},
+    {"logprob_bprop", fast(logprob_bprop), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train8", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -13,15 +13,18 @@ __all__ = [
     "DTYPE_F32", "DTYPE_BF16", "DTYPE_F16", "DTYPE_E4M3", "DTYPE_E5M2", "DTYPE_E8M0",
     "BLOCK_ROW", "BLOCK_COL", "BLOCK_TILE", "MAJOR_K", "MAJOR_MN",
     "ACT_SILU", "ACT_GELU", "ACT_GELU_TANH",
-    "Quant8Desc", "Gemm8Desc", "LayerNormDesc", "Act8Desc",
+    "INDEX_I32", "INDEX_I64",
+    "Quant8Desc", "Gemm8Desc", "LayerNormDesc", "Act8Desc", "RmsNormDesc", "LogprobDesc",
     "quant8", "dequant8", "gemm8", "layer_norm_fprop", "layer_norm_bprop_workspace",
     "layer_norm_bprop", "act8_fprop", "act8_bprop", "empty_packed", "empty_scales",
+    "rms_norm_fprop", "rms_norm_bprop_workspace", "rms_norm_bprop", "logprob_fprop", "logprob_bprop",
 ]
 
 DTYPE_F32, DTYPE_BF16, DTYPE_F16, DTYPE_E4M3, DTYPE_E5M2, DTYPE_E8M0 = range(6)
 BLOCK_ROW, BLOCK_COL, BLOCK_TILE = range(3)
 MAJOR_K, MAJOR_MN = range(2)
 ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(3)
+INDEX_I32, INDEX_I64 = range(2)
 
 _vp = ctypes.c_void_p
 torch = None      # imported with the library, at the first call
@@ -99,6 +102,33 @@ class Act8Desc(ctypes.Structure):
                    1 if gated else 0)
 
 
+class RmsNormDesc(ctypes.Structure):
+    """maxdnn_rms_norm_desc."""
+
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64) for n in ("ldx", "ldr", "ldy", "ldq")] + \
+               [(n, ctypes.c_int32) for n in ("x_type", "y_type", "w_type", "q_type")] + [("eps", ctypes.c_float)]
+
+    @classmethod
+    def make(cls, rows, cols, eps=1e-6, x_type=DTYPE_BF16, y_type=None, w_type=DTYPE_F32, q_type=DTYPE_E4M3,
+             ldx=None, ldr=None, ldy=None, ldq=None) -> "RmsNormDesc":
+        return cls(int(rows), int(cols), _or(ldx, cols), _or(ldr, cols), _or(ldy, cols), _or(ldq, _round16(cols)), int(x_type),
+                   _or(y_type, x_type), int(w_type), int(q_type), float(eps))
+
+
+class LogprobDesc(ctypes.Structure):
+    """maxdnn_logprob_desc."""
+
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in ("ldx", "ldd", "ldq")] + \
+               [(n, ctypes.c_int32) for n in ("x_type", "q_type", "target_type", "top")] + [("scale", ctypes.c_float)]
+
+    @classmethod
+    def make(cls, rows, cols, top=0, scale=1.0, x_type=DTYPE_BF16, q_type=DTYPE_E5M2, target_type=INDEX_I64, ldx=None, ldd=None,
+             ldq=None) -> "LogprobDesc":
+        return cls(int(rows), int(cols), _or(ldx, cols), _or(ldd, cols), _or(ldq, _round16(cols)), int(x_type), int(q_type),
+                   int(target_type), int(top), float(scale))
+
+
 _lib = None
 
 
@@ -106,6 +136,7 @@ class _NoPlain:
     """Stands in where the marshalling module is not built: every call goes through the checks below."""
 
     quant8 = dequant8 = gemm8 = layer_norm_fprop = layer_norm_bprop = act8_fprop = act8_bprop = staticmethod(lambda *a: -1)
+    rms_norm_fprop = rms_norm_bprop = logprob_fprop = logprob_bprop = staticmethod(lambda *a: -1)
 
 
 _plain = _NoPlain
@@ -132,6 +163,8 @@ def _load_plain(lib):
         return _NoPlain
     _train8.bind(*(ctypes.cast(getattr(lib, "maxdnn_" + n), ctypes.c_void_p).value for n in (
         "quant8", "dequant8", "gemm8", "layer_norm_fprop", "layer_norm_bprop", "act8_fprop", "act8_bprop")))
+    _train8.bind_more(*(ctypes.cast(getattr(lib, "maxdnn_" + n), ctypes.c_void_p).value for n in (
+        "rms_norm_fprop", "rms_norm_bprop", "logprob_fprop", "logprob_bprop")))
     return _train8
 
 
@@ -163,7 +196,12 @@ def _library():
                 ("maxdnn_layer_norm_bprop_workspace", [P(LayerNormDesc), P(sz)]),
                 ("maxdnn_layer_norm_bprop", [P(LayerNormDesc)] + [_vp] * 10 + [sz, _vp]),
                 ("maxdnn_act8_fprop", [P(Act8Desc)] + [_vp] * 7),
-                ("maxdnn_act8_bprop", [P(Act8Desc)] + [_vp] * 5)):
+                ("maxdnn_act8_bprop", [P(Act8Desc)] + [_vp] * 5),
+                ("maxdnn_rms_norm_fprop", [P(RmsNormDesc)] + [_vp] * 11),
+                ("maxdnn_rms_norm_bprop_workspace", [P(RmsNormDesc), P(sz)]),
+                ("maxdnn_rms_norm_bprop", [P(RmsNormDesc)] + [_vp] * 9 + [sz, _vp]),
+                ("maxdnn_logprob_fprop", [P(LogprobDesc)] + [_vp] * 8),
+                ("maxdnn_logprob_bprop", [P(LogprobDesc)] + [_vp] * 12)):
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = ctypes.c_int, args
         _plain = _load_plain(lib)
@@ -385,3 +423,107 @@ def act8_bprop(desc: Act8Desc, da, h, dh, h_scale=None, stream=None) -> None:
         _mat(h, desc.h_type, r, many * c, desc.ldc if packed else desc.ldh, "h"),
         _scales(h_scale, many * _n_scales(BLOCK_ROW, r, c), "h_scale") if packed else None,
         _mat(dh, desc.x_type, r, many * c, desc.ldh, "dh"), _stream(stream)), "maxdnn_act8_bprop")
+
+
+def _or_none(t, check, *args):
+    return None if t is None else check(t, *args)
+
+
+def _scratch(t):
+    """(address, bytes) of a workspace that may not be given."""
+    if t is None:
+        return None, 0
+    _on_device(t, "workspace")
+    if not t.is_contiguous():
+        raise TypeError("workspace must be a contiguous CUDA tensor")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def rms_norm_fprop(desc: RmsNormDesc, x, gamma=None, residual=None, sum=None, y=None, rstd=None, packed=None, checkpoint=None,
+                   stream=None) -> None:
+    """maxdnn_rms_norm_fprop; sum: x + residual, packed: (q, s) of y, checkpoint: (c, sc) of the sum."""
+    lib = _library()
+    none = (None, None)
+    status = _plain.rms_norm_fprop(desc, x, residual, gamma, sum, y, rstd, *(packed or none), *(checkpoint or none),
+                                   None if stream is None else stream.cuda_stream)
+    if status >= 0:
+        return _raise(status, "maxdnn_rms_norm_fprop")
+    r, c = desc.rows, desc.cols
+    n = _n_scales(BLOCK_ROW, r, c)
+    q, s = _pair(packed, desc.q_type, r, c, desc.ldq, n, "packed")
+    k, sk = _pair(checkpoint, desc.q_type, r, c, desc.ldq, n, "checkpoint")
+    _raise(lib.maxdnn_rms_norm_fprop(
+        ctypes.byref(desc), _mat(x, desc.x_type, r, c, desc.ldx, "x"), _or_none(residual, _mat, desc.x_type, r, c, desc.ldr, "residual"),
+        _or_none(gamma, _vec, desc.w_type, c, "gamma"), _or_none(sum, _mat, desc.x_type, r, c, desc.ldr, "sum"),
+        _or_none(y, _mat, desc.y_type, r, c, desc.ldy, "y"), _or_none(rstd, _vec, DTYPE_F32, r, "rstd"), q, s, k, sk, _stream(stream)),
+        "maxdnn_rms_norm_fprop")
+
+
+def rms_norm_bprop_workspace(desc: RmsNormDesc) -> int:
+    """Bytes of device scratch maxdnn_rms_norm_bprop needs for dgamma."""
+    n = ctypes.c_size_t()
+    _raise(_library().maxdnn_rms_norm_bprop_workspace(ctypes.byref(desc), ctypes.byref(n)), "maxdnn_rms_norm_bprop_workspace")
+    return int(n.value)
+
+
+def rms_norm_bprop(desc: RmsNormDesc, dy, h, gamma, rstd, dx, dgamma=None, workspace=None, dsum=None, h_scale=None,
+                   stream=None) -> None:
+    """maxdnn_rms_norm_bprop; h: wide (the forward pass's sum), or the checkpoint with its h_scale."""
+    lib = _library()
+    status = _plain.rms_norm_bprop(desc, dy, h, h_scale, gamma, rstd, dsum, dx, dgamma, workspace,
+                                   None if stream is None else stream.cuda_stream)
+    if status >= 0:
+        return _raise(status, "maxdnn_rms_norm_bprop")
+    r, c, f32 = desc.rows, desc.cols, DTYPE_F32
+    ws, ws_bytes = _scratch(workspace)
+    _raise(lib.maxdnn_rms_norm_bprop(
+        ctypes.byref(desc), _mat(dy, desc.y_type, r, c, desc.ldy, "dy"), _mat(h, desc.x_type, r, c, desc.ldx, "h"),
+        None if desc.x_type < DTYPE_E4M3 else _scales(h_scale, _n_scales(BLOCK_ROW, r, c), "h_scale"),
+        _or_none(gamma, _vec, desc.w_type, c, "gamma"), _vec(rstd, f32, r, "rstd"), _or_none(dsum, _mat, desc.y_type, r, c, desc.ldr, "dsum"),
+        _mat(dx, desc.y_type, r, c, desc.ldy, "dx"), _or_none(dgamma, _vec, f32, c, "dgamma"), ws, ws_bytes, _stream(stream)),
+        "maxdnn_rms_norm_bprop")
+
+
+def _index(t, code, n, what):
+    """Address of a contiguous tensor of n numbers of tokens."""
+    _on_device(t, what)
+    if code not in (INDEX_I32, INDEX_I64) or t.dtype != (torch.int32, torch.int64)[code]:
+        raise TypeError("%s has dtype %s, which is not what the descriptor says" % (what, t.dtype))
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s has shape %s, expected %d contiguous elements" % (what, tuple(t.shape), n))
+    return t.data_ptr()
+
+
+def logprob_fprop(desc: LogprobDesc, x, target=None, logprob=None, lse=None, entropy=None, top_logprob=None, top_index=None,
+                  stream=None) -> None:
+    """maxdnn_logprob_fprop."""
+    lib = _library()
+    status = _plain.logprob_fprop(desc, x, target, logprob, lse, entropy, top_logprob, top_index,
+                                  None if stream is None else stream.cuda_stream)
+    if status >= 0:
+        return _raise(status, "maxdnn_logprob_fprop")
+    r, f32, k = desc.rows, DTYPE_F32, desc.top
+    _raise(lib.maxdnn_logprob_fprop(
+        ctypes.byref(desc), _mat(x, desc.x_type, r, desc.cols, desc.ldx, "x"), _or_none(target, _index, desc.target_type, r, "target"),
+        _or_none(logprob, _vec, f32, r, "logprob"), _or_none(lse, _vec, f32, r, "lse"), _or_none(entropy, _vec, f32, r, "entropy"),
+        _or_none(top_logprob, _vec, f32, r * k, "top_logprob"), _or_none(top_index, _index, INDEX_I32, r * k, "top_index"), _stream(stream)),
+        "maxdnn_logprob_fprop")
+
+
+def logprob_bprop(desc: LogprobDesc, x, target, lse, dlogprob=None, entropy=None, dentropy=None, dx=None, row=None, col=None,
+                  stream=None) -> None:
+    """maxdnn_logprob_bprop; row, col: (values, scales) of the packed gradient."""
+    lib = _library()
+    none = (None, None)
+    status = _plain.logprob_bprop(desc, x, target, lse, dlogprob, entropy, dentropy, dx, *(row or none), *(col or none),
+                                  None if stream is None else stream.cuda_stream)
+    if status >= 0:
+        return _raise(status, "maxdnn_logprob_bprop")
+    r, c, f32 = desc.rows, desc.cols, DTYPE_F32
+    q, s = _pair(row, desc.q_type, r, c, desc.ldq, _n_scales(BLOCK_ROW, r, c), "row")
+    qc, sc = _pair(col, desc.q_type, r, c, desc.ldq, _n_scales(BLOCK_COL, r, c), "col")
+    _raise(lib.maxdnn_logprob_bprop(
+        ctypes.byref(desc), _mat(x, desc.x_type, r, c, desc.ldx, "x"), _or_none(target, _index, desc.target_type, r, "target"),
+        _vec(lse, f32, r, "lse"), _or_none(dlogprob, _vec, f32, r, "dlogprob"), _or_none(entropy, _vec, f32, r, "entropy"),
+        _or_none(dentropy, _vec, f32, r, "dentropy"), _or_none(dx, _mat, desc.x_type, r, c, desc.ldd, "dx"), q, s, qc, sc, _stream(stream)),
+        "maxdnn_logprob_bprop")
