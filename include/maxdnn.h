@@ -661,8 +661,8 @@ maxdnn_status maxdnn_logprob_bprop(const maxdnn_logprob_desc* desc, const void* 
  * memory, [steps][3] numbers a, b, c (read during the call); null: 3.4445, -4.7750, 2.0315 for every step.  The products
  * run on the tensor cores on operands rounded to FP16 with 32-bit sums; X itself is kept in 22 bits, the diagonals of A and
  * of the polynomial in 32, so that the result is about 1e-3 (of its norm) from the formula's, whatever the spectrum: less
- * than its rounding to BF16.  A matrix of zeros gives zeros, one with a NaN or infinity gives NaN.  The coefficients
- * have to keep every singular value of X below 100 (the default ones: below 1.3).  workspace: 16-byte
+ * than its rounding to BF16, and whatever the size of G, also far below eps.  A matrix of zeros gives zeros (with eps > 0), one with a NaN or infinity gives NaN.  The coefficients
+ * have to keep every singular value of X below 10 (the default ones: below 1.3).  workspace: 16-byte
  * aligned, its contents do not matter.  NOT_SUPPORTED: rows or cols above 65536, steps above 32.
  */
 typedef struct maxdnn_ortho_desc {

@@ -54,6 +54,7 @@ EXPORTED_SYMBOLS = [
     "maxdnn_act8_bprop",
     "maxdnn_rms_norm_fprop", "maxdnn_rms_norm_bprop_workspace", "maxdnn_rms_norm_bprop",
     "maxdnn_logprob_fprop", "maxdnn_logprob_bprop",
+    "maxdnn_orthogonalise_workspace", "maxdnn_orthogonalise",
 ]
 
 

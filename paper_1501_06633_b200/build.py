@@ -16,7 +16,8 @@ import warnings
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmaxdnn.so")
-SOURCES = ["maxdnn_api.cu", "train8_api.cu", "norm_api.cu", "rms_api.cu", "logprob_api.cu", "gemm8_api.cu", "plan.cpp", "gemm8_plan.cpp"]
+SOURCES = ["maxdnn_api.cu", "train8_api.cu", "norm_api.cu", "rms_api.cu", "logprob_api.cu", "gemm8_api.cu", "ortho_api.cu",
+           "plan.cpp", "gemm8_plan.cpp", "ortho_plan.cpp"]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "--threads", "0"]
 

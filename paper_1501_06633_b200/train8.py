@@ -14,10 +14,11 @@ __all__ = [
     "BLOCK_ROW", "BLOCK_COL", "BLOCK_TILE", "MAJOR_K", "MAJOR_MN",
     "ACT_SILU", "ACT_GELU", "ACT_GELU_TANH",
     "INDEX_I32", "INDEX_I64",
-    "Quant8Desc", "Gemm8Desc", "LayerNormDesc", "Act8Desc", "RmsNormDesc", "LogprobDesc",
+    "Quant8Desc", "Gemm8Desc", "LayerNormDesc", "Act8Desc", "RmsNormDesc", "LogprobDesc", "OrthoDesc",
     "quant8", "dequant8", "gemm8", "layer_norm_fprop", "layer_norm_bprop_workspace",
     "layer_norm_bprop", "act8_fprop", "act8_bprop", "empty_packed", "empty_scales",
     "rms_norm_fprop", "rms_norm_bprop_workspace", "rms_norm_bprop", "logprob_fprop", "logprob_bprop",
+    "orthogonalise_workspace", "orthogonalise",
 ]
 
 DTYPE_F32, DTYPE_BF16, DTYPE_F16, DTYPE_E4M3, DTYPE_E5M2, DTYPE_E8M0 = range(6)
@@ -129,6 +130,20 @@ class LogprobDesc(ctypes.Structure):
                    int(target_type), int(top), float(scale))
 
 
+class OrthoDesc(ctypes.Structure):
+    """maxdnn_ortho_desc."""
+
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "rows", "cols", "steps")] + \
+               [(n, ctypes.c_int64) for n in ("ldx", "ldo", "stride_x", "stride_o")] + \
+               [("x_type", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+    @classmethod
+    def make(cls, rows, cols, batch=1, steps=5, x_type=DTYPE_BF16, eps=1e-7, ldx=None, ldo=None, stride_x=None, stride_o=None) -> "OrthoDesc":
+        ldx, ldo = _or(ldx, cols), _or(ldo, cols)
+        return cls(int(batch), int(rows), int(cols), int(steps), ldx, ldo, _or(stride_x, int(rows) * ldx), _or(stride_o, int(rows) * ldo),
+                   int(x_type), float(eps))
+
+
 _lib = None
 
 
@@ -201,7 +216,9 @@ def _library():
                 ("maxdnn_rms_norm_bprop_workspace", [P(RmsNormDesc), P(sz)]),
                 ("maxdnn_rms_norm_bprop", [P(RmsNormDesc)] + [_vp] * 9 + [sz, _vp]),
                 ("maxdnn_logprob_fprop", [P(LogprobDesc)] + [_vp] * 8),
-                ("maxdnn_logprob_bprop", [P(LogprobDesc)] + [_vp] * 12)):
+                ("maxdnn_logprob_bprop", [P(LogprobDesc)] + [_vp] * 12),
+                ("maxdnn_orthogonalise_workspace", [P(OrthoDesc), P(sz)]),
+                ("maxdnn_orthogonalise", [P(OrthoDesc)] + [_vp] * 4 + [sz, _vp])):
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = ctypes.c_int, args
         _plain = _load_plain(lib)
@@ -527,3 +544,40 @@ def logprob_bprop(desc: LogprobDesc, x, target, lse, dlogprob=None, entropy=None
         _vec(lse, f32, r, "lse"), _or_none(dlogprob, _vec, f32, r, "dlogprob"), _or_none(entropy, _vec, f32, r, "entropy"),
         _or_none(dentropy, _vec, f32, r, "dentropy"), _or_none(dx, _mat, desc.x_type, r, c, desc.ldd, "dx"), q, s, qc, sc, _stream(stream)),
         "maxdnn_logprob_bprop")
+
+
+def orthogonalise_workspace(desc: OrthoDesc) -> int:
+    """Bytes of device scratch maxdnn_orthogonalise needs."""
+    n = ctypes.c_size_t()
+    _raise(_library().maxdnn_orthogonalise_workspace(ctypes.byref(desc), ctypes.byref(n)), "maxdnn_orthogonalise_workspace")
+    return int(n.value)
+
+
+def _matrices(t, dtype, batch, rows, cols, ld, stride, what):
+    """Address of [batch][rows][cols] with row pitch ld, `stride` elements from matrix to matrix: such a 3-d view, or one matrix."""
+    if batch == 1 and getattr(t, "dim", lambda: 0)() == 2:
+        return _mat(t, dtype, rows, cols, ld, what)
+    _on_device(t, what)
+    if not 0 <= dtype < len(_TYPES) or t.dtype not in _TYPES[dtype]:
+        raise TypeError("%s has dtype %s, which is not what the descriptor says" % (what, t.dtype))
+    if t.shape != (batch, rows, cols):
+        raise ValueError("%s has shape %s, expected (%d, %d, %d)" % (what, tuple(t.shape), batch, rows, cols))
+    if t.numel() and ((cols > 1 and t.stride(2) != 1) or (rows > 1 and t.stride(1) != ld) or (batch > 1 and t.stride(0) != stride)):
+        raise ValueError("%s has strides %s, expected (%d, %d, 1)" % (what, tuple(t.stride()), stride, ld))
+    return t.data_ptr()
+
+
+def orthogonalise(desc: OrthoDesc, x, out, workspace, coefficients=None, stream=None) -> None:
+    """maxdnn_orthogonalise; coefficients: (a, b, c) for every step, or one such triple for each."""
+    lib = _library()
+    b, r, c = desc.batch, desc.rows, desc.cols
+    numbers = None
+    if coefficients is not None:
+        each = [tuple(k) for k in coefficients] if hasattr(coefficients[0], "__len__") else [tuple(coefficients)] * desc.steps
+        if len(each) != desc.steps or any(len(k) != 3 for k in each):
+            raise ValueError("coefficients: three numbers, or three for each of %d steps" % desc.steps)
+        numbers = (ctypes.c_float * (3 * desc.steps))(*[float(v) for k in each for v in k])
+    ws, ws_bytes = _scratch(workspace)
+    _raise(lib.maxdnn_orthogonalise(
+        ctypes.byref(desc), _matrices(x, desc.x_type, b, r, c, desc.ldx, desc.stride_x, "x"), numbers,
+        _matrices(out, DTYPE_BF16, b, r, c, desc.ldo, desc.stride_o, "out"), ws, ws_bytes, _stream(stream)), "maxdnn_orthogonalise")
