@@ -25,64 +25,76 @@ maxdnn_status matrix_map(CUtensorMap* m, const Matrices& x, int batch, uint32_t 
   const uint32_t box[3] = {box_cols, box_rows, 1u};
   return runtime_encode(m, x.type, 3, x.p, dims, str, box, swz);
 }
-maxdnn_status operand_map(CUtensorMap* m, const Matrices& x, int batch, bool mn, int rows) {
-  return matrix_map(m, x, batch, 64u, mn ? 64u : (uint32_t)rows, CU_TENSOR_MAP_SWIZZLE_128B);
-}
-maxdnn_status part_map(CUtensorMap* m, const Matrices& x, int batch) {
-  return matrix_map(m, x, batch, 32u, 32u, CU_TENSOR_MAP_SWIZZLE_64B);
-}
+maxdnn_status operand_map(CUtensorMap* m, const Matrices& x, int batch) { return matrix_map(m, x, batch, 64u, 64u, CU_TENSOR_MAP_SWIZZLE_128B); }
+maxdnn_status part_map(CUtensorMap* m, const Matrices& x, int batch) { return matrix_map(m, x, batch, 32u, 32u, CU_TENSOR_MAP_SWIZZLE_64B); }
 
-struct OrthoMaps { CUtensorMap a, b, in, in_lo, out, out_lo; };
-
-template <int NT, bool PAIR, int KIND>
-maxdnn_status launch_ortho(const RuntimeDevice& dev, const OrthoProduct& p, const OrthoMaps& m, const OrthoArgs& args, cudaStream_t stream) {
-  static std::atomic<bool> done[64];
-  if (!done[dev.index].load(std::memory_order_acquire)) {      // raising it twice does no harm
-    if (cudaFuncSetAttribute(ortho_product_kernel<NT, PAIR, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess) {
-      cudaGetLastError();
-      return MAXDNN_CUDA_ERROR;
-    }
-    done[dev.index].store(true, std::memory_order_release);
-  }
-  return launch_early(ortho_product_kernel<NT, PAIR, KIND>, (unsigned)p.grid, kOrthoThreads, (size_t)p.smem_bytes, PAIR ? 2 : 1, stream, m.a,
-                      m.b, m.in, m.in_lo, m.out, m.out_lo, args);
-}
-
-template <int KIND>
-maxdnn_status run_product(const RuntimeDevice& dev, const OrthoProduct& p, const OrthoMaps& m, OrthoArgs args, bool a_mn, bool b_mn, int batch,
-                          cudaStream_t stream) {
-  args.M = p.M;
-  args.N = p.N;
-  args.batch = batch;
-  args.m_tiles = p.m_tiles;
-  args.n_tiles = p.n_tiles;
-  args.tiles = p.tiles;
-  args.k_steps = p.k_steps;
-  args.stages = p.stages;
-  args.a_mn = a_mn;
-  args.b_mn = b_mn;
-  args.b_rows = p.b_rows;
-  args.b_stage_bytes = p.b_stage_bytes;
-  // instruction descriptor: fp32 accumulator, FP16 operands, majors, N / 8, M / 16
-  args.idesc = (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(p.nt >> 3) << 17) |
-               ((uint32_t)((p.pair ? 2 : 1) * kOrthoTileM >> 4) << 24);
-  args.test_missing_arrival = (uint32_t)option(OPT_TEST_MISSING_ARRIVAL);
-  args.wc = runtime_wait_ctx(dev);
-#define MAXDNN_ORTHO_CASE(NT, PAIR) \
-  if (p.nt == (NT) && (p.pair != 0) == (PAIR)) return launch_ortho<NT, PAIR, KIND>(dev, p, m, args, stream);
-  MAXDNN_ORTHO_CASE(256, true)
-  MAXDNN_ORTHO_CASE(128, true)
-  MAXDNN_ORTHO_CASE(128, false)
-  MAXDNN_ORTHO_CASE(64, false)
-#undef MAXDNN_ORTHO_CASE
+// Runs f with the kernel of a shape, and its PAIR.
+template <class F>
+maxdnn_status by_shape(int pair, int nt, F f) {
+  if (pair && nt == 256) return f(ortho_chain_kernel<256, true>);
+  if (pair && nt == 128) return f(ortho_chain_kernel<128, true>);
+  if (!pair && nt == 128) return f(ortho_chain_kernel<128, false>);
+  if (!pair && nt == 64) return f(ortho_chain_kernel<64, false>);
   return MAXDNN_NOT_SUPPORTED;
 }
+
+constexpr size_t kOrthoSmem = 227 * 1024;      // a CTA has an SM to itself
+
+cudaLaunchConfig_t chain_config(cudaLaunchAttribute (&attr)[2], int grid, int pair, size_t smem, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid, 1, 1);
+  cfg.blockDim = dim3(kOrthoThreads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  attr[0].id = cudaLaunchAttributeCooperative;      // its CTAs wait for one another
+  attr[0].val.cooperative = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = pair ? 2 : 1;
+  return cfg;
+}
+
+// CTAs and pairs of CTAs that a device runs at the same time, set up on its first call.
+maxdnn_status chain_slots(const RuntimeDevice& dev, int (&slots)[2]) {
+  static std::atomic<int> known[64];      // pairs + 1
+  int pairs = known[dev.index].load(std::memory_order_acquire) - 1;
+  if (pairs < 0) {
+    for (int pair = 0; pair < 2; ++pair)
+      for (int nt : {256, 128, 64}) {
+        if (pair ? nt == 64 : nt == 256) continue;
+        const maxdnn_status st = by_shape(pair, nt, [&](auto kern) {
+          if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kOrthoSmem) != cudaSuccess) {
+            cudaGetLastError();
+            return MAXDNN_CUDA_ERROR;
+          }
+          return MAXDNN_OK;
+        });
+        if (st != MAXDNN_OK) return st;
+      }
+    cudaLaunchAttribute attr[2];
+    const cudaLaunchConfig_t cfg = chain_config(attr, dev.sm_count / 2 * 2, 1, kOrthoSmem, nullptr);
+    if (cudaOccupancyMaxActiveClusters(&pairs, ortho_chain_kernel<256, true>, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      pairs = 0;
+    }
+    pairs = std::min(pairs, dev.sm_count / 2);
+    known[dev.index].store(pairs + 1, std::memory_order_release);
+  }
+  slots[0] = dev.sm_count;
+  slots[1] = pairs;
+  return MAXDNN_OK;
+}
+
+constexpr int kNominalSlots[2] = {148, 74};      // (the workspace's layout does not depend on the device)
 
 maxdnn_status orthogonalise_workspace(const maxdnn_ortho_desc* d, size_t* bytes) {
   maxdnn_status st = check_ortho(d);
   if (st != MAXDNN_OK || !bytes) return st != MAXDNN_OK ? st : MAXDNN_INVALID_VALUE;
   OrthoPlan p;
-  if ((st = plan_ortho(*d, 148, &p)) != MAXDNN_OK) return st;      // (the layout does not depend on the device)
+  if ((st = plan_ortho(*d, kNominalSlots, &p)) != MAXDNN_OK) return st;
   *bytes = (size_t)p.bytes;
   return MAXDNN_OK;
 }
@@ -97,11 +109,13 @@ maxdnn_status orthogonalise(const maxdnn_ortho_desc* d, const void* x, const flo
     for (int i = 0; i < 3 * d->steps; ++i)
       if (!std::isfinite(coefficients[i])) return MAXDNN_INVALID_VALUE;
   OrthoPlan p;
-  if ((st = plan_ortho(*d, 148, &p)) != MAXDNN_OK) return st;
+  if ((st = plan_ortho(*d, kNominalSlots, &p)) != MAXDNN_OK) return st;
   if (!workspace || !aligned16(workspace) || workspace_bytes < (size_t)p.bytes) return MAXDNN_INVALID_VALUE;
   RuntimeDevice dev;
   if ((st = runtime_device(&dev)) != MAXDNN_OK) return st;
-  if (dev.sm_count != 148 && (st = plan_ortho(*d, dev.sm_count, &p)) != MAXDNN_OK) return st;
+  int slots[2];
+  if ((st = chain_slots(dev, slots)) != MAXDNN_OK) return st;
+  if ((st = plan_ortho(*d, slots, &p)) != MAXDNN_OK) return st;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const int batch = d->batch;
   auto up8 = [](int64_t v) { return (v + 7) / 8 * 8; };
@@ -125,6 +139,7 @@ maxdnn_status orthogonalise(const maxdnn_ortho_desc* d, const void* x, const flo
   s.diag_a = reinterpret_cast<float*>(ws + p.diag_a);
   s.diag_b = reinterpret_cast<float*>(ws + p.diag_b);
   s.post = reinterpret_cast<float*>(ws + p.post);
+  s.done = reinterpret_cast<uint32_t*>(ws + p.done);
   s.growth = 1.f;
   float grown = 1.f;
   for (int i = 0; i < d->steps; ++i) {
@@ -153,70 +168,50 @@ maxdnn_status orthogonalise(const maxdnn_ortho_desc* d, const void* x, const flo
   });
   if (st != MAXDNN_OK) return st;
 
-  // ---- tensor-copy descriptors: Gram and update read X [0] and X [1] in turn
-  OrthoMaps gram[2], poly, update[2], last;
-  memset(gram, 0, sizeof(gram));
-  memset(&poly, 0, sizeof(poly));
-  memset(update, 0, sizeof(update));
+  // ---- all steps
+  OrthoMaps maps;
+  memset(&maps, 0, sizeof(maps));
   auto ok = [&](maxdnn_status r) { st = st == MAXDNN_OK ? r : st; };
-  const bool tall = p.tall != 0;
   for (int w = 0; w < 2; ++w) {
-    // the reduction runs along the longer side: rows of X where tall
-    ok(operand_map(&gram[w].a, mx[w][0], batch, tall, kOrthoTileM));
-    ok(operand_map(&gram[w].b, mx[w][0], batch, tall, p.gram.b_rows));
-    ok(part_map(&gram[w].out, ma, batch));
-    // X from the right (its rows are the reduction), or from the left
-    if (tall) {
-      ok(operand_map(&update[w].a, mx[w][0], batch, false, kOrthoTileM));
-      ok(operand_map(&update[w].b, mb, batch, false, p.update.b_rows));
-    } else {
-      ok(operand_map(&update[w].a, mb, batch, false, kOrthoTileM));
-      ok(operand_map(&update[w].b, mx[w][0], batch, true, p.update.b_rows));
-    }
-    ok(part_map(&update[w].in, mx[w][0], batch));
-    ok(part_map(&update[w].in_lo, mx[w][1], batch));
-    ok(part_map(&update[w].out, mx[1 - w][0], batch));
-    ok(part_map(&update[w].out_lo, mx[1 - w][1], batch));
+    ok(operand_map(&maps.x[w], mx[w][0], batch));
+    ok(part_map(&maps.x_hi[w], mx[w][0], batch));
+    ok(part_map(&maps.x_lo[w], mx[w][1], batch));
   }
-  ok(operand_map(&poly.a, ma, batch, false, kOrthoTileM));
-  ok(operand_map(&poly.b, ma, batch, false, p.poly.b_rows));
-  ok(part_map(&poly.in, ma, batch));
-  ok(part_map(&poly.out, mb, batch));
-  last = update[(d->steps - 1) & 1];
-  if (bulk_out) ok(part_map(&last.out, mo, batch));
+  ok(operand_map(&maps.a, ma, batch));
+  ok(operand_map(&maps.b, mb, batch));
+  ok(part_map(&maps.a_part, ma, batch));
+  ok(part_map(&maps.b_part, mb, batch));
+  if (bulk_out) ok(part_map(&maps.out, mo, batch));
   if (st != MAXDNN_OK) return st;
-
-  // ---- steps
   OrthoArgs args = {};
-  args.diag = p.diag;
-  args.diag_cols = tall;
+  for (int i = 0; i < 3; ++i) args.product[i] = p.product[i];
+  args.steps = d->steps;
+  args.batch = batch;
+  args.stages = p.stages;
+  args.tall = p.tall;
   args.bulk_out = bulk_out;
+  args.diag_a = s.diag_a;
+  args.diag_b = s.diag_b;
+  args.diag = p.diag;
+  args.post = s.post;
+  args.done = s.done;
   args.out = static_cast<__nv_bfloat16*>(out);
   args.ldo = d->ldo;
   args.stride_o = d->stride_o;
-  args.post = s.post;
-  float* diag_a = reinterpret_cast<float*>(ws + p.diag_a);
-  float* diag_b = reinterpret_cast<float*>(ws + p.diag_b);
-  for (int i = 0; i < d->steps; ++i) {
-    const float* c = coefficients ? coefficients + 3 * i : kOrthoCoefficients;
-    args.ca = c[0];
-    args.cb = c[1];
-    args.cc = c[2];
-    args.scale = std::ldexp(1.f, -2 * kOrthoScaleBits);
-    args.diag_in = nullptr;
-    args.diag_out = diag_a;
-    if ((st = run_product<kOrthoGram>(dev, p.gram, gram[i & 1], args, tall, tall, batch, stream)) != MAXDNN_OK) return st;
-    args.diag_in = diag_a;
-    args.diag_out = diag_b;
-    if ((st = run_product<kOrthoPoly>(dev, p.poly, poly, args, false, false, batch, stream)) != MAXDNN_OK) return st;
-    args.scale = std::ldexp(1.f, -kOrthoScaleBits);
-    args.diag_in = diag_b;
-    args.diag_out = nullptr;
-    st = i + 1 < d->steps ? run_product<kOrthoUpdate>(dev, p.update, update[i & 1], args, false, !tall, batch, stream)
-                          : run_product<kOrthoLast>(dev, p.update, last, args, false, !tall, batch, stream);
-    if (st != MAXDNN_OK) return st;
-  }
-  return MAXDNN_OK;
+  args.test_missing_arrival = (uint32_t)option(OPT_TEST_MISSING_ARRIVAL);
+  for (int i = 0; i < d->steps; ++i)
+    for (int k = 0; k < 3; ++k) args.coefficients[i][k] = coefficients ? coefficients[3 * i + k] : kOrthoCoefficients[k];
+  args.wc = runtime_wait_ctx(dev);
+  return by_shape(p.pair, p.nt, [&](auto kern) {
+    cudaLaunchAttribute attr[2];
+    const cudaLaunchConfig_t cfg = chain_config(attr, p.grid, p.pair, (size_t)p.smem_bytes, stream);
+    if (cudaLaunchKernelEx(&cfg, kern, maps, args) != cudaSuccess) {
+      cudaGetLastError();
+      return MAXDNN_CUDA_ERROR;
+    }
+    runtime_count_launch();
+    return MAXDNN_OK;
+  });
 }
 
 }  // namespace

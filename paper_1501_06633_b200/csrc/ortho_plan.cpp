@@ -9,9 +9,18 @@ namespace maxdnn {
 
 namespace {
 
-// Tile shapes with what a stage of 64 reduction steps takes in a long run and what a tile takes besides, in microseconds.
-struct Shape { int pair, nt; double step, tile; };
-constexpr Shape kShapes[] = {{1, 256, 0.29, 3.0}, {1, 128, 0.18, 2.2}, {0, 128, 0.17, 2.0}, {0, 64, 0.13, 1.6}};
+// Tile shapes with what the MMAs of a stage of 64 reduction steps take, what a tile's end takes and what a product takes
+// besides its tiles (a first copy, the exchange between CTAs), in microseconds.
+struct Shape { int pair, nt; double step, end, fixed; };
+constexpr Shape kShapes[] = {{1, 256, 0.30, 3.5, 3.0}, {1, 128, 0.16, 2.0, 3.0}, {0, 128, 0.15, 2.0, 3.0}, {0, 64, 0.09, 1.2, 3.0}};
+// What all SMs together read from the second-level cache (bytes in a microsecond; 4096 x 4096: 46 bytes a cycle and SM), and
+// how long a copy takes from its start to its end: a ring of stages cannot be faster than that for all of its stages.
+constexpr double kCacheRate = 11.0e6, kCopyTime = 1.0;
+int b_stage_bytes(const Shape& s) { return (s.pair ? s.nt / 2 : s.nt) * kOrthoBlockK * 2; }
+int ring_stages(int b_stage) {
+  const int fixed = 1024 + 512 + 2048 + kOrthoStaging, per_stage = 2 * kOrthoTileM * kOrthoBlockK + b_stage + 16;
+  return std::min(8, (232448 - fixed) / per_stage);
+}
 
 int64_t tiles_of(int64_t M, int64_t N, int tile_m, int nt, bool symmetric) {
   const int64_t mt = (M + tile_m - 1) / tile_m, n_tiles = (N + nt - 1) / nt;
@@ -21,34 +30,27 @@ int64_t tiles_of(int64_t M, int64_t N, int tile_m, int nt, bool symmetric) {
   return all;
 }
 
-void plan_product(OrthoProduct* p, int64_t M, int64_t N, int64_t K, bool symmetric, int batch, int sm_count) {
-  double best = 0;
-  for (const Shape& s : kShapes) {
-    const int tile_m = s.pair ? 2 * kOrthoTileM : kOrthoTileM;
-    const int64_t tiles = tiles_of(M, N, tile_m, s.nt, symmetric), slots = s.pair ? sm_count / 2 : sm_count;
-    const int64_t k_steps = (K + kOrthoBlockK - 1) / kOrthoBlockK, waves = (tiles * batch + slots - 1) / slots;
-    // a tile's result is stored while the next one's sums run
-    const double t = waves * std::max(k_steps * s.step, s.tile) + s.tile;
-    if (best > 0 && t >= best) continue;
-    best = t;
-    p->M = (int32_t)M;
-    p->N = (int32_t)N;
-    p->K = (int32_t)K;
-    p->symmetric = symmetric;
-    p->pair = s.pair;
-    p->nt = s.nt;
-    p->m_tiles = (int32_t)((M + tile_m - 1) / tile_m);
-    p->n_tiles = (int32_t)((N + s.nt - 1) / s.nt);
-    p->tiles = (int32_t)tiles;
-    p->k_steps = (int32_t)k_steps;
-    p->b_rows = s.pair ? s.nt / 2 : s.nt;
-    p->b_stage_bytes = p->b_rows * 2 * kOrthoBlockK;
-    p->grid = (int32_t)(std::min<int64_t>(tiles * batch, slots) * (s.pair ? 2 : 1));
-  }
-  const int fixed = 1024 + 512 + kOrthoStaging, per_stage = 2 * kOrthoTileM * kOrthoBlockK + p->b_stage_bytes + 16;
-  p->stages = std::min(8, (232448 - fixed) / per_stage);
-  p->smem_bytes = fixed + p->stages * per_stage;
-  if (p->pair) p->smem_bytes = std::max(p->smem_bytes, cluster_smem_floor(2 * p->nt));
+// The tiles of one product in a given shape; returns the time that it should take.
+double plan_product(OrthoProduct* p, int64_t M, int64_t N, int64_t K, bool symmetric, int batch, const Shape& s, int slots) {
+  const int tile_m = s.pair ? 2 * kOrthoTileM : kOrthoTileM;
+  const int64_t tiles = tiles_of(M, N, tile_m, s.nt, symmetric), all = tiles * batch;
+  p->M = (int32_t)M;
+  p->N = (int32_t)N;
+  p->symmetric = symmetric;
+  p->m_tiles = (int32_t)((M + tile_m - 1) / tile_m);
+  p->n_tiles = (int32_t)((N + s.nt - 1) / s.nt);
+  p->tiles = (int32_t)tiles;
+  p->k_steps = (int32_t)((K + kOrthoBlockK - 1) / kOrthoBlockK);
+  // halves have to be boxes of 64 columns for each CTA
+  const int64_t rest = all % slots;
+  const bool halves = rest > 0 && 2 * rest <= slots && s.nt / 2 / (s.pair ? 2 : 1) >= 64;
+  p->full = (int32_t)(halves ? all - rest : all);
+  p->items = (int32_t)(p->full + (halves ? 2 * rest : 0));
+  const int64_t active = std::min<int64_t>(p->items, slots) * (s.pair ? 2 : 1);
+  const double fill = (double)active * (2 * kOrthoTileM * kOrthoBlockK + b_stage_bytes(s)) / kCacheRate;
+  const double step = std::max(std::max(s.step, fill), kCopyTime / ring_stages(b_stage_bytes(s)));
+  const double tile = std::max(p->k_steps * step, s.end), whole = (double)((all - rest) / slots);
+  return s.fixed + whole * tile + (rest == 0 ? 0.0 : halves ? 0.6 * tile : tile) + s.end;
 }
 
 }  // namespace
@@ -63,7 +65,7 @@ maxdnn_status check_ortho(const maxdnn_ortho_desc* d) {
   return MAXDNN_OK;
 }
 
-maxdnn_status plan_ortho(const maxdnn_ortho_desc& d, int sm_count, OrthoPlan* p) {
+maxdnn_status plan_ortho(const maxdnn_ortho_desc& d, const int (&slots)[2], OrthoPlan* p) {
   *p = OrthoPlan();
   p->tall = d.rows > d.cols;
   p->n = std::min(d.rows, d.cols);
@@ -83,14 +85,43 @@ maxdnn_status plan_ortho(const maxdnn_ortho_desc& d, int sm_count, OrthoPlan* p)
   p->a = take(batch * p->n * p->pitch_n * 2);
   p->b = take(batch * p->n * p->pitch_n * 2);
   p->diag_a = take(batch * p->diag * 4);
-  p->diag_b = take(batch * p->diag * 4);
+  p->diag_b = take(batch * p->diag * 8);
   p->post = take(batch * 4);
+  p->done = take(4);
   p->sums = take(batch * p->parts * 8);
-  p->bytes = std::max<int64_t>(at, 16);
-  plan_product(&p->gram, p->n, p->n, p->m, true, d.batch, sm_count);
-  plan_product(&p->poly, p->n, p->n, p->n, true, d.batch, sm_count);
-  plan_product(&p->update, d.rows, d.cols, p->n, false, d.batch, sm_count);
-  if ((int64_t)p->update.tiles * batch > (1 << 30) || (int64_t)p->gram.tiles * batch > (1 << 30)) return MAXDNN_NOT_SUPPORTED;
+  p->bytes = at;
+  // one shape for all products of the launch: the one that a step should take least in
+  double best = 0;
+  for (const Shape& s : kShapes) {
+    OrthoProduct q[3] = {};
+    const int n_slots = slots[s.pair];
+    if (n_slots <= 0) continue;
+    const int tile_m = s.pair ? 2 * kOrthoTileM : kOrthoTileM;
+    // (numbers of tiles are 32 bits)
+    if (tiles_of(d.rows, d.cols, tile_m, s.nt, false) * batch > (1 << 28) || tiles_of(p->n, p->n, tile_m, s.nt, true) * batch > (1 << 28)) continue;
+    const double t = plan_product(&q[kOrthoGram], p->n, p->n, p->m, true, d.batch, s, n_slots) +
+                     plan_product(&q[kOrthoPoly], p->n, p->n, p->n, true, d.batch, s, n_slots) +
+                     plan_product(&q[kOrthoUpdate], d.rows, d.cols, p->n, false, d.batch, s, n_slots);
+    if (best > 0 && t >= best) continue;
+    best = t;
+    p->pair = s.pair;
+    p->nt = s.nt;
+    int32_t most = 0;
+    for (int i = 0; i < 3; ++i) {
+      p->product[i] = q[i];
+      most = std::max(most, q[i].items);
+    }
+    p->grid = std::min<int32_t>(most, n_slots) * (s.pair ? 2 : 1);
+  }
+  if (best == 0) return MAXDNN_NOT_SUPPORTED;
+  p->product[kOrthoGram].a_mode = p->product[kOrthoGram].b_mode = p->tall ? kOrthoRowsAreK : kOrthoKAlongRows;
+  p->product[kOrthoPoly].a_mode = p->product[kOrthoPoly].b_mode = kOrthoSymmetric;
+  p->product[kOrthoUpdate].a_mode = p->tall ? kOrthoKAlongRows : kOrthoSymmetric;
+  p->product[kOrthoUpdate].b_mode = p->tall ? kOrthoSymmetric : kOrthoRowsAreK;
+  const int b_stage = (p->pair ? p->nt / 2 : p->nt) * kOrthoBlockK * 2;
+  p->stages = ring_stages(b_stage);
+  p->smem_bytes = 1024 + 512 + 2048 + kOrthoStaging + p->stages * (2 * kOrthoTileM * kOrthoBlockK + b_stage + 16);
+  if (p->pair) p->smem_bytes = std::max(p->smem_bytes, cluster_smem_floor(2 * p->nt));
   return MAXDNN_OK;
 }
 

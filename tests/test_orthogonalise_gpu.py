@@ -149,3 +149,38 @@ def test_repeated_and_on_another_stream():
             torch.cuda.synchronize()
             assert torch.equal(out, call(y, "bf16"))
         assert mx.last_device_status() == mx.OK
+
+
+def test_two_calls_at_once():
+    """Each call's CTAs wait for one another: two of them, and a product, on streams of their own."""
+    xs = [gradients(1, 900, 1300, "bf16", 30), gradients(3, 400, 300, "bf16", 31)]
+    want = [call(x, "bf16") for x in xs]
+    outs = [torch.zeros_like(w) for w in want]
+    ds = [mx.OrthoDesc.make(x.shape[1], x.shape[2], batch=x.shape[0]) for x in xs]
+    wss = [torch.empty(mx.orthogonalise_workspace(d), dtype=torch.uint8, device="cuda") for d in ds]
+    q, s = mx.empty_packed(2048, 2048), mx.empty_scales(mx.BLOCK_ROW, 2048, 2048)
+    mx.quant8(mx.Quant8Desc.make(2048, 2048), torch.randn(2048, 2048, device="cuda").to(torch.bfloat16), row=(q, s))
+    g = mx.Gemm8Desc.make(2048, 2048, 2048, b_block=mx.BLOCK_ROW)
+    c, wc = (torch.zeros(2048, 2048, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    mx.gemm8(g, q, s, q, s, wc)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for d, x, out, ws, st in zip(ds, xs, outs, wss, streams):
+            mx.orthogonalise(d, x, out, ws, stream=st)
+        mx.gemm8(g, q, s, q, s, c, stream=streams[2])
+    torch.cuda.synchronize()
+    assert mx.last_device_status() == mx.OK
+    assert all(torch.equal(o, w) for o, w in zip(outs, want)) and torch.equal(c, wc)
+
+
+def test_a_wait_that_runs_out_is_reported():
+    x = gradients(1, 300, 300, "bf16", 40)
+    want = call(x, "bf16")
+    d = mx.OrthoDesc.make(300, 300)
+    out, ws = torch.empty_like(want), torch.empty(mx.orthogonalise_workspace(d), dtype=torch.uint8, device="cuda")
+    mx.set_option("TEST_MISSING_ARRIVAL", 1)
+    mx.orthogonalise(d, x, out, ws)
+    mx.reset_options()
+    assert mx.last_device_status() == mx.DEVICE_TIMEOUT
+    assert torch.equal(call(x, "bf16"), want)
