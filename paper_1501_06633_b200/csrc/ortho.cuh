@@ -166,13 +166,6 @@ __device__ __forceinline__ int epilogue_any(bool p) {
       : "memory");
   return r;
 }
-// Eight neighbouring entries of a diagonal, from shared memory.
-__device__ __forceinline__ void load_diag8(const float* p, float (&v)[8]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-  v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-
 template <int NT, bool PAIR>
 __global__ void __launch_bounds__(kOrthoThreads, 1)
 ortho_chain_kernel(const __grid_constant__ OrthoMaps maps, const __grid_constant__ OrthoArgs args) {
@@ -465,63 +458,55 @@ ortho_chain_kernel(const __grid_constant__ OrthoMaps maps, const __grid_constant
           uint8_t* row = part + lane * 64;
           const bool diagonal = (KIND == kOrthoGram || KIND == kOrthoPoly) && n0 == m_warp;      // the part's diagonal is the matrix's
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {                    // eight columns
+          for (int i = 0; i < 4; ++i) {                    // eight columns, in pairs
             uint4* hi_at = reinterpret_cast<uint4*>(row + ((i ^ swz) << 4));
             uint4* lo_at = reinterpret_cast<uint4*>(row + 2048 + ((i ^ swz) << 4));
-            float x[8], y[8];
+            F2 x[4], lo[4];
             if constexpr (kLoads > 0) {
               Raw8<MAXDNN_F16> raw;
               raw.a = *hi_at;
-              to_float8<MAXDNN_F16>(raw, x);
+              to_pairs<MAXDNN_F16>(raw, x);
             }
-            if constexpr (KIND == kOrthoGram) {
-#pragma unroll
-              for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(v[8 * i + k]) * gram_scale;
-            } else if constexpr (KIND == kOrthoPoly) {
-              float r8[8];
-              load_diag8(diag_here + 8 * i, r8);
-#pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const float r_here = diagonal && 8 * i + k == lane ? r_m : 0.f;
-                const float square = fmaf(r_here, r_here, fmaf(r_m + r8[k], x[k], __uint_as_float(v[8 * i + k])));
-                y[k] = fmaf(cb, x[k] + r_here, cc * square);
-              }
-            } else {
+            if constexpr (kLoads > 1) {
               Raw8<MAXDNN_F16> raw;
               raw.a = *lo_at;
-              float lo[8];
-              to_float8<MAXDNN_F16>(raw, lo);
-              if (args.tall) {
-                float r8[8], d8[8];
-                load_diag8(diag_here + 8 * i, r8);
-                load_diag8(diag_here + 32 + 8 * i, d8);
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                  y[k] = fmaf(ca + r8[k], x[k], fmaf((ca + d8[k]) * (1.f / kOrthoLo), lo[k], __uint_as_float(v[8 * i + k])));
-              } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) y[k] = fmaf(k_hi, x[k], fmaf(k_lo, lo[k], __uint_as_float(v[8 * i + k])));
-              }
+              to_pairs<MAXDNN_F16>(raw, lo);
             }
-            uint32_t w[4];
-            if constexpr (KIND == kOrthoLast) {
+            uint32_t w[4], z[4];
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const __nv_bfloat162 t = __floats2bfloat162_rn(y[2 * k] * out_scale, y[2 * k + 1] * out_scale);
-                w[k] = *reinterpret_cast<const uint32_t*>(&t);
+            for (int k = 0; k < 4; ++k) {
+              const F2 sum = ((F2)v[8 * i + 2 * k + 1] << 32) | v[8 * i + 2 * k];
+              const bool mine = diagonal && 8 * i + 2 * k == (lane & ~1);      // one of the two is on the diagonal
+              F2 y2;
+              if constexpr (KIND == kOrthoGram) {
+                y2 = mul2(sum, f2(gram_scale));
+              } else if constexpr (KIND == kOrthoPoly) {
+                const F2 r2 = *reinterpret_cast<const F2*>(diag_here + 8 * i + 2 * k);
+                y2 = fma2(f2(cb), x[k], mul2(f2(cc), fma2(add2(f2(r_m), r2), x[k], sum)));
+              } else if (args.tall) {
+                const F2 r2 = *reinterpret_cast<const F2*>(diag_here + 8 * i + 2 * k);
+                const F2 d2 = *reinterpret_cast<const F2*>(diag_here + 32 + 8 * i + 2 * k);
+                y2 = fma2(add2(f2(ca), r2), x[k], fma2(mul2(add2(f2(ca), d2), f2(1.f / kOrthoLo)), lo[k], sum));
+              } else {
+                y2 = fma2(f2(k_hi), x[k], fma2(f2(k_lo), lo[k], sum));
               }
-            } else {
-              uint32_t z[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const __half2 t = __floats2half2_rn(y[2 * k], y[2 * k + 1]);
+              float2 y = unf2(y2);
+              if constexpr (KIND == kOrthoLast) {
+                const __nv_bfloat162 t = __floats2bfloat162_rn(y.x * out_scale, y.y * out_scale);
                 w[k] = *reinterpret_cast<const uint32_t*>(&t);
-                const float2 back = __half22float2(t);
+              } else {
+                // (A_mm has r besides what FP16 holds of it, on both sides of its square too)
+                if (KIND == kOrthoPoly && mine) (lane & 1 ? y.y : y.x) += r_m * fmaf(cc, r_m, cb);
+                const __half2 t = __floats2half2_rn(y.x, y.y);
+                w[k] = *reinterpret_cast<const uint32_t*>(&t);
                 if constexpr (KIND == kOrthoUpdate) {
-                  const __half2 rest = __floats2half2_rn((y[2 * k] - back.x) * kOrthoLo, (y[2 * k + 1] - back.y) * kOrthoLo);
+                  const float2 back = __half22float2(t);
+                  const float2 left = unf2(mul2(add2(f2(y.x, y.y), f2(-back.x, -back.y)), f2(kOrthoLo)));
+                  const __half2 rest = __floats2half2_rn(left.x, left.y);
                   z[k] = *reinterpret_cast<const uint32_t*>(&rest);
-                } else if (diagonal && m < p.M && (8 * i + 2 * k) == (lane & ~1)) {
-                  const float all = lane & 1 ? y[2 * k + 1] : y[2 * k], rest = all - (lane & 1 ? back.y : back.x);
+                } else if (mine && m < p.M) {
+                  const float2 back = __half22float2(t);
+                  const float all = lane & 1 ? y.y : y.x, rest = all - (lane & 1 ? back.y : back.x);
                   if (KIND == kOrthoGram) {
                     args.diag_a[o.matrix * args.diag + m] = rest;
                   } else {
@@ -530,8 +515,8 @@ ortho_chain_kernel(const __grid_constant__ OrthoMaps maps, const __grid_constant
                   }
                 }
               }
-              if constexpr (KIND == kOrthoUpdate) *lo_at = make_uint4(z[0], z[1], z[2], z[3]);
             }
+            if constexpr (KIND == kOrthoUpdate) *lo_at = make_uint4(z[0], z[1], z[2], z[3]);
             *hi_at = make_uint4(w[0], w[1], w[2], w[3]);
           }
           const uint32_t src = slots + 4096u * slot;

@@ -5,6 +5,7 @@
 
 #include "api8.h"
 #include "ortho.cuh"
+#include "ortho_small.cuh"
 
 namespace maxdnn {
 namespace {
@@ -90,6 +91,51 @@ maxdnn_status chain_slots(const RuntimeDevice& dev, int (&slots)[2]) {
 
 constexpr int kNominalSlots[2] = {148, 74};      // (the workspace's layout does not depend on the device)
 
+// Matrices that a cluster has to itself.
+bool small_matrices(const maxdnn_ortho_desc& d) {
+  return std::min(d.rows, d.cols) <= kSmallN && std::max(d.rows, d.cols) <= kSmallSlice * kSmallMaxCluster;
+}
+
+maxdnn_status orthogonalise_small(const RuntimeDevice& dev, const maxdnn_ortho_desc& d, const void* x, const float* coefficients, void* out,
+                                  cudaStream_t stream) {
+  OrthoSmallArgs a = {};
+  a.x = x;
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.ldx = d.ldx;
+  a.ldo = d.ldo;
+  a.stride_x = d.stride_x;
+  a.stride_o = d.stride_o;
+  a.rows = d.rows;
+  a.cols = d.cols;
+  a.steps = d.steps;
+  a.eps = d.eps;
+  for (int i = 0; i < d.steps; ++i)
+    for (int k = 0; k < 3; ++k) a.coefficients[i][k] = coefficients ? coefficients[3 * i + k] : kOrthoCoefficients[k];
+  a.test_missing_arrival = (uint32_t)option(OPT_TEST_MISSING_ARRIVAL);
+  a.wc = runtime_wait_ctx(dev);
+  const int parts = (std::max(d.rows, d.cols) + kSmallSlice - 1) / kSmallSlice;
+  const size_t smem = (size_t)std::max(kSmallSmem, cluster_smem_floor(kSmallTmem));
+  const bool whole = d.cols % 8 == 0 && vec_ok(d.x_type, d.ldx) && (d.batch == 1 || vec_ok(d.x_type, d.stride_x));
+  return by_wide(d.x_type, [&](auto xt) {
+    return by_edge(whole, [&](auto edge) {
+      constexpr int X = decltype(xt)::value;
+      constexpr bool E = decltype(edge)::value != 0;
+      const bool tall = d.rows > d.cols;
+      auto kern = tall ? ortho_small_kernel<X, true, E> : ortho_small_kernel<X, false, E>;
+      static std::atomic<bool> done[2][64];
+      if (!done[tall][dev.index].load(std::memory_order_acquire)) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
+            cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+          cudaGetLastError();
+          return MAXDNN_CUDA_ERROR;
+        }
+        done[tall][dev.index].store(true, std::memory_order_release);
+      }
+      return launch_early(kern, (unsigned)(d.batch * parts), kSmallThreads, smem, parts, stream, a);
+    });
+  });
+}
+
 maxdnn_status orthogonalise_workspace(const maxdnn_ortho_desc* d, size_t* bytes) {
   maxdnn_status st = check_ortho(d);
   if (st != MAXDNN_OK || !bytes) return st != MAXDNN_OK ? st : MAXDNN_INVALID_VALUE;
@@ -113,6 +159,7 @@ maxdnn_status orthogonalise(const maxdnn_ortho_desc* d, const void* x, const flo
   if (!workspace || !aligned16(workspace) || workspace_bytes < (size_t)p.bytes) return MAXDNN_INVALID_VALUE;
   RuntimeDevice dev;
   if ((st = runtime_device(&dev)) != MAXDNN_OK) return st;
+  if (small_matrices(*d)) return orthogonalise_small(dev, *d, x, coefficients, out, stream);
   int slots[2];
   if ((st = chain_slots(dev, slots)) != MAXDNN_OK) return st;
   if ((st = plan_ortho(*d, slots, &p)) != MAXDNN_OK) return st;
