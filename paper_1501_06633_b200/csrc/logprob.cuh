@@ -9,10 +9,11 @@
 // values and the two sums relative to it (in 32 bits), which are joined by warp, CTA and cluster at the end.
 // Differences to the maximum come first, so a term's error does not grow with the size of the logits.
 //
-// The largest values come from the same reading.  Pairs of threads have 128 maxima between them; the k-th largest of
+// The largest values come from the same reading.  Groups of threads have 64 maxima between them; the k-th largest of
 // those is a bound that at least k values reach, and hardly more than k do (a value above it is missed only by threads
-// whose maximum is below it, and those have none).  The few threads whose maximum reaches the bound read their values
-// again, a warp together for each, and the values that reach it are ranked by value and index.  Rows where more than
+// whose maximum is below it, and those have none).  The maxima of the threads' segments (up to
+// 16 in each) tell where the values are that reach the bound; all threads read those few segments again and rank what they find by value
+// and index.  Rows where more than
 // kLpCandidates values do (many equal ones, as masks by the type's lowest value give) take the values above the bound
 // and then the first equal ones in order; what still does not fit (large values at one residue of the thread's stride),
 // and rows with NaN, take the largest one at a time.
@@ -26,7 +27,9 @@
 namespace maxdnn {
 
 constexpr int kLpThreads = 256;
-constexpr int kLpBounds = 128;            // maxima that the bound is taken from
+constexpr int kLpBatch = 8;               // loads of 16 bytes that a thread has under way
+constexpr int kLpSegments = 16;           // parts of a thread's values whose maxima are kept
+constexpr int kLpBounds = 64;             // maxima that the bound is taken from
 constexpr int kLpCandidates = 1024;
 constexpr int kLpMaxTop = 32;
 constexpr int kLpMaxCluster = 8;
@@ -100,6 +103,31 @@ struct LpVec {
     const uint32_t w = XT == MAXDNN_F32 ? 0xFF800000u : XT == MAXDNN_BF16 ? 0xFF80FF80u : 0xFC00FC00u;
     return make_uint4(w, w, w, w);
   }
+  // The largest value (NaN do not count), without widening 16-bit ones.
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    uint32_t r;
+    if constexpr (XT == MAXDNN_BF16) asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else if constexpr (XT == MAXDNN_F16) asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else r = __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    return r;
+  }
+  static __device__ __forceinline__ float most(uint32_t w) {
+    if constexpr (XT == MAXDNN_F32) {
+      return fmaxf(__uint_as_float(w), -__int_as_float(0x7F800000));
+    } else {
+      const uint32_t both = larger(larger(w, (w >> 16) | (w << 16)), masked().x);      // (a NaN alone: -inf)
+      if constexpr (XT == MAXDNN_BF16) return __uint_as_float(both << 16);
+      else return __half2float(__ushort_as_half((unsigned short)both));
+    }
+  }
+  static __device__ __forceinline__ float most(uint4 w) { return most(larger(larger(w.x, w.y), larger(w.z, w.w))); }
+  template <int N>
+  static __device__ __forceinline__ float most(const uint4 (&w)[N]) {
+    uint32_t r = larger(larger(w[0].x, w[0].y), larger(w[0].z, w[0].w));
+#pragma unroll
+    for (int i = 1; i < N; ++i) r = larger(r, larger(larger(w[i].x, w[i].y), larger(w[i].z, w[i].w)));
+    return most(r);
+  }
   static __device__ __forceinline__ void pairs(uint4 w, F2 (&p)[V / 2]) {
     if constexpr (XT == MAXDNN_F32) {
       p[0] = ((F2)w.y << 32) | w.x;
@@ -118,6 +146,8 @@ __device__ __forceinline__ float lp_one(const typename ElemOf<XT>::T* p) {
   else return __half2float(*p);
 }
 
+template <int N> struct LpCount { static constexpr int value = N; };
+
 // What a CTA shows the others of its cluster.
 struct LpShared {
   LpSums sums;
@@ -133,9 +163,10 @@ struct LpPart {
   int32_t v0, v1;                          // this CTA's vectors
   int64_t c0, c1;                          // this CTA's columns
   int64_t extra;                           // this thread's single column, or -1
+  int32_t segments, segment_vecs;          // a thread's vectors in so many segments of so many (whole batches)
 };
 
-template <int XT>
+template <int XT, int THREADS>
 __device__ __forceinline__ LpPart<XT> lp_part(const void* x, int64_t first, int64_t cols, int rank, int parts, int t) {
   typedef typename ElemOf<XT>::T T;
   constexpr int V = LpVec<XT>::V;
@@ -148,6 +179,10 @@ __device__ __forceinline__ LpPart<XT> lp_part(const void* x, int64_t first, int6
   p.v1 = (int32_t)(nv * (rank + 1) / parts);
   p.c0 = rank == 0 ? 0 : p.head + (int64_t)p.v0 * V;
   p.c1 = rank == parts - 1 ? cols : p.head + (int64_t)p.v1 * V;
+  const int batches = (p.v1 - p.v0 + THREADS * kLpBatch - 1) / (THREADS * kLpBatch);
+  const int per_segment = (batches + kLpSegments - 1) / kLpSegments;
+  p.segment_vecs = kLpBatch * per_segment;
+  p.segments = batches == 0 ? 0 : (batches + per_segment - 1) / per_segment;
   p.extra = -1;
   if (rank == 0 && t < p.head) p.extra = t;
   if (rank == parts - 1 && t >= 32 && t - 32 < tail) p.extra = cols - tail + t - 32;
@@ -163,20 +198,22 @@ __device__ __forceinline__ uint64_t lp_max_key(uint64_t k) {
   return k;
 }
 
+template <int THREADS>
 struct LpScratch {
   uint64_t keys[kLpCandidates];
+  float segment[kLpSegments][THREADS];          // maxima of the threads' segments
+  uint16_t again[kLpSegments * THREADS];        // segments that are read again
   float bounds[kLpBounds];
   float bound;
-  int32_t count;
-  int32_t per_warp[kLpThreads / 32];
-  uint64_t warp_key[kLpThreads / 32];
+  int32_t count, n_again;
+  int32_t per_warp[THREADS / 32];
+  uint64_t warp_key[THREADS / 32];
 };
 
 // The part's values that reach `bound` (STRICT: exceed it), as keys in no particular order; returns how many.
-template <int XT, bool STRICT>
-__device__ __forceinline__ int lp_collect(const LpPart<XT>& p, float mine, float bound, LpScratch* w, int t) {
-  constexpr int V = LpVec<XT>::V;
-  const int lane = t & 31, warp = t >> 5;
+template <int XT, int THREADS, bool STRICT>
+__device__ __forceinline__ int lp_collect(const LpPart<XT>& p, float mine, float bound, LpScratch<THREADS>* w, int t) {
+  constexpr int V = LpVec<XT>::V, U = 4;
   auto reaches = [&](float v) { return (STRICT ? v > bound : v >= bound) && v > -lp_inf(); };
   auto push = [&](float v, int64_t c) {
     const int at = atomicAdd(&w->count, 1);
@@ -186,21 +223,38 @@ __device__ __forceinline__ int lp_collect(const LpPart<XT>& p, float mine, float
     const float v = lp_one<XT>(p.row + p.extra);
     if (reaches(v)) push(v, p.extra);
   }
-  uint32_t flagged = __ballot_sync(0xFFFFFFFFu, reaches(mine));
-  while (flagged) {
-    const int who = warp * 32 + __ffs(flagged) - 1;
-    flagged &= flagged - 1;
+  // the segments of threads whose maximum reaches it
+  if (reaches(mine))
+    for (int s = 0; s < p.segments; ++s)
+      if (reaches(w->segment[s][t])) w->again[atomicAdd(&w->n_again, 1)] = (uint16_t)(s * THREADS + t);
+  __syncthreads();
+  // their vectors, shared by all threads, U loads of each under way
+  const int each = p.segment_vecs, all = w->n_again * each;
+  for (int i0 = t; i0 < all; i0 += THREADS * U) {
     if (*reinterpret_cast<volatile int32_t*>(&w->count) > kLpCandidates) break;      // (it will be taken another way)
-    for (int64_t v = (int64_t)p.v0 + who + (int64_t)kLpThreads * lane; v < p.v1; v += 32 * kLpThreads) {
-      const int64_t c = p.head + v * V;
-      const uint4 raw = *reinterpret_cast<const uint4*>(p.row + c);
-      F2 q[V / 2];
-      LpVec<XT>::pairs(raw, q);
+    uint4 raw[U];
+    int64_t at[U];
 #pragma unroll
-      for (int i = 0; i < V / 2; ++i) {
-        const float2 u = unf2(q[i]);
-        if (reaches(u.x)) push(u.x, c + 2 * i);
-        if (reaches(u.y)) push(u.y, c + 2 * i + 1);
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + THREADS * u;
+      at[u] = p.v1;
+      if (i < all) {
+        const int which = w->again[i / each];
+        at[u] = (int64_t)p.v0 + which % THREADS + (int64_t)THREADS * (which / THREADS * each + i % each);
+      }
+      raw[u] = at[u] < p.v1 ? *reinterpret_cast<const uint4*>(p.row + p.head + at[u] * V) : LpVec<XT>::masked();
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (!reaches(LpVec<XT>::most(raw[u]))) continue;
+      F2 q[V / 2];
+      LpVec<XT>::pairs(raw[u], q);
+      const int64_t c = p.head + at[u] * V;
+#pragma unroll
+      for (int k = 0; k < V / 2; ++k) {
+        const float2 v = unf2(q[k]);
+        if (reaches(v.x)) push(v.x, c + 2 * k);
+        if (reaches(v.y)) push(v.y, c + 2 * k + 1);
       }
     }
   }
@@ -209,17 +263,17 @@ __device__ __forceinline__ int lp_collect(const LpPart<XT>& p, float mine, float
 }
 
 // The first `need` values equal to `bound` in the order of their columns, behind `have` keys; returns how many keys there are.
-template <int XT>
-__device__ __noinline__ int lp_first_equal(const LpPart<XT>& p, float bound, int have, int need, LpScratch* w, int t) {
+template <int XT, int THREADS>
+__device__ __noinline__ int lp_first_equal(const LpPart<XT>& p, float bound, int have, int need, LpScratch<THREADS>* w, int t) {
   const int lane = t & 31, warp = t >> 5;
   int found = 0;
-  for (int64_t c = p.c0; c < p.c1 && found < need; c += kLpThreads) {
+  for (int64_t c = p.c0; c < p.c1 && found < need; c += THREADS) {
     const bool hit = c + t < p.c1 && lp_one<XT>(p.row + c + t) == bound;
     const uint32_t hits = __ballot_sync(0xFFFFFFFFu, hit);
     if (lane == 0) w->per_warp[warp] = __popc(hits);
     __syncthreads();
     int at = found, all = 0;
-    for (int i = 0; i < kLpThreads / 32; ++i) {
+    for (int i = 0; i < THREADS / 32; ++i) {
       at += i < warp ? w->per_warp[i] : 0;
       all += w->per_warp[i];
     }
@@ -232,14 +286,14 @@ __device__ __noinline__ int lp_first_equal(const LpPart<XT>& p, float bound, int
 }
 
 // The `top` largest values one after the other; returns how many there are.
-template <int XT>
-__device__ __noinline__ int lp_one_by_one(const LpPart<XT>& p, int top, LpScratch* w, int t) {
+template <int XT, int THREADS>
+__device__ __noinline__ int lp_one_by_one(const LpPart<XT>& p, int top, LpScratch<THREADS>* w, int t) {
   const int lane = t & 31, warp = t >> 5;
   uint64_t last = ~0ull;
   int n = 0;
   for (; n < top; ++n) {
     uint64_t best = 0;
-    for (int64_t c = p.c0 + t; c < p.c1; c += kLpThreads) {
+    for (int64_t c = p.c0 + t; c < p.c1; c += THREADS) {
       const float v = lp_one<XT>(p.row + c);
       const uint64_t k = v == -lp_inf() ? 0 : lp_key(v, c);
       if ((n == 0 || k < last) && k > best) best = k;
@@ -247,7 +301,7 @@ __device__ __noinline__ int lp_one_by_one(const LpPart<XT>& p, int top, LpScratc
     best = lp_max_key(best);
     if (lane == 0) w->warp_key[warp] = best;
     __syncthreads();
-    for (int i = 0; i < kLpThreads / 32; ++i) best = w->warp_key[i] > best ? w->warp_key[i] : best;
+    for (int i = 0; i < THREADS / 32; ++i) best = w->warp_key[i] > best ? w->warp_key[i] : best;
     __syncthreads();
     if (best == 0) break;
     if (t == 0) w->keys[n] = best;
@@ -258,14 +312,14 @@ __device__ __noinline__ int lp_one_by_one(const LpPart<XT>& p, int top, LpScratc
 }
 
 // The part's `top` largest values in falling order into sh->best.
-template <int XT>
-__device__ __forceinline__ void lp_largest(const LpPart<XT>& p, float mine, bool strange, int top, LpScratch* w, LpShared* sh, int t) {
-  constexpr int kEach = kLpThreads / kLpBounds;
+template <int XT, int THREADS>
+__device__ __forceinline__ void lp_largest(const LpPart<XT>& p, float mine, bool strange, int top, LpScratch<THREADS>* w, LpShared* sh, int t) {
+  constexpr int kEach = THREADS / kLpBounds;
   float m = mine;
 #pragma unroll
   for (int d = 1; d < kEach; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
   if (t % kEach == 0) w->bounds[t / kEach] = m;
-  if (t == 0) w->count = 0;
+  if (t == 0) w->count = w->n_again = 0;
   const bool nan = __syncthreads_or(strange) != 0;
   int n;
   if (!nan) {
@@ -282,41 +336,42 @@ __device__ __forceinline__ void lp_largest(const LpPart<XT>& p, float mine, bool
     }
     __syncthreads();
     const float bound = w->bound;
-    n = lp_collect<XT, false>(p, mine, bound, w, t);
+    n = lp_collect<XT, THREADS, false>(p, mine, bound, w, t);
     if (n > kLpCandidates) {
       __syncthreads();
-      if (t == 0) w->count = 0;
+      if (t == 0) w->count = w->n_again = 0;
       __syncthreads();
-      n = lp_collect<XT, true>(p, mine, bound, w, t);
-      if (n < top) n = lp_first_equal<XT>(p, bound, n, top - n, w, t);
+      n = lp_collect<XT, THREADS, true>(p, mine, bound, w, t);
+      if (n < top) n = lp_first_equal<XT, THREADS>(p, bound, n, top - n, w, t);
     }
     __syncthreads();
   }
-  if (nan || n > kLpCandidates) n = lp_one_by_one<XT>(p, top, w, t);
-  for (int i = t; i < n; i += kLpThreads) {
+  if (nan || n > kLpCandidates) n = lp_one_by_one<XT, THREADS>(p, top, w, t);
+  for (int i = t; i < n; i += THREADS) {
     const uint64_t k = w->keys[i];
     int rank = 0;
-    for (int j = 0; j < n && rank < top; ++j) rank += w->keys[j] > k;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) rank += w->keys[j] > k;
     if (rank < top) sh->best[rank] = k;
   }
   if (t == 0) sh->count = n < top ? n : top;
 }
 
-template <int XT, bool ENTROPY>
-__global__ void __launch_bounds__(kLpThreads, 4) logprob_fprop_kernel(const __grid_constant__ LogprobArgs args) {
+template <int XT, bool ENTROPY, int THREADS>
+__global__ void __launch_bounds__(THREADS, 768 / THREADS) logprob_fprop_kernel(const __grid_constant__ LogprobArgs args) {
   let_next_start();
   wait_for_previous();
-  constexpr int V = LpVec<XT>::V, U = 4;
+  constexpr int V = LpVec<XT>::V, U = kLpBatch;
   __shared__ LpShared shared;
-  __shared__ __align__(16) LpScratch scratch;
-  __shared__ LpSums per_warp[kLpThreads / 32];
+  __shared__ __align__(16) LpScratch<THREADS> scratch;
+  __shared__ LpSums per_warp[THREADS / 32];
   __shared__ uint64_t merged[kLpMaxTop];
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int rank = (int)cluster_ctarank();
   uint32_t parts;
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
   const int64_t r = blockIdx.x / parts;
-  const LpPart<XT> p = lp_part<XT>(args.x, r * args.ldx, args.cols, rank, (int)parts, t);
+  const LpPart<XT> p = lp_part<XT, THREADS>(args.x, r * args.ldx, args.cols, rank, (int)parts, t);
   const float c = args.scale * kLog2e;
   LpSums sum = {-lp_inf(), 0.f, 0.f};
   float single = -lp_inf(), given = 0.f;
@@ -327,61 +382,76 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_fprop_kernel(const __gr
     if (token >= 0) given = lp_one<XT>(p.row + token);
   }
   const uint4* vec = reinterpret_cast<const uint4*>(p.row + p.head);
-  // U vectors
-  auto take = [&](const uint4 (&raw)[U]) {
-    F2 x[U][V / 2];
-    float most = -lp_inf();
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      LpVec<XT>::pairs(raw[u], x[u]);
-#pragma unroll
-      for (int i = 0; i < V / 2; ++i) {
-        const float2 w = unf2(x[u][i]);
-        most = fmaxf(most, fmaxf(w.x, w.y));
-      }
-    }
+  // Some vectors: their maximum first
+  auto take = [&](auto& raw) {
+    constexpr int N = sizeof(raw) / sizeof(uint4);
+    const float most = LpVec<XT>::most(raw);
     if (most > sum.m) lp_raise(sum, most, c);
     if (sum.m == -lp_inf()) {      // nothing above -inf so far: a NaN still has to show
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int u = 0; u < N; ++u) {
+        F2 x[V / 2];
+        LpVec<XT>::pairs(raw[u], x);
 #pragma unroll
         for (int i = 0; i < V / 2; ++i) {
-          const float2 w = unf2(x[u][i]);
+          const float2 w = unf2(x[i]);
           if (w.x != w.x || w.y != w.y) sum.s = w.x + w.y;
         }
-      return;
+      }
+      return most;
     }
     const F2 mm = f2(-sum.m), cc = f2(c);
     F2 s = 0, tt = 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < N; ++u) {
+      F2 x[V / 2];
+      LpVec<XT>::pairs(raw[u], x);
 #pragma unroll
       for (int i = 0; i < V / 2; ++i) {
-        const F2 d = mul2(add2(x[u][i], mm), cc);
+        const F2 d = mul2(add2(x[i], mm), cc);
         const float2 w = unf2(d);
         const F2 e = f2(exp2_fast(w.x), exp2_fast(w.y));
         s = add2(s, e);
         if (ENTROPY) tt = fma2(e, f2(fmaxf(w.x, kLpFar), fmaxf(w.y, kLpFar)), tt);
       }
+    }
     sum.s += sum2(s);
     if (ENTROPY) sum.t += sum2(tt);
+    return most;
   };
+  // (a segment is several batches; its maximum is kept for the search of the largest values)
   int64_t v = (int64_t)p.v0 + t;
-  for (; v + (U - 1) * kLpThreads < p.v1; v += U * kLpThreads) {
-    uint4 raw[U];
+  for (int segment = 0; segment < p.segments; ++segment) {
+    float top_here = -lp_inf();
+#pragma unroll 1
+    for (int i = 0; i < p.segment_vecs; i += U, v += U * THREADS) {
+      const int64_t left = p.v1 - (v - t);          // vectors of the CTA
+      if (left >= U * THREADS) {
+        uint4 raw[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = load_global(vec + v + u * kLpThreads);
-    take(raw);
-  }
-  if (v < p.v1 || p.extra >= 0) {
-    uint4 raw[U];
+        for (int u = 0; u < U; ++u) raw[u] = load_global(vec + v + u * THREADS);
+        top_here = fmaxf(top_here, take(raw));
+        continue;
+      }
+      // the last ones, with no more of them masked than there are
+      auto some = [&](auto count) {
+        constexpr int N = decltype(count)::value;
+        uint4 raw[N];
 #pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = v + u * kLpThreads < p.v1 ? load_global(vec + v + u * kLpThreads) : LpVec<XT>::masked();
-    take(raw);
-    if (p.extra >= 0) {
-      const LpSums one = {single == single ? single : -lp_inf(), single != single ? single : single == -lp_inf() ? 0.f : 1.f, 0.f};
-      sum = lp_join(sum, one, c);
+        for (int u = 0; u < N; ++u) raw[u] = v + u * THREADS < p.v1 ? load_global(vec + v + u * THREADS) : LpVec<XT>::masked();
+        top_here = fmaxf(top_here, take(raw));
+      };
+      if (left > U / 2 * THREADS) some(LpCount<U>());
+      else if (left > U / 4 * THREADS) some(LpCount<U / 2>());
+      else if (left > U / 8 * THREADS) some(LpCount<U / 4>());
+      else if (left > 0) some(LpCount<U / 8>());
+      else break;
     }
+    if (args.top) scratch.segment[segment][t] = top_here;
+  }
+  if (p.extra >= 0) {
+    const LpSums one = {single == single ? single : -lp_inf(), single != single ? single : single == -lp_inf() ? 0.f : 1.f, 0.f};
+    sum = lp_join(sum, one, c);
   }
   const float mine = sum.m;
   // (+inf shows as a NaN of the sum, except where it is a thread's single value)
@@ -398,12 +468,16 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_fprop_kernel(const __gr
     sum.t += __shfl_xor_sync(0xFFFFFFFFu, sum.t, d);
   }
   if (lane == 0) per_warp[warp] = sum;
-  if (args.top) lp_largest<XT>(p, mine, strange, args.top, &scratch, &shared, t);
+  if (args.top) lp_largest<XT, THREADS>(p, mine, strange, args.top, &scratch, &shared, t);
   __syncthreads();
-  if (t == 0) {
-    LpSums all = per_warp[0];
-    for (int i = 1; i < kLpThreads / 32; ++i) all = lp_join(all, per_warp[i], c);
-    shared.sums = all;
+  if (warp == 0) {
+    LpSums all = per_warp[lane % (THREADS / 32)];
+#pragma unroll
+    for (int d = THREADS / 64; d > 0; d >>= 1) {
+      const LpSums other = {__shfl_xor_sync(0xFFFFFFFFu, all.m, d), __shfl_xor_sync(0xFFFFFFFFu, all.s, d), __shfl_xor_sync(0xFFFFFFFFu, all.t, d)};
+      all = lp_join(all, other, c);
+    }
+    if (lane == 0) shared.sums = all;
   }
   if (parts > 1) {
     cluster_arrive();      // (release and acquire: the CTAs' results are visible)
@@ -426,9 +500,9 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_fprop_kernel(const __gr
     if (args.top) {
       // candidates of all CTAs: place i is number i % top of CTA i / top
       uint64_t* keys = scratch.keys;
-      if (t < kLpMaxTop) merged[t] = 0;
-      __syncthreads();
-      for (int i = t; i < (int)parts * args.top; i += kLpThreads) {
+      if (t < kLpMaxTop) merged[t] = parts == 1 && t < shared.count ? shared.best[t] : 0;
+      if (parts > 1) __syncthreads();
+      for (int i = t; parts > 1 && i < (int)parts * args.top; i += THREADS) {
         const uint32_t who = (uint32_t)(i / args.top), in = (uint32_t)(i % args.top);
         uint32_t count;
         asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(count) : "r"(peer(&shared.count, who)) : "memory");
@@ -437,7 +511,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_fprop_kernel(const __gr
         keys[i] = k;
       }
       __syncthreads();
-      for (int i = t; i < (int)parts * args.top; i += kLpThreads) {
+      for (int i = t; parts > 1 && i < (int)parts * args.top; i += THREADS) {
         const uint64_t k = keys[i];
         if (k == 0) continue;
         int at = 0;
@@ -558,15 +632,17 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_bprop_kernel(const __gr
   }
 }
 
-// The gradient packed in 8 bits: a CTA has a tile of 128 x 128, thread t eight columns (8 (t mod 16)) of the eight rows
-// t / 16 + 16 k as 32-bit values, which serve both packed forms (and the wide one) after one reading.
+// The gradient packed in 8 bits: a CTA has a tile of 128 x 128, thread t eight columns (8 (t mod 16)) of the four rows
+// t / 16 + 32 k as 32-bit values, which serve both packed forms (and the wide one) after one reading.
+constexpr int kLpPackThreads = 512;
+constexpr int kLpPackRows = kBlock8 * (kBlock8 / 8) / kLpPackThreads, kLpPackStep = kBlock8 / kLpPackRows;
 template <int XT, int QT, bool EDGE>
-__global__ void __launch_bounds__(kLpThreads, 2) logprob_bprop_packed_kernel(const __grid_constant__ LogprobArgs args) {
+__global__ void __launch_bounds__(kLpPackThreads, 2) logprob_bprop_packed_kernel(const __grid_constant__ LogprobArgs args) {
   let_next_start();
   wait_for_previous();
   typedef typename ElemOf<XT>::T T;
   __shared__ LpRow rows[kBlock8];
-  __shared__ float col_part[kLpThreads / 32][kBlock8];   // per warp: maxima of its rows
+  __shared__ float col_part[kLpPackThreads / 32][kBlock8];   // per warp: maxima of its rows
   __shared__ float col_inv[kBlock8];
   __shared__ uint8_t row_byte[kBlock8];
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -574,23 +650,23 @@ __global__ void __launch_bounds__(kLpThreads, 2) logprob_bprop_packed_kernel(con
   const int r0 = rb * kBlock8, c0 = cb * kBlock8 + 8 * (t & 15), rg = t >> 4;
   const int n = vector_cols<EDGE>(args.cols, c0);
   const T* x = static_cast<const T*>(args.x);
-  Raw8<XT> raw[8];
+  Raw8<XT> raw[kLpPackRows];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const int r = r0 + rg + 16 * k;
+  for (int k = 0; k < kLpPackRows; ++k) {
+    const int r = r0 + rg + kLpPackStep * k;
     raw[k] = load_raw8<XT, EDGE>(x + (int64_t)r * args.ldx + c0, r < args.rows ? n : 0);
   }
   if (t < kBlock8 && r0 + t < args.rows) rows[t] = lp_row(args, r0 + t);
   __syncthreads();
-  F2 g[8][4];
-  float col_max[8], row_max[8];
+  F2 g[kLpPackRows][4];
+  float col_max[8], row_max[kLpPackRows];
 #pragma unroll
   for (int i = 0; i < 8; ++i) col_max[i] = 0.f;
   const F2 scale = f2(args.scale);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const int r = r0 + rg + 16 * k, have = r < args.rows ? n : 0;
-    const LpRow w = rows[rg + 16 * k];
+  for (int k = 0; k < kLpPackRows; ++k) {
+    const int r = r0 + rg + kLpPackStep * k, have = r < args.rows ? n : 0;
+    const LpRow w = rows[rg + kLpPackStep * k];
     const F2 ml = f2(-w.lse), a = f2(w.a), d = f2(w.d);
     to_pairs<XT>(raw[k], g[k]);
 #pragma unroll
@@ -616,13 +692,13 @@ __global__ void __launch_bounds__(kLpThreads, 2) logprob_bprop_packed_kernel(con
   }
   float most = 0.f;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) most = fmaxf(most, row_max[k]);
+  for (int k = 0; k < kLpPackRows; ++k) most = fmaxf(most, row_max[k]);
   const bool fix = __syncthreads_or(isinf(most)) != 0;   // rare: a tile that holds an infinity, which enters no scale
   if (fix) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) col_max[i] = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < kLpPackRows; ++k) {
       row_max[k] = finite_max8(g[k][0], g[k][1], g[k][2], g[k][3]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -634,7 +710,7 @@ __global__ void __launch_bounds__(kLpThreads, 2) logprob_bprop_packed_kernel(con
   }
   if (args.q_row) {
 #pragma unroll
-    for (int k = 0; k < 8; k += 2) {
+    for (int k = 0; k < kLpPackRows; k += 2) {
       uint32_t b[2];
       if (block_bytes<QT>(row_max[k], row_max[k + 1], &b[0], &b[1])) {
         b[0] = scale_byte<QT>(max_over_block_lanes(row_max[k]));
@@ -642,8 +718,8 @@ __global__ void __launch_bounds__(kLpThreads, 2) logprob_bprop_packed_kernel(con
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int r = r0 + rg + 16 * (k + i);
-        if ((t & 15) == 0) row_byte[rg + 16 * (k + i)] = (uint8_t)b[i];
+        const int r = r0 + rg + kLpPackStep * (k + i);
+        if ((t & 15) == 0) row_byte[rg + kLpPackStep * (k + i)] = (uint8_t)b[i];
         store_bytes8<EDGE>(args.q_row + (int64_t)r * args.ldq + c0, pack8<QT>(g[k + i], inv_scale_of(b[i]), fix), r < args.rows ? n : 0);
       }
     }
@@ -664,7 +740,7 @@ __global__ void __launch_bounds__(kLpThreads, 2) logprob_bprop_packed_kernel(con
   if (t < kBlock8) {
     float m = 0.f;
 #pragma unroll
-    for (int w = 0; w < kLpThreads / 32; ++w) m = fmaxf(m, col_part[w][t]);
+    for (int w = 0; w < kLpPackThreads / 32; ++w) m = fmaxf(m, col_part[w][t]);
     const uint32_t b = scale_byte<QT>(m);
     col_inv[t] = inv_scale_of(b);
     if (cb * kBlock8 + t < args.cols) args.s_col[(int64_t)rb * args.cols + cb * kBlock8 + t] = (uint8_t)b;
@@ -677,8 +753,8 @@ __global__ void __launch_bounds__(kLpThreads, 2) logprob_bprop_packed_kernel(con
     inv[i] = f2(u.x, u.y);
   }
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const int r = r0 + rg + 16 * k;
+  for (int k = 0; k < kLpPackRows; ++k) {
+    const int r = r0 + rg + kLpPackStep * k;
     store_bytes8<EDGE>(args.q_col + (int64_t)r * args.ldq + c0, pack8<QT>(g[k], inv, fix), r < args.rows ? n : 0);
   }
 }

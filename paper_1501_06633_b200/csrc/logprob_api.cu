@@ -18,10 +18,10 @@ maxdnn_status check_logprob(const maxdnn_logprob_desc* d) {
 
 bool aligned_to(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
-// CTAs that share a row: as many as fill the device (four to an SM), each with 4096 columns or more.
+// CTAs that share a row: as many as fill the device (three to an SM), each with 4096 columns or more.
 int logprob_cluster(const maxdnn_logprob_desc& d, int sm_count) {
   int c = 1;
-  while (c < kLpMaxCluster && (int64_t)d.rows * c * 2 <= (int64_t)sm_count * 4 && d.cols / (2 * c) >= 4096) c *= 2;
+  while (c < kLpMaxCluster && (int64_t)d.rows * c * 2 <= (int64_t)sm_count * 3 && d.cols / (2 * c) >= 4096) c *= 2;
   return c;
 }
 
@@ -55,7 +55,11 @@ maxdnn_status logprob_fprop(const maxdnn_logprob_desc* d, const void* x, const v
   a.scale = d->scale;
   return by_wide(d->x_type, [&](auto xt) {
     constexpr int X = decltype(xt)::value;
-    return launch_early(entropy ? logprob_fprop_kernel<X, true> : logprob_fprop_kernel<X, false>, (unsigned)(d->rows * parts), kLpThreads, 0,
+    // many rows: smaller CTAs, so that the end of one row is under way next to the readings of more others
+    if (parts == 1 && d->rows >= 6 * dev.sm_count)
+      return launch_early(entropy ? logprob_fprop_kernel<X, true, 128> : logprob_fprop_kernel<X, false, 128>, (unsigned)d->rows, 128, 0, 1,
+                          stream, a);
+    return launch_early(entropy ? logprob_fprop_kernel<X, true, 256> : logprob_fprop_kernel<X, false, 256>, (unsigned)(d->rows * parts), 256, 0,
                         parts, stream, a);
   });
 }
@@ -108,7 +112,7 @@ maxdnn_status logprob_bprop(const maxdnn_logprob_desc* d, const void* x, const v
     if (packed)
       return by_fp8(d->q_type, [&](auto qt) {
         return by_edge(d->cols % 8 == 0 && vec_ok(d->x_type, d->ldx), [&](auto edge) {
-          return launch_early(logprob_bprop_packed_kernel<X, decltype(qt)::value, decltype(edge)::value != 0>, (unsigned)grid, kLpThreads, 0, 1,
+          return launch_early(logprob_bprop_packed_kernel<X, decltype(qt)::value, decltype(edge)::value != 0>, (unsigned)grid, kLpPackThreads, 0, 1,
                               stream, a);
         });
       });

@@ -13,7 +13,7 @@
 //   X' = a X + B X                                MMA
 //
 // With one launch and two cluster barriers a step instead of three products through memory with a wait for all CTAs after each
-// (about 4 us apiece), 16 x 512 x 128 takes XX us instead of 84.
+// (about 4 us apiece), 16 x 512 x 128 takes 51 us instead of 84, 128 x 128 30 instead of 69.
 // All waits on barriers in shared memory are bounded; a wait that runs out leaves the launch's results invalid and its status says so.
 #pragma once
 #include "ortho.cuh"
@@ -41,8 +41,8 @@ struct OrthoSmallArgs {
   WaitCtx wc;
 };
 
-__device__ __forceinline__ void st_cluster_u32x2(uint32_t addr, uint32_t a, uint32_t b) {
-  asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+__device__ __forceinline__ void st_cluster_u32x4(uint32_t addr, const uint32_t (&w)[4]) {
+  asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
 }
 __device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
@@ -252,6 +252,12 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
   // start of reduction step j (16 entries) in an image of `rows` rows: along its rows, or across them
   auto along = [](uint32_t at, int rows, int j) { return make_smem_desc(at + (uint32_t)((j >> 2) * rows * 128 + (j & 3) * 32), 16384u, 1024u, 2u); };
   auto across = [](uint32_t at, int rows, int j) { return make_smem_desc(at + (uint32_t)(j * 2048), (uint32_t)rows * 128u, 1024u, 2u); };
+  // the warps whose 32 x 32 entries of A and B hold part of the diagonal, and the others
+  auto by_diagonal = [&](auto f) {
+    if (group == q) f(OrthoKindOf<1>());
+    else f(OrthoKindOf<0>());
+  };
+
   for (int step = 0; step < args.steps; ++step) {
     const float ca = args.coefficients[step][0], cb = args.coefficients[step][1], cc = args.coefficients[step][2];
     // ---- A: this CTA's part
@@ -269,21 +275,23 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
       tmem_ld_32x32(t_row + (uint32_t)(32 * group), v);
       tmem_wait_ld();
       if (parts == 1) {
+        by_diagonal([&](auto diagonal) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t w[4];
+          for (int i = 0; i < 4; ++i) {
+            uint32_t w[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float2 y = make_float2(__uint_as_float(v[8 * i + 2 * k]) * scale, __uint_as_float(v[8 * i + 2 * k + 1]) * scale);
-            const __half2 h = __floats2half2_rn(y.x, y.y);
-            w[k] = *reinterpret_cast<const uint32_t*>(&h);
-            if (group == q && 8 * i + 2 * k == (lane & ~1)) {
-              const float2 back = __half22float2(h);
-              r_a[m] = lane & 1 ? y.y - back.y : y.x - back.x;
+            for (int k = 0; k < 4; ++k) {
+              const float2 y = make_float2(__uint_as_float(v[8 * i + 2 * k]) * scale, __uint_as_float(v[8 * i + 2 * k + 1]) * scale);
+              const __half2 h = __floats2half2_rn(y.x, y.y);
+              w[k] = *reinterpret_cast<const uint32_t*>(&h);
+              if (decltype(diagonal)::value && 8 * i + 2 * k == (lane & ~1)) {
+                const float2 back = __half22float2(h);
+                r_a[m] = lane & 1 ? y.y - back.y : y.x - back.x;
+              }
             }
+            *reinterpret_cast<uint4*>(square_a + image_at(kSmallN, m, 4 * group + i)) = make_uint4(w[0], w[1], w[2], w[3]);
           }
-          *reinterpret_cast<uint4*>(square_a + image_at(kSmallN, m, 4 * group + i)) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        });
       } else {
         float* to = partial + m * kSmallPitch + 32 * group;
 #pragma unroll
@@ -295,42 +303,53 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
     if (parts > 1) {
       cluster_arrive();
       cluster_wait();
-      // its share of A's entries, four neighbours at a time and up to four of those at once: the CTAs' parts in their order
-      const int v0 = (int)(kSmallN * kSmallN / 4 * (uint32_t)rank / parts), v1 = (int)(kSmallN * kSmallN / 4 * ((uint32_t)rank + 1) / parts);
-      for (int e0 = v0 + t; e0 < v1; e0 += 4 * kSmallThreads) {
-        float4 s[4];
-        uint32_t from[4];
+      // its share of A's entries, four neighbours at a time and several of those at once: the CTAs' parts in their order
+      // (neighbouring lanes join theirs to 16 bytes, which each writes to every other CTA: shares are whole eights)
+      const int v0 = (int)(kSmallN * kSmallN / 8 * (uint32_t)rank / parts) * 2, v1 = (int)(kSmallN * kSmallN / 8 * ((uint32_t)rank + 1) / parts) * 2;
+      auto share = [&](auto at_once) {
+        constexpr int N = decltype(at_once)::value;
+        for (int e0 = v0 + t; e0 - lane < v1; e0 += N * kSmallThreads) {      // (whole warps: lanes exchange)
+          float4 s[N];
+          uint32_t from[N];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int e = min(e0 + k * kSmallThreads, v1 - 1);      // (past its share: the last one again, not written)
-          from[k] = u_partial + 4u * (uint32_t)((e >> 5) * kSmallPitch + 4 * (e & 31));
-          s[k] = ld_cluster_float4(map_to_cta(from[k], 0));
-        }
-        for (uint32_t c = 1; c < parts; ++c) {
-          float4 p[4];
+          for (int k = 0; k < N; ++k) {
+            const int e = min(e0 + k * kSmallThreads, v1 - 1);      // (past its share: the last one again, not written)
+            from[k] = u_partial + 4u * (uint32_t)((e >> 5) * kSmallPitch + 4 * (e & 31));
+            s[k] = ld_cluster_float4(map_to_cta(from[k], 0));
+          }
+#pragma unroll 2
+          for (uint32_t c = 1; c < parts; ++c) {
+            float4 p[N];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) p[k] = ld_cluster_float4(map_to_cta(from[k], c));
+            for (int k = 0; k < N; ++k) p[k] = ld_cluster_float4(map_to_cta(from[k], c));
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            s[k].x += p[k].x; s[k].y += p[k].y; s[k].z += p[k].z; s[k].w += p[k].w;
+            for (int k = 0; k < N; ++k) {
+              s[k].x += p[k].x; s[k].y += p[k].y; s[k].z += p[k].z; s[k].w += p[k].w;
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < N; ++k) {
+            const int e = e0 + k * kSmallThreads, em = e >> 5, en = 4 * (e & 31);
+            const float x0 = s[k].x * scale, x1 = s[k].y * scale, x2 = s[k].z * scale, x3 = s[k].w * scale;
+            const __half2 a = __floats2half2_rn(x0, x1), b = __floats2half2_rn(x2, x3);
+            const uint32_t wa = *reinterpret_cast<const uint32_t*>(&a), wb = *reinterpret_cast<const uint32_t*>(&b);
+            const uint32_t oa = __shfl_xor_sync(0xFFFFFFFFu, wa, 1), ob = __shfl_xor_sync(0xFFFFFFFFu, wb, 1);
+            if (e >= v1) continue;
+            const uint32_t to = u_a + image_at(kSmallN, em, en >> 3);
+            const uint32_t w[4] = {lane & 1 ? oa : wa, lane & 1 ? ob : wb, lane & 1 ? wa : oa, lane & 1 ? wb : ob};
+            for (uint32_t c = lane & 1; c < parts; c += 2) st_cluster_u32x4(map_to_cta(to, c), w);
+            if ((em & ~3) == en) {
+              const float2 fa = __half22float2(a), fb = __half22float2(b);
+              const float rest = em == en ? x0 - fa.x : em == en + 1 ? x1 - fa.y : em == en + 2 ? x2 - fb.x : x3 - fb.y;
+              for (uint32_t c = 0; c < parts; ++c) st_cluster_f32(map_to_cta(smem_u32(&r_a[em]), c), rest);
+            }
           }
         }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int e = e0 + k * kSmallThreads, em = e >> 5, en = 4 * (e & 31);
-          if (e >= v1) break;
-          const float x0 = s[k].x * scale, x1 = s[k].y * scale, x2 = s[k].z * scale, x3 = s[k].w * scale;
-          const __half2 a = __floats2half2_rn(x0, x1), b = __floats2half2_rn(x2, x3);
-          const uint32_t to = u_a + image_at(kSmallN, em, en >> 3) + (uint32_t)((en & 4) * 2);
-          for (uint32_t c = 0; c < parts; ++c)
-            st_cluster_u32x2(map_to_cta(to, c), *reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
-          if ((em & ~3) == en) {
-            const float2 fa = __half22float2(a), fb = __half22float2(b);
-            const float rest = em == en ? x0 - fa.x : em == en + 1 ? x1 - fa.y : em == en + 2 ? x2 - fb.x : x3 - fb.y;
-            for (uint32_t c = 0; c < parts; ++c) st_cluster_f32(map_to_cta(smem_u32(&r_a[em]), c), rest);
-          }
-        }
-      }
+      };
+      // (a share is 2048 fours for two CTAs, 1024 for four)
+      if (parts <= 2) share(OrthoKindOf<4>());
+      else if (parts <= 4) share(OrthoKindOf<2>());
+      else share(OrthoKindOf<1>());
       asm volatile("fence.proxy.async;" ::: "memory");      // (what went to the other CTAs is read by their MMAs)
       cluster_arrive();
       cluster_wait();
@@ -349,31 +368,34 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
       tmem_ld_32x32(t_row + (uint32_t)(32 * group), v);
       tmem_wait_ld();
       const F2 rm2 = f2(r_m), cb2 = f2(cb), cc2 = f2(cc);
+      by_diagonal([&](auto diagonal) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t at = image_at(kSmallN, m, 4 * group + i);
-        Raw8<MAXDNN_F16> raw;
-        raw.a = *reinterpret_cast<const uint4*>(square_a + at);
-        F2 a[4];
-        to_pairs<MAXDNN_F16>(raw, a);
-        uint32_t w[4];
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t at = image_at(kSmallN, m, 4 * group + i);
+          Raw8<MAXDNN_F16> raw;
+          raw.a = *reinterpret_cast<const uint4*>(square_a + at);
+          F2 a[4];
+          to_pairs<MAXDNN_F16>(raw, a);
+          uint32_t w[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const F2 r2 = *reinterpret_cast<const F2*>(&r_a[32 * group + 8 * i + 2 * k]);
-          const F2 acc = ((F2)v[8 * i + 2 * k + 1] << 32) | v[8 * i + 2 * k];
-          float2 y = unf2(fma2(cb2, a[k], mul2(cc2, fma2(add2(rm2, r2), a[k], acc))));
-          const bool mine = group == q && 8 * i + 2 * k == (lane & ~1);      // the diagonal: A_mm has r besides
-          if (mine) (lane & 1 ? y.y : y.x) += r_m * fmaf(cc, r_m, cb);
-          const __half2 h = __floats2half2_rn(y.x, y.y);
-          w[k] = *reinterpret_cast<const uint32_t*>(&h);
-          if (mine) {
-            const float2 back = __half22float2(h);
-            d_b[m] = lane & 1 ? y.y : y.x;
-            h_b[m] = lane & 1 ? back.y : back.x;
+          for (int k = 0; k < 4; ++k) {
+            const F2 r2 = *reinterpret_cast<const F2*>(&r_a[32 * group + 8 * i + 2 * k]);
+            const F2 acc = ((F2)v[8 * i + 2 * k + 1] << 32) | v[8 * i + 2 * k];
+            float2 y = unf2(fma2(cb2, a[k], mul2(cc2, fma2(add2(rm2, r2), a[k], acc))));
+            // the diagonal: A_mm has r besides, on both sides of its square too
+            const bool mine = decltype(diagonal)::value && 8 * i + 2 * k == (lane & ~1);
+            if (mine) (lane & 1 ? y.y : y.x) += r_m * fmaf(cc, r_m, cb);
+            const __half2 h = __floats2half2_rn(y.x, y.y);
+            w[k] = *reinterpret_cast<const uint32_t*>(&h);
+            if (mine) {
+              const float2 back = __half22float2(h);
+              d_b[m] = lane & 1 ? y.y : y.x;
+              h_b[m] = lane & 1 ? back.y : back.x;
+            }
           }
+          *reinterpret_cast<uint4*>(square_b + at) = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        *reinterpret_cast<uint4*>(square_b + at) = make_uint4(w[0], w[1], w[2], w[3]);
-      }
+      });
     }
     // ---- X
     product([&] {
