@@ -540,9 +540,9 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) logprob_fprop_kernel(c
 
 // ---- backward ----
 // What a row's values are turned into gradients with: g = p (a + d ln p), and `add` at the target.
-struct LpRow { float lse, a, d, add; int32_t target; };
+struct __align__(16) LpRow { float minus_lse, a, d, add; };
 
-__device__ __forceinline__ LpRow lp_row(const LogprobArgs& args, int64_t r) {
+__device__ __forceinline__ LpRow lp_row(const LogprobArgs& args, int64_t r, int32_t* target) {
   LpRow w;
   const float lse = load_global(args.lse + r);
   const int64_t at = lp_target(args, r);
@@ -551,30 +551,36 @@ __device__ __forceinline__ LpRow lp_row(const LogprobArgs& args, int64_t r) {
   const float h = args.dentropy ? load_global(args.entropy + r) : 0.f;
   // a row of which nothing is left: no p at all
   const bool nothing = lse == -lp_inf();
-  w.lse = nothing ? lp_inf() : lse;
+  w.minus_lse = nothing ? -lp_inf() : -lse;
   w.a = nothing ? 0.f : -args.scale * (dlp + dh * h);
   w.d = nothing ? 0.f : -args.scale * dh;
   w.add = nothing ? 0.f : args.scale * dlp;
-  w.target = nothing ? -1 : (int32_t)at;
+  *target = nothing ? -1 : (int32_t)at;
   return w;
 }
 
+// The larger of two values; NaN stay.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 // Gradients of a pair of logits.
 __device__ __forceinline__ F2 lp_grad2(F2 x, F2 scale, F2 minus_lse, F2 a, F2 d) {
   const float2 l = unf2(fma2(x, scale, minus_lse));
-  const F2 lnp = f2(l.x < kLpFar ? kLpFar : l.x, l.y < kLpFar ? kLpFar : l.y);      // (NaN stay)
+  const F2 lnp = f2(max_nan(l.x, kLpFar), max_nan(l.y, kLpFar));
   const float2 e = unf2(mul2(lnp, f2(kLog2e)));
   return mul2(f2(exp2_fast(e.x), exp2_fast(e.y)), fma2(d, lnp, a));
 }
 // `add` at the target among eight columns from c on.
-__device__ __forceinline__ void lp_add_target(F2 (&v)[4], const LpRow& w, int64_t c) {
-  const int64_t in = w.target - c;
-  if (w.target < 0 || in < 0 || in >= 8) return;
+__device__ __forceinline__ void lp_add_target(F2 (&v)[4], float add, int32_t target, int32_t c) {
+  const uint32_t in = (uint32_t)(target - c);
+  if (in >= 8u) return;      // (no target: -1, which is below every column)
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float2 u = unf2(v[i]);
-    if (in == 2 * i) u.x += w.add;
-    if (in == 2 * i + 1) u.y += w.add;
+    if (in == 2u * i) u.x += add;
+    if (in == 2u * i + 1u) u.y += add;
     v[i] = f2(u.x, u.y);
   }
 }
@@ -609,8 +615,9 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_bprop_kernel(const __gr
     n[i] = v < nv ? (SAME ? 8 : (int)(cols - 8 * v < 8 ? cols - 8 * v : 8)) : 0;
     raw[i] = load_raw8<XT, !SAME>(x + head + 8 * v, n[i]);
   }
-  const LpRow w = lp_row(args, r);
-  const F2 scale = f2(args.scale), ml = f2(-w.lse), a = f2(w.a), d = f2(w.d);
+  int32_t target;
+  const LpRow w = lp_row(args, r, &target);
+  const F2 scale = f2(args.scale), ml = f2(w.minus_lse), a = f2(w.a), d = f2(w.d);
 #pragma unroll
   for (int i = 0; i < kLpBackVecs; ++i) {
     const int64_t c = head + 8 * (first + i * kLpThreads);
@@ -618,7 +625,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_bprop_kernel(const __gr
     to_pairs<XT>(raw[i], g);
 #pragma unroll
     for (int k = 0; k < 4; ++k) g[k] = lp_grad2(g[k], scale, ml, a, d);
-    lp_add_target(g, w, c);
+    lp_add_target(g, w.add, target, (int32_t)c);
     store_pairs<XT, !SAME>(dx + c, g, n[i]);
   }
   if (SAME && chunk == 0) {      // single values in front and behind
@@ -626,7 +633,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_bprop_kernel(const __gr
     const int64_t c = t < head ? t : t >= 32 && t - 32 < tail ? cols - tail + t - 32 : -1;
     if (c >= 0) {
       const float v = lp_one<XT>(x + c);
-      const float g = unf2(lp_grad2(f2(v), scale, ml, a, d)).x + (c == w.target ? w.add : 0.f);
+      const float g = unf2(lp_grad2(f2(v), scale, ml, a, d)).x + (c == target ? w.add : 0.f);
       dx[c] = from_float<XT>(g);
     }
   }
@@ -642,6 +649,7 @@ __global__ void __launch_bounds__(kLpPackThreads, 2) logprob_bprop_packed_kernel
   wait_for_previous();
   typedef typename ElemOf<XT>::T T;
   __shared__ LpRow rows[kBlock8];
+  __shared__ int32_t targets[kBlock8];
   __shared__ float col_part[kLpPackThreads / 32][kBlock8];   // per warp: maxima of its rows
   __shared__ float col_inv[kBlock8];
   __shared__ uint8_t row_byte[kBlock8];
@@ -656,7 +664,11 @@ __global__ void __launch_bounds__(kLpPackThreads, 2) logprob_bprop_packed_kernel
     const int r = r0 + rg + kLpPackStep * k;
     raw[k] = load_raw8<XT, EDGE>(x + (int64_t)r * args.ldx + c0, r < args.rows ? n : 0);
   }
-  if (t < kBlock8 && r0 + t < args.rows) rows[t] = lp_row(args, r0 + t);
+  // what is behind the last row has no p and no target
+  if (t < kBlock8) {
+    if (r0 + t < args.rows) rows[t] = lp_row(args, r0 + t, &targets[t]);
+    else rows[t] = {-lp_inf(), 0.f, 0.f, 0.f}, targets[t] = -1;
+  }
   __syncthreads();
   F2 g[kLpPackRows][4];
   float col_max[8], row_max[kLpPackRows];
@@ -664,31 +676,33 @@ __global__ void __launch_bounds__(kLpPackThreads, 2) logprob_bprop_packed_kernel
   for (int i = 0; i < 8; ++i) col_max[i] = 0.f;
   const F2 scale = f2(args.scale);
 #pragma unroll
-  for (int k = 0; k < kLpPackRows; ++k) {
-    const int r = r0 + rg + kLpPackStep * k, have = r < args.rows ? n : 0;
-    const LpRow w = rows[rg + kLpPackStep * k];
-    const F2 ml = f2(-w.lse), a = f2(w.a), d = f2(w.d);
-    to_pairs<XT>(raw[k], g[k]);
+  for (int k = 0; k < kLpPackRows; k += 2) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      g[k][i] = lp_grad2(g[k][i], scale, ml, a, d);
-      // what is not in the matrix takes no part in the maxima
-      if (EDGE) {
-        const float2 u = unf2(g[k][i]);
-        g[k][i] = f2(2 * i < have ? u.x : 0.f, 2 * i + 1 < have ? u.y : 0.f);
-      } else if (have == 0) {
-        g[k][i] = 0;
+    for (int h = 0; h < 2; ++h) {
+      const int in = rg + kLpPackStep * (k + h), r = r0 + in, have = r < args.rows ? n : 0;
+      const LpRow w = rows[in];
+      // (columns behind the last one: no p either, so that they take no part in the maxima)
+      const F2 ml = f2(n > 0 ? w.minus_lse : -lp_inf()), a = f2(w.a), d = f2(w.d);
+      F2 (&v)[4] = g[k + h];
+      to_pairs<XT>(raw[k + h], v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[i] = lp_grad2(v[i], scale, ml, a, d);
+        if (EDGE) {
+          const float2 u = unf2(v[i]);
+          v[i] = f2(2 * i < have ? u.x : 0.f, 2 * i + 1 < have ? u.y : 0.f);
+        }
       }
+      lp_add_target(v, w.add, targets[in], c0);
+      row_max[k + h] = max8(v);
+      if (args.dx) store_pairs<XT, true>(static_cast<T*>(args.dx) + (int64_t)r * args.ldd + c0, v, have);
     }
-    if (have > 0) lp_add_target(g[k], w, c0);
-    row_max[k] = max8(g[k]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float2 u = unf2(g[k][i]);
-      col_max[2 * i] = max3abs(col_max[2 * i], u.x, 0.f);
-      col_max[2 * i + 1] = max3abs(col_max[2 * i + 1], u.y, 0.f);
+      const float2 u = unf2(g[k][i]), w = unf2(g[k + 1][i]);
+      col_max[2 * i] = max3abs(col_max[2 * i], u.x, w.x);
+      col_max[2 * i + 1] = max3abs(col_max[2 * i + 1], u.y, w.y);
     }
-    if (args.dx) store_pairs<XT, true>(static_cast<T*>(args.dx) + (int64_t)r * args.ldd + c0, g[k], have);
   }
   float most = 0.f;
 #pragma unroll
@@ -708,55 +722,61 @@ __global__ void __launch_bounds__(kLpPackThreads, 2) logprob_bprop_packed_kernel
       }
     }
   }
-  if (args.q_row) {
+  // (both ways apart: the test in every conversion costs a tenth of the kernel's instructions)
+  auto pack = [&](auto fixes) {
+    constexpr bool FIX = decltype(fixes)::value != 0;
+    if (args.q_row) {
 #pragma unroll
-    for (int k = 0; k < kLpPackRows; k += 2) {
-      uint32_t b[2];
-      if (block_bytes<QT>(row_max[k], row_max[k + 1], &b[0], &b[1])) {
-        b[0] = scale_byte<QT>(max_over_block_lanes(row_max[k]));
-        b[1] = scale_byte<QT>(max_over_block_lanes(row_max[k + 1]));
-      }
+      for (int k = 0; k < kLpPackRows; k += 2) {
+        uint32_t b[2];
+        if (block_bytes<QT>(row_max[k], row_max[k + 1], &b[0], &b[1])) {
+          b[0] = scale_byte<QT>(max_over_block_lanes(row_max[k]));
+          b[1] = scale_byte<QT>(max_over_block_lanes(row_max[k + 1]));
+        }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int r = r0 + rg + kLpPackStep * (k + i);
-        if ((t & 15) == 0) row_byte[rg + kLpPackStep * (k + i)] = (uint8_t)b[i];
-        store_bytes8<EDGE>(args.q_row + (int64_t)r * args.ldq + c0, pack8<QT>(g[k + i], inv_scale_of(b[i]), fix), r < args.rows ? n : 0);
+        for (int i = 0; i < 2; ++i) {
+          const int r = r0 + rg + kLpPackStep * (k + i);
+          if ((t & 15) == 0) row_byte[rg + kLpPackStep * (k + i)] = (uint8_t)b[i];
+          store_bytes8<EDGE>(args.q_row + (int64_t)r * args.ldq + c0, pack8<QT>(g[k + i], inv_scale_of(b[i]), FIX), r < args.rows ? n : 0);
+        }
       }
     }
-  }
-  if (args.q_col) {
+    if (args.q_col) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) col_max[i] = fmaxf(col_max[i], __shfl_xor_sync(0xFFFFFFFFu, col_max[i], 16));
-    if (lane < 16) {
+      for (int i = 0; i < 8; ++i) col_max[i] = fmaxf(col_max[i], __shfl_xor_sync(0xFFFFFFFFu, col_max[i], 16));
+      if (lane < 16) {
 #pragma unroll
-      for (int i = 0; i < 8; i += 4)
-        *reinterpret_cast<float4*>(&col_part[warp][8 * lane + i]) =
-            make_float4(col_max[i], col_max[i + 1], col_max[i + 2], col_max[i + 3]);
+        for (int i = 0; i < 8; i += 4)
+          *reinterpret_cast<float4*>(&col_part[warp][8 * lane + i]) =
+              make_float4(col_max[i], col_max[i + 1], col_max[i + 2], col_max[i + 3]);
+      }
     }
-  }
-  __syncthreads();
-  if (args.q_row && t < kBlock8 && r0 + t < args.rows) args.s_row[(int64_t)cb * args.rows + r0 + t] = row_byte[t];
-  if (!args.q_col) return;
-  if (t < kBlock8) {
-    float m = 0.f;
+    __syncthreads();
+    if (args.q_row && t < kBlock8 && r0 + t < args.rows) args.s_row[(int64_t)cb * args.rows + r0 + t] = row_byte[t];
+    if (!args.q_col) return;
+    if (t < kBlock8) {
+      float m = 0.f;
 #pragma unroll
-    for (int w = 0; w < kLpPackThreads / 32; ++w) m = fmaxf(m, col_part[w][t]);
-    const uint32_t b = scale_byte<QT>(m);
-    col_inv[t] = inv_scale_of(b);
-    if (cb * kBlock8 + t < args.cols) args.s_col[(int64_t)rb * args.cols + cb * kBlock8 + t] = (uint8_t)b;
-  }
-  __syncthreads();
-  F2 inv[4];
+      for (int w = 0; w < kLpPackThreads / 32; ++w) m = fmaxf(m, col_part[w][t]);
+      const uint32_t b = scale_byte<QT>(m);
+      col_inv[t] = inv_scale_of(b);
+      if (cb * kBlock8 + t < args.cols) args.s_col[(int64_t)rb * args.cols + cb * kBlock8 + t] = (uint8_t)b;
+    }
+    __syncthreads();
+    F2 inv[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 u = *reinterpret_cast<const float2*>(&col_inv[8 * (t & 15) + 2 * i]);
-    inv[i] = f2(u.x, u.y);
-  }
+    for (int i = 0; i < 4; ++i) {
+      const float2 u = *reinterpret_cast<const float2*>(&col_inv[8 * (t & 15) + 2 * i]);
+      inv[i] = f2(u.x, u.y);
+    }
 #pragma unroll
-  for (int k = 0; k < kLpPackRows; ++k) {
-    const int r = r0 + rg + kLpPackStep * k;
-    store_bytes8<EDGE>(args.q_col + (int64_t)r * args.ldq + c0, pack8<QT>(g[k], inv, fix), r < args.rows ? n : 0);
-  }
+    for (int k = 0; k < kLpPackRows; ++k) {
+      const int r = r0 + rg + kLpPackStep * k;
+      store_bytes8<EDGE>(args.q_col + (int64_t)r * args.ldq + c0, pack8<QT>(g[k], inv, FIX), r < args.rows ? n : 0);
+    }
+  };
+  if (fix) pack(LpCount<1>());
+  else pack(LpCount<0>());
 }
 
 }  // namespace maxdnn

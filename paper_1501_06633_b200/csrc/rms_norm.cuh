@@ -10,10 +10,14 @@
 // row's alignment (the copy starts at the 16 bytes that hold the row's first value), so a row's loads cost no
 // registers and no issue slots while the row before is packed.  The exchange of the row's one sum is also what
 // tells that a stage has been read.  Few rows are read directly: a ring would only add its start.
+// Rows that do not start at multiples of 16 bytes are shifted on their way from the stage to registers, and results go back
+// into the stage as they will lie in memory, from where a bulk copy stores the row's whole 16-byte units (16-byte vectors in
+// pieces of 2 and 4 bytes would be five times the stores; 1531 x 2309 backward 17.0 -> XX us).
 // Sums are in 32 bits; sixteen neighbouring lanes hold a block of 128 columns, so packing takes four shuffles
 // for two blocks.
 #pragma once
 #include "layer_norm.cuh"
+#include "umma_util.cuh"
 
 namespace maxdnn {
 
@@ -48,6 +52,12 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
+// The 16 bytes that start `s` bytes (a multiple of 2, the same for a whole row) into 32.
+__device__ __forceinline__ uint4 shifted16(uint4 lo, uint4 hi, uint32_t s) {
+  if (s == 0) return lo;
+  return words_at(lo, hi, s);
+}
+
 // One input of a ring stage: the units around `cols` values at `row`.
 struct RmsRow {
   const void* from;
@@ -60,6 +70,40 @@ __device__ __forceinline__ RmsRow rms_row(const void* base, int64_t first, int c
   r.from = reinterpret_cast<const void*>(at - r.shift);
   r.bytes = (r.shift + (uint32_t)cols * (uint32_t)elem + 15u) & ~15u;
   return r;
+}
+
+// Eight values of a row in a stage: `at` is the first one's place.  Whole vectors without the masks that a row's end needs.
+template <int DT, bool EDGE>
+__device__ __forceinline__ Raw8<DT> stage_raw8(const uint8_t* at, int n) {
+  typedef typename ElemOf<DT>::T T;
+  if constexpr (EDGE && !is_fp8(DT)) {
+    if (n == 8) {
+      const uint32_t s = (uint32_t)(reinterpret_cast<uintptr_t>(at) & 15u);
+      const uint4* q = reinterpret_cast<const uint4*>(at - s);
+      Raw8<DT> r = {};
+      const uint4 c0 = q[0], c1 = q[1];
+      r.a = shifted16(c0, c1, s);
+      if constexpr (DT == MAXDNN_F32) r.b = shifted16(c1, s ? q[2] : c1, s);
+      return r;
+    }
+  }
+  return load_raw8<DT, EDGE>(reinterpret_cast<const T*>(at), n);
+}
+
+// A row that the group's threads have written into a stage as it will lie in memory (`shift` bytes into the units at `from`, all
+// of them behind a fence and a barrier): whole units by one bulk copy, which thread 0 has to wait for, and single values in
+// front and behind by the group's first threads.
+template <class T>
+__device__ __forceinline__ void store_staged(T* row, const uint8_t* from, uint32_t shift, int cols, int t) {
+  const uint32_t end = shift + (uint32_t)cols * (uint32_t)sizeof(T), u0 = (shift + 15u) & ~15u, u1 = end & ~15u;
+  uint8_t* to = reinterpret_cast<uint8_t*>(row) - shift;
+  if (t == 0 && u1 > u0) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to + u0), "r"(smem_u32(from) + u0), "r"(u1 - u0)
+                 : "memory");
+  }
+  const uint32_t front = (u1 > u0 ? u0 : end), back = u1 > u0 ? u1 : end;      // (a row inside one unit: all of it in front)
+  const uint32_t at = t < 8 ? shift + t * (uint32_t)sizeof(T) : back + (t - 8) * (uint32_t)sizeof(T);
+  if (t < 16 && at < (t < 8 ? front : end)) *reinterpret_cast<T*>(to + at) = *reinterpret_cast<const T*>(from + at);
 }
 
 // Sum over the WR warps of a row's group.
@@ -78,11 +122,20 @@ __device__ __forceinline__ float rms_total(float v, float (&slots)[2][WR], int f
   return v;
 }
 
+// All threads of a row's group, and what they wrote for the copy engine.
+template <int WR>
+__device__ __forceinline__ void rms_group_barrier(int group) {
+  fence_proxy_async_smem();
+  if constexpr (WR > 1) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(WR * 32) : "memory");
+  else __syncwarp();
+}
+
 template <int XT, int WR, bool EDGE, bool RING>
 __global__ void __launch_bounds__(rms_threads(WR), WR > 8 ? 1 : 3)
 rms_norm_fprop_kernel(const __grid_constant__ RmsNormArgs args) {
   typedef typename ElemOf<XT>::T T;
   constexpr int kGroups = rms_groups(WR), kStep = 256 * WR;      // columns from a thread's first vector to its second
+  constexpr bool kStaged = EDGE && RING;
   __shared__ float slots[kGroups][2][WR];
   __shared__ __align__(8) uint64_t full[kGroups][kRmsMaxDepth];
   extern __shared__ __align__(16) uint8_t ring[];
@@ -113,6 +166,9 @@ rms_norm_fprop_kernel(const __grid_constant__ RmsNormArgs args) {
   };
   if (RING && t == 0)
     for (int d = 0; d < args.depth; ++d) fetch(first + d * step, d);
+  // whole warps without a second vector leave its work out, where that work is long or a row has many warps (elsewhere the
+  // test costs more: 4096 x 8192 packed 38 -> 41 us)
+  const bool second = !(EDGE || WR > 16) || 256 * in_row + kStep < args.cols;
   int n[2];
   F2 g[2][4];
 #pragma unroll
@@ -126,15 +182,18 @@ rms_norm_fprop_kernel(const __grid_constant__ RmsNormArgs args) {
   bool ok = true;
   for (int64_t r = first; r < args.rows; r += step, flip ^= 1) {
     Raw8<XT> rx[2], rr[2];
+    uint8_t* at_x = mine + (size_t)slot * stage;
+    const uint32_t sr = (uint32_t)((uintptr_t)(r * args.ldr) * sizeof(T)) & 15u;
     if constexpr (RING) {
       // (a wait that ran out ends the launch's other waits too; its rows are then not valid)
       ok &= mbar_wait(bars + 8u * slot, phase, args.wc, kDevTimeoutFull);
-      const uint32_t sx = (uint32_t)((uintptr_t)(r * args.ldx) * sizeof(T)) & 15u, sr = (uint32_t)((uintptr_t)(r * args.ldr) * sizeof(T)) & 15u;
-      const uint8_t* at = mine + (size_t)slot * stage;
+      const uint32_t sx = (uint32_t)((uintptr_t)(r * args.ldx) * sizeof(T)) & 15u;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        rx[j] = load_raw8<XT, EDGE>(reinterpret_cast<const T*>(at + (EDGE ? sx : 0u)) + 8 * t + kStep * j, n[j]);
-        if (res) rr[j] = load_raw8<XT, EDGE>(reinterpret_cast<const T*>(at + part + (EDGE ? sr : 0u)) + 8 * t + kStep * j, n[j]);
+        if (j == 1 && !second) break;
+        const uint32_t in = (uint32_t)(8 * t + kStep * j) * (uint32_t)sizeof(T);
+        rx[j] = stage_raw8<XT, EDGE>(at_x + (EDGE ? sx : 0u) + in, n[j]);
+        if (res) rr[j] = stage_raw8<XT, EDGE>(at_x + part + (EDGE ? sr : 0u) + in, n[j]);
       }
     } else {
 #pragma unroll
@@ -143,9 +202,10 @@ rms_norm_fprop_kernel(const __grid_constant__ RmsNormArgs args) {
         if (res) rr[j] = load_raw8<XT, EDGE>(res + r * args.ldr + 8 * t + kStep * j, n[j]);
       }
     }
-    F2 h[2][4], sq = 0;
+    F2 h[2][4] = {}, sq = 0;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
+      if (j == 1 && !second) break;
       to_pairs<XT>(rx[j], h[j]);
       if (res) {
         F2 b[4];
@@ -157,41 +217,62 @@ rms_norm_fprop_kernel(const __grid_constant__ RmsNormArgs args) {
       for (int i = 0; i < 4; ++i) sq = fma2(h[j][i], h[j][i], sq);
     }
     const float rstd = 1.f / sqrtf(rms_total<WR>(sum2(sq), slots[group], flip, group, lane, in_row) * args.inv_cols + args.eps);
-    if constexpr (RING) {
-      // every thread of the group has read this stage: the sum above needed its values
+    // every thread of the group has read this stage: the sum above needed its values
+    if (RING && !kStaged) {
       if (t == 0) fetch(r + args.depth * step, slot);
       if (++slot == args.depth) { slot = 0; phase ^= 1u; }
     }
     if (t == 0 && args.rstd) args.rstd[r] = rstd;
     if (args.sum) {
+      // (where there is a residual, its place in the stage is the sum's)
+      T* to = kStaged && res ? reinterpret_cast<T*>(at_x + part + sr) : static_cast<T*>(args.sum) + r * args.ldr;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) store_pairs<XT, EDGE>(static_cast<T*>(args.sum) + r * args.ldr + 8 * t + kStep * j, h[j], n[j]);
+      for (int j = 0; j < 2; ++j)
+        if (j == 0 || second) store_pairs<XT, EDGE>(to + 8 * t + kStep * j, h[j], n[j]);
     }
+    const uint32_t sy = (uint32_t)((uintptr_t)(r * args.ldy) * sizeof(T)) & 15u;
     const int64_t at = r * args.ldq + 8 * t, scale_at = (int64_t)(t >> 4) * args.rows + r, scale_step = (int64_t)(kStep / kBlock8) * args.rows;
     if (args.c)
       norm_pack<kEitherFp8, EDGE>(h[0], h[1], args.q_e5m2, args.c + at, args.c + at + kStep, args.sc + scale_at, args.sc + scale_at + scale_step,
                                   n[0], n[1], lane);
-    if (!args.y && !args.q) continue;
-    const F2 rs = f2(rstd);
+    if (!kStaged && !args.y && !args.q) continue;
+    if (!kStaged || args.y || args.q) {
+      const F2 rs = f2(rstd);
+      T* to = kStaged ? reinterpret_cast<T*>(at_x + sy) : static_cast<T*>(args.y) + r * args.ldy;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < 2; ++j) {
+        if (j == 1 && !second) break;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        h[j][i] = mul2(mul2(h[j][i], rs), g[j][i]);
-        // columns past the end take part in the block's maximum: zeros (0 x infinity is none)
-        if (EDGE) {
-          const float2 u = unf2(h[j][i]);
-          h[j][i] = f2(2 * i < n[j] ? u.x : 0.f, 2 * i + 1 < n[j] ? u.y : 0.f);
-        } else if (n[j] == 0) {
-          h[j][i] = 0;
+        for (int i = 0; i < 4; ++i) {
+          h[j][i] = mul2(mul2(h[j][i], rs), g[j][i]);
+          // columns past the end take part in the block's maximum: zeros (0 x infinity is none)
+          if (EDGE) {
+            const float2 u = unf2(h[j][i]);
+            h[j][i] = f2(2 * i < n[j] ? u.x : 0.f, 2 * i + 1 < n[j] ? u.y : 0.f);
+          } else if (n[j] == 0) {
+            h[j][i] = 0;
+          }
         }
+        if (args.y) store_pairs<XT, EDGE>(to + 8 * t + kStep * j, h[j], n[j]);
       }
-      if (args.y) store_pairs<XT, EDGE>(static_cast<T*>(args.y) + r * args.ldy + 8 * t + kStep * j, h[j], n[j]);
+      if (args.q)
+        norm_pack<kEitherFp8, EDGE>(h[0], h[1], args.q_e5m2, args.q + at, args.q + at + kStep, args.s + scale_at, args.s + scale_at + scale_step,
+                                    n[0], n[1], lane);
     }
-    if (args.q)
-      norm_pack<kEitherFp8, EDGE>(h[0], h[1], args.q_e5m2, args.q + at, args.q + at + kStep, args.s + scale_at, args.s + scale_at + scale_step,
-                                  n[0], n[1], lane);
+    if constexpr (kStaged) {
+      rms_group_barrier<WR>(group);
+      if (args.sum && res) store_staged(static_cast<T*>(args.sum) + r * args.ldr, at_x + part, sr, args.cols, t);
+      if (args.y) store_staged(static_cast<T*>(args.y) + r * args.ldy, at_x, sy, args.cols, t);
+      if (t == 0) {
+        // this row's copies may still be read; the row's before have been: its stage takes the next row
+        bulk_commit();
+        bulk_wait_read<1>();
+        if (r > first) fetch(r - step + args.depth * step, slot == 0 ? args.depth - 1 : slot - 1);
+      }
+      if (++slot == args.depth) { slot = 0; phase ^= 1u; }
+    }
   }
+  if (kStaged && t == 0) bulk_wait_all();
   if (RING && !ok && t == 0)      // leaving early: give copies already issued time to land
     for (int i = 0; i < args.depth; ++i) mbar_wait_grace(bars + 8u * i, i < slot ? phase ^ 1u : phase);
 }
@@ -263,6 +344,9 @@ rms_norm_bprop_kernel(const __grid_constant__ RmsNormArgs args) {
   typedef typename ElemOf<YT>::T TY;
   constexpr int kGroups = rms_groups(WR), kStep = 256 * WR;
   constexpr bool kAgain = WR > 16;
+  // dx goes through dy's place in the stage (not where dy is read again for it: other threads' shifted vectors overlap it)
+  constexpr int kStagedAt = EDGE && !kAgain ? 1 : 0;
+  const bool second = !(EDGE || WR > 16) || 256 * (int)((threadIdx.x >> 5) % WR) + kStep < args.cols;      // (see above)
   __shared__ float slots[kGroups][2][WR];
   __shared__ __align__(8) uint64_t full[kGroups][kRmsMaxDepth];
   __shared__ float fold[kGroups > 1 ? 512 * WR : 1];
@@ -335,20 +419,23 @@ rms_norm_bprop_kernel(const __grid_constant__ RmsNormArgs args) {
     const uint32_t sd = EDGE ? (uint32_t)((uintptr_t)(r * args.ldr) * sizeof(TY)) & 15u : 0u;
     // hh and dy of eight columns
     auto values = [&](int j, F2 (&hh)[4], F2 (&e)[4]) {
-      to_pairs<XT>(load_raw8<XT, EDGE>(reinterpret_cast<const TX*>(at + sx) + 8 * t + kStep * j, n[j]), hh);
-      to_pairs<YT>(load_raw8<YT, EDGE>(reinterpret_cast<const TY*>(at + part_x + sy) + 8 * t + kStep * j, n[j]), e);
+      const uint32_t in = (uint32_t)(8 * t + kStep * j);
+      to_pairs<XT>(stage_raw8<XT, EDGE>(at + sx + in * (uint32_t)sizeof(TX), n[j]), hh);
+      to_pairs<YT>(stage_raw8<YT, EDGE>(at + part_x + sy + in * (uint32_t)sizeof(TY), n[j]), e);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         hh[i] = mul2(hh[i], k[j]);
         if (is_fp8(XT)) hh[i] = mul2(hh[i], f2(rstd));
       }
     };
+    const uint8_t* at_sums = at + part_x + part_y + sd;
     F2 hh[2][4], e[2][4], part = 0;
     Raw8<YT> rd[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
+      if (j == 1 && !second) break;
       values(j, hh[j], e[j]);
-      if (!kAgain && ds) rd[j] = load_raw8<YT, EDGE>(reinterpret_cast<const TY*>(at + part_x + part_y + sd) + 8 * t + kStep * j, n[j]);
+      if (!kAgain && ds) rd[j] = stage_raw8<YT, EDGE>(at_sums + (uint32_t)(8 * t + kStep * j) * (uint32_t)sizeof(TY), n[j]);
       if (n[j] > 0) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -359,13 +446,14 @@ rms_norm_bprop_kernel(const __grid_constant__ RmsNormArgs args) {
       }
     }
     const float s = rms_total<WR>(sum2(part), slots[group], flip, group, lane, in_row) * args.inv_cols;
-    if (!kAgain && t == 0) fetch(r + args.depth, slot);
+    if (!EDGE && !kAgain && t == 0) fetch(r + args.depth, slot);
     const F2 rs = f2(rstd), ms = f2(-s * rstd);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
+      if (j == 1 && !second) break;
       if (kAgain) {
         values(j, hh[j], e[j]);
-        if (ds) rd[j] = load_raw8<YT, EDGE>(reinterpret_cast<const TY*>(at + part_x + part_y + sd) + 8 * t + kStep * j, n[j]);
+        if (ds) rd[j] = stage_raw8<YT, EDGE>(at_sums + (uint32_t)(8 * t + kStep * j) * (uint32_t)sizeof(TY), n[j]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) e[j][i] = mul2(e[j][i], g[j][i]);
       }
@@ -378,14 +466,26 @@ rms_norm_bprop_kernel(const __grid_constant__ RmsNormArgs args) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = fma2(hh[j][i], ms, mul2(e[j][i], rs));
       }
-      store_pairs<YT, EDGE>(static_cast<TY*>(args.dx) + r * args.ldy + 8 * t + kStep * j, o, n[j]);
+      if (kStagedAt == 0) store_pairs<YT, EDGE>(static_cast<TY*>(args.dx) + r * args.ldy + 8 * t + kStep * j, o, n[j]);
+      else store_pairs<YT, EDGE>(reinterpret_cast<TY*>(mine + (size_t)slot * stage + part_x + sy) + 8 * t + kStep * j, o, n[j]);
     }
-    if (kAgain) {
-      __syncthreads();
+    if (kStagedAt != 0) {
+      rms_group_barrier<WR>(group);
+      store_staged(static_cast<TY*>(args.dx) + r * args.ldy, at + part_x, sy, args.cols, t);
+      if (t == 0) {
+        // this row's copy may still be read; the row's before has been: its stage takes the next row
+        bulk_commit();
+        bulk_wait_read<1>();
+        if (r > r0) fetch(r - 1 + args.depth, slot == 0 ? args.depth - 1 : slot - 1);
+      }
+    } else if (EDGE || kAgain) {
+      if (WR > 1) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(WR * 32) : "memory");
+      else __syncwarp();
       if (t == 0) fetch(r + args.depth, slot);
     }
     if (++slot == args.depth) { slot = 0; phase ^= 1u; }
   }
+  if (kStagedAt != 0 && t == 0) bulk_wait_all();
   if (!ok && t == 0)
     for (int i = 0; i < args.depth; ++i) mbar_wait_grace(bars + 8u * i, i < slot ? phase ^ 1u : phase);
   if (!args.partial) return;
@@ -476,7 +576,7 @@ __global__ void __launch_bounds__(1024) rms_norm_bprop_long_kernel(const __grid_
 }
 
 // dg from the CTAs' sums, in CTA order.  A CTA takes 32 columns; each of its 16 warps takes every sixteenth sum, four at a
-// time, and the warps' results are added in warp order.
+// time, and the warps' results are added in warp order.  (Eight at a time behind tests of the end: 3 us more; 32 warps: 1 us more.)
 __global__ void __launch_bounds__(512) rms_norm_fold_kernel(const float* partial, int parts, int cols, float* dgamma) {
   let_next_start();
   wait_for_previous();
