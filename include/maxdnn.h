@@ -626,7 +626,7 @@ maxdnn_status maxdnn_rms_norm_bprop(const maxdnn_rms_norm_desc* desc, const void
  * both [rows][top]; a place for which no logit above -inf is left holds -inf and index -1.  A NaN counts as
  * larger than every number.  A row without any logit above -inf (all masked) has lse = -inf, logprob = -inf
  * (0 without a token), entropy = 0 and a gradient of zeros.  A row with a NaN or +inf has lse, logprob, entropy and
- * top_logprob NaN.  scale: positive and finite.  NOT_SUPPORTED: top above 32, more than 2^30 columns.
+ * top_logprob NaN.  scale: positive and finite.  NOT_SUPPORTED: top above 32, more than 2^30 rows or columns.
  */
 typedef enum maxdnn_index { MAXDNN_INDEX_I32 = 0, MAXDNN_INDEX_I64 = 1 } maxdnn_index;
 
@@ -663,7 +663,8 @@ maxdnn_status maxdnn_logprob_bprop(const maxdnn_logprob_desc* desc, const void* 
  * of the polynomial in 32, so that the result is about 1e-3 (of its norm) from the formula's, whatever the spectrum: less
  * than its rounding to BF16, and whatever the size of G, also far below eps.  A matrix of zeros gives zeros (with eps > 0), one with a NaN or infinity gives NaN.  The coefficients
  * have to keep every singular value of X below 10 (the default ones: below 1.3).  workspace: 16-byte
- * aligned, its contents do not matter.  NOT_SUPPORTED: rows or cols above 65536, steps above 32.
+ * aligned, its contents do not matter, for one call at a time.  The CTAs of a call may wait for one another (a cooperative
+ * launch).  NOT_SUPPORTED: rows, cols or batch above 65536, steps above 32.
  */
 typedef struct maxdnn_ortho_desc {
   int32_t batch, rows, cols, steps;

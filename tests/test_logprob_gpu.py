@@ -104,6 +104,29 @@ def test_alternatives_where_values_are_equal_or_masked(rows, cols, kind):
         check(x, kind, 1.0, target, 3)
 
 
+@pytest.mark.parametrize("rows,threads", [(300, 256), (900, 128)])
+def test_alternatives_of_long_rows_whose_large_values_lie_close_together(rows, threads):
+    """More values above the bound than there is room for, in fewer threads than alternatives: the rows' large values lie at one
+    place of the threads' stride; in others all values but a few are equal."""
+    cols = 150000
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    x = torch.randn(rows, cols, device="cuda", generator=gen).to(torch.bfloat16)
+    n = np.arange(cols)
+    rng = np.random.default_rng(4)
+    special = {0: np.where((n // 8) % threads < 4, 20 + 10 * rng.random(cols), -rng.random(cols)),
+               7: np.where((n // 8) % threads < 8, 20 + n * 1e-4, 0.0), rows - 1: np.where(n % 50021 == 3, 5.0, -7.0)}
+    for r, v in special.items():
+        x[r] = torch.from_numpy(as_held(v[None], "bf16")[0]).to(torch.bfloat16).cuda()
+    for top in (3, 32):
+        v, at = torch.empty(rows, top, device="cuda"), torch.empty(rows, top, dtype=torch.int32, device="cuda")
+        lse = torch.empty(rows, device="cuda")
+        mx.logprob_fprop(mx.LogprobDesc.make(rows, cols, top=top), x, lse=lse, top_logprob=v, top_index=at)
+        some = [*special, 1, rows // 2]
+        want, _, _, tlp, idx, a1, _ = ref.forward(down(x[some]), 1.0, np.full(len(some), -1), top)
+        np.testing.assert_array_equal(at[some].cpu().numpy(), idx)
+        close(down(v[some]), tlp, (2.0 ** -17 + 2.0 ** -22 * a1)[:, None] + 4 * U * np.abs(tlp))
+
+
 @pytest.mark.parametrize("cols", [300, 9000, 70000])
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
 def test_rows_that_are_not_finite(cols, kind):

@@ -69,7 +69,8 @@ BWD = (P, P, P, P, P, P, 2 * P, P, P, P, P, None)          # x target lse dlogpr
 @pytest.mark.parametrize("fields,status", [
     (dict(rows=-1), INVALID), (dict(cols=0), INVALID), (dict(ldx=99), INVALID), (dict(x_type=mx.DTYPE_E4M3), INVALID), (dict(top=-1), INVALID),
     (dict(top=33), UNSUPPORTED), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=float("inf")), INVALID),
-    (dict(scale=float("nan")), INVALID), (dict(target_type=2), INVALID), (dict(cols=MOST, ldx=MOST, ldd=MOST, ldq=2 ** 31), UNSUPPORTED)])
+    (dict(scale=float("nan")), INVALID), (dict(target_type=2), INVALID), (dict(cols=MOST, ldx=MOST, ldd=MOST, ldq=2 ** 31), UNSUPPORTED),
+    (dict(rows=MOST), UNSUPPORTED), (dict(rows=2 ** 30 + 1), UNSUPPORTED)])
 def test_logprob_refusals(fields, status):
     assert call("logprob_fprop", changed(mx.LogprobDesc.make(10, 100, top=3), **fields), *FWD) == status
     assert call("logprob_bprop", changed(mx.LogprobDesc.make(10, 100, top=3), **fields), *BWD) == status
@@ -92,7 +93,6 @@ def test_logprob_missing_and_misaligned():
     assert call("logprob_bprop", d, P, P, P, None, P, None, P, *[None] * 5) == INVALID       # no gradient given
     assert call("logprob_bprop", d, P, P, P, P, P, P, None, *[None] * 5) == INVALID          # nothing asked for
     assert call("logprob_bprop", mx.LogprobDesc.make(10, 100, ldd=112), P, P, P, P, P, P, P, *[None] * 5) == INVALID   # in place, other pitch
-    assert call("logprob_fprop", mx.LogprobDesc.make(2 ** 29, 40000), P, None, None, P, None, None, None, None) != mx.OK
 
 
 def test_no_rows_and_null_descriptors():

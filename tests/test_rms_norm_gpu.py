@@ -114,6 +114,29 @@ def test_bprop(rows, cols, pad, kind, packed):
     assert mx.last_device_status() == mx.OK
 
 
+@pytest.mark.parametrize("rows,cols,pad", [(40, 300, 5), (7, 4096, 8), (3, 9000, 3), (400, 2051, 1), (2, 20000, 4)])
+def test_bprop_of_packed_rows_of_any_pitch_and_in_place(rows, cols, pad):
+    """The packed sum's rows at any place, and dx in dy's memory."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    h, dy = (torch.randn(rows, cols, device="cuda", generator=gen).to(torch.bfloat16) for _ in range(2))
+    q, s = mx.empty_packed(rows, cols), mx.empty_scales(mx.BLOCK_ROW, rows, cols)
+    mx.quant8(mx.Quant8Desc.make(rows, cols), h, row=(q, s))
+    rstd, dg, dg2 = torch.rand(rows, device="cuda", generator=gen) + 0.5, torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    want = torch.empty_like(dy)
+    for ld in (q.stride(0), cols + pad):
+        wide = torch.full((rows, ld), 0x7F, dtype=torch.uint8, device="cuda").view(q.dtype)
+        wide.view(torch.uint8)[:, :cols] = q.view(torch.uint8)
+        d = mx.RmsNormDesc.make(rows, cols, x_type=mx.DTYPE_E4M3, y_type=mx.DTYPE_BF16, ldx=ld)
+        ws = torch.empty(mx.rms_norm_bprop_workspace(d), dtype=torch.uint8, device="cuda")
+        into = want if ld == q.stride(0) else dy
+        mx.rms_norm_bprop(d, dy, wide[:, :cols], None, rstd, into, dg if into is want else dg2, ws, h_scale=s)
+    # (the two ways may add the row's sum in another order: half a step of the result, and SUM_TOL of its terms)
+    hh = down(q) * np.repeat(ref.value_of(bytes_of(s)).T, ref.BLOCK, 1)[:, :cols] * down(rstd)[:, None]
+    assert np.all(np.abs(down(want) - down(dy)) <= 2.0 ** -7 * np.abs(down(want)) + SUM_TOL * down(rstd)[:, None] * (1 + np.abs(hh)) * 8)
+    assert float((dg - dg2).abs().max()) <= 1e-4 * float(dg.abs().max())
+    assert mx.last_device_status() == mx.OK
+
+
 def test_gradients_against_differences():
     rows, cols, step = 3, 40, 1e-2
     rng = np.random.default_rng(0)
