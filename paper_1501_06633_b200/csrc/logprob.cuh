@@ -515,6 +515,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) logprob_fprop_kernel(c
         const uint64_t k = keys[i];
         if (k == 0) continue;
         int at = 0;
+#pragma unroll 8
         for (int j = 0; j < (int)parts * args.top; ++j) at += keys[j] > k;
         if (at < args.top) merged[at] = k;
       }
@@ -539,7 +540,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) logprob_fprop_kernel(c
 }
 
 // ---- backward ----
-// What a row's values are turned into gradients with: g = p (a + d ln p), and `add` at the target.
+// What a row's values are turned into gradients with: g = p (a + d ln p); add: scale dlp.
 struct __align__(16) LpRow { float minus_lse, a, d, add; };
 
 __device__ __forceinline__ LpRow lp_row(const LogprobArgs& args, int64_t r, int32_t* target) {
@@ -572,15 +573,23 @@ __device__ __forceinline__ F2 lp_grad2(F2 x, F2 scale, F2 minus_lse, F2 a, F2 d)
   const float2 e = unf2(mul2(lnp, f2(kLog2e)));
   return mul2(f2(exp2_fast(e.x), exp2_fast(e.y)), fma2(d, lnp, a));
 }
-// `add` at the target among eight columns from c on.
-__device__ __forceinline__ void lp_add_target(F2 (&v)[4], float add, int32_t target, int32_t c) {
+// The gradient at the target, from its logit: 1 - p as -(exp(ln p) - 1), which loses nothing where p is near 1 (the difference of
+// p from 1 would have p's error, 2^-22, instead of its own).
+__device__ __forceinline__ float lp_target_grad(const LogprobArgs& args, const LpRow& w, int64_t row, float x) {
+  const float lnp = max_nan(fmaf(x, args.scale, w.minus_lse), kLpFar);
+  const float dh = args.dentropy ? load_global(args.dentropy + row) : 0.f;
+  const float h = args.dentropy ? load_global(args.entropy + row) : 0.f;
+  return fmaf(-w.add, expm1f(lnp), -args.scale * dh * expf(lnp) * (lnp + h));
+}
+// `value` in the place of the target's gradient among eight columns from c on.
+__device__ __forceinline__ void lp_set_target(F2 (&v)[4], float value, int32_t target, int32_t c) {
   const uint32_t in = (uint32_t)(target - c);
   if (in >= 8u) return;      // (no target: -1, which is below every column)
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float2 u = unf2(v[i]);
-    if (in == 2u * i) u.x += add;
-    if (in == 2u * i + 1u) u.y += add;
+    if (in == 2u * i) u.x = value;
+    if (in == 2u * i + 1u) u.y = value;
     v[i] = f2(u.x, u.y);
   }
 }
@@ -618,6 +627,12 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_bprop_kernel(const __gr
   int32_t target;
   const LpRow w = lp_row(args, r, &target);
   const F2 scale = f2(args.scale), ml = f2(w.minus_lse), a = f2(w.a), d = f2(w.d);
+  // the target's gradient: by the thread that has its vector, which reads the logit before it writes there (dx may be x)
+  // and writes the entry once more behind its vectors
+  const int64_t in = target - head;
+  const uint64_t mine = (uint64_t)((in >> 3) - first);
+  const bool own = in >= 0 && in < 8 * nv && mine < kLpThreads * kLpBackVecs && mine % kLpThreads == 0;
+  const float own_x = own ? lp_one<XT>(x + target) : 0.f;
 #pragma unroll
   for (int i = 0; i < kLpBackVecs; ++i) {
     const int64_t c = head + 8 * (first + i * kLpThreads);
@@ -625,15 +640,15 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_bprop_kernel(const __gr
     to_pairs<XT>(raw[i], g);
 #pragma unroll
     for (int k = 0; k < 4; ++k) g[k] = lp_grad2(g[k], scale, ml, a, d);
-    lp_add_target(g, w.add, target, (int32_t)c);
     store_pairs<XT, !SAME>(dx + c, g, n[i]);
   }
+  if (own) dx[target] = from_float<XT>(lp_target_grad(args, w, r, own_x));
   if (SAME && chunk == 0) {      // single values in front and behind
     const int64_t tail = cols - head - 8 * nv;
     const int64_t c = t < head ? t : t >= 32 && t - 32 < tail ? cols - tail + t - 32 : -1;
     if (c >= 0) {
       const float v = lp_one<XT>(x + c);
-      const float g = unf2(lp_grad2(f2(v), scale, ml, a, d)).x + (c == target ? w.add : 0.f);
+      const float g = c != target ? unf2(lp_grad2(f2(v), scale, ml, a, d)).x : lp_target_grad(args, w, r, v);
       dx[c] = from_float<XT>(g);
     }
   }
@@ -666,8 +681,13 @@ __global__ void __launch_bounds__(kLpPackThreads, 2) logprob_bprop_packed_kernel
   }
   // what is behind the last row has no p and no target
   if (t < kBlock8) {
-    if (r0 + t < args.rows) rows[t] = lp_row(args, r0 + t, &targets[t]);
-    else rows[t] = {-lp_inf(), 0.f, 0.f, 0.f}, targets[t] = -1;
+    if (r0 + t < args.rows) {
+      LpRow w = lp_row(args, r0 + t, &targets[t]);
+      // the target's gradient, where this tile has it (read before a thread writes to dx, which may be x)
+      if ((uint32_t)(targets[t] - cb * kBlock8) < (uint32_t)kBlock8)
+        w.add = lp_target_grad(args, w, r0 + t, lp_one<XT>(x + (int64_t)(r0 + t) * args.ldx + targets[t]));
+      rows[t] = w;
+    } else rows[t] = {-lp_inf(), 0.f, 0.f, 0.f}, targets[t] = -1;
   }
   __syncthreads();
   F2 g[kLpPackRows][4];
@@ -693,7 +713,7 @@ __global__ void __launch_bounds__(kLpPackThreads, 2) logprob_bprop_packed_kernel
           v[i] = f2(2 * i < have ? u.x : 0.f, 2 * i + 1 < have ? u.y : 0.f);
         }
       }
-      lp_add_target(v, w.add, targets[in], c0);
+      lp_set_target(v, w.add, targets[in], c0);
       row_max[k + h] = max8(v);
       if (args.dx) store_pairs<XT, true>(static_cast<T*>(args.dx) + (int64_t)r * args.ldd + c0, v, have);
     }

@@ -244,6 +244,24 @@ def test_gradient_of_rows_that_are_not_finite_stays_in_its_row():
         assert np.isnan(down(q)[1]).all() and np.isfinite(down(q)[[0, 2]]).all()
 
 
+@pytest.mark.parametrize("packed", [False, True])
+def test_gradient_of_tokens_that_are_nearly_certain(packed):
+    """dlogprob (1 - p) where p is near 1: relative to itself (ln p has one rounding, exp(ln p) - 1 a unit in its last place and the
+    product one), not to p."""
+    rows, cols = 16, 264
+    x = torch.zeros(rows, cols, device="cuda")
+    tok = torch.arange(rows, device="cuda") * 16
+    x[torch.arange(rows), tok] = 4.0 + torch.arange(rows, device="cuda") * 1.5
+    lse = torch.logsumexp(x.double(), 1).float()
+    d = mx.LogprobDesc.make(rows, cols, x_type=mx.DTYPE_F32)
+    dx, one = torch.empty_like(x), torch.ones(rows, device="cuda")
+    more = dict(row=(mx.empty_packed(rows, cols, mx.DTYPE_E5M2), mx.empty_scales(mx.BLOCK_ROW, rows, cols))) if packed else {}
+    mx.logprob_bprop(d, x, tok, lse, dlogprob=one, dx=dx, **more)
+    got = down(dx)[np.arange(rows), tok.cpu().numpy()]
+    want = -np.expm1(down(x)[np.arange(rows), tok.cpu().numpy()] - down(lse))
+    assert np.all(np.abs(got - want) <= 2.0 ** -21 * np.abs(want))
+
+
 def test_gradient_against_differences():
     rows, cols, step, scale = 3, 50, 1e-2, 0.8
     rng = np.random.default_rng(2)
