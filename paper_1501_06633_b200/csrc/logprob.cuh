@@ -20,6 +20,13 @@
 //
 // All loads are aligned: the values in front of the row's first multiple of 16 bytes, and behind its last, go to
 // single threads.
+//
+// Bound by memory where there are rows for all SMs: 2048 x 131072 bf16 in 97 us without the largest values, 115 us with five
+// (537 MB: 5.5 and 4.7 TB/s; the rereading and ranking at a row's end is hidden only by the other CTAs of the SM, of which
+// there are six).  301 x 49999 fp32: 15.6 us.  One row of 131072, eight CTAs: 5.0 us, with
+// 20 largest values 9.7, all latency (loads, three levels of joins, a second reading).
+// Backward: 2048 x 131072 bf16 170 us (1074 MB, 6.3 TB/s).  Packed both ways, 4096 x 32000 in 139 us: 23 instructions a value over a
+// vector of 32 lanes (IPC 0.61), its 524 MB would take 80.
 #pragma once
 #include "fp8_util.cuh"
 #include "umma_util.cuh"

@@ -18,10 +18,12 @@ maxdnn_status check_logprob(const maxdnn_logprob_desc* d) {
 
 bool aligned_to(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
-// CTAs that share a row: as many as fill the device (three to an SM), each with 4096 columns or more.
+// CTAs that share a row, each with 16384 columns or more (joining costs as much as reading those: 20 rows of 32000 in 7.8 us
+// by one CTA each and 8.7 by four): two where that gives an SM three at most (222 rows of 131072: 17.2 us, 18.9 by one), four and
+// eight where it gives two (20 rows 10.8 us, 14.1 by one; 110 rows by four, three to an SM: 19.8 us, 13.7 by two).
 int logprob_cluster(const maxdnn_logprob_desc& d, int sm_count) {
   int c = 1;
-  while (c < kLpMaxCluster && (int64_t)d.rows * c * 2 <= (int64_t)sm_count * 3 && d.cols / (2 * c) >= 4096) c *= 2;
+  while (c < kLpMaxCluster && (int64_t)d.rows * c * 2 <= (int64_t)sm_count * (c == 1 ? 3 : 2) && d.cols / (2 * c) >= 16384) c *= 2;
   return c;
 }
 
@@ -55,8 +57,9 @@ maxdnn_status logprob_fprop(const maxdnn_logprob_desc* d, const void* x, const v
   a.scale = d->scale;
   return by_wide(d->x_type, [&](auto xt) {
     constexpr int X = decltype(xt)::value;
-    // many rows: smaller CTAs, so that the end of one row is under way next to the readings of more others
-    if (parts == 1 && d->rows >= 6 * dev.sm_count)
+    // many rows: smaller CTAs, so that the end of one row is under way next to the readings of more others (4000 rows of 32000: 72 us
+    // instead of 89, of 131072: 199 instead of 212; 500 rows: 16.7 and 44.2 us instead of 15.9 and 41.3)
+    if (parts == 1 && d->rows >= 4 * dev.sm_count)
       return launch_early(entropy ? logprob_fprop_kernel<X, true, 128> : logprob_fprop_kernel<X, false, 128>, (unsigned)d->rows, 128, 0, 1,
                           stream, a);
     return launch_early(entropy ? logprob_fprop_kernel<X, true, 256> : logprob_fprop_kernel<X, false, 256>, (unsigned)(d->rows * parts), 256, 0,

@@ -18,9 +18,9 @@
 // ("MN-major").  X is read along either axis the same way, so nothing is transposed in memory.
 //
 // One launch.  Kernels of their own for each product would start 3 steps times, and a start (launch, barriers, tensor memory, the
-// first copies) with the end of the kernel before costs about 6 us.  Here the CTAs of a cooperative launch go from product to product: the warps
-// that finish tiles report a CTA's end of a product to a counter in memory, and one warp of each CTA waits for all of them and lets
-// the CTA's others on.
+// first copies) with the end of the kernel before costs about 6 us; the exchange that replaces it costs about 4.  Here the CTAs of
+// a cooperative launch go from product to product: the warps that finish tiles report a CTA's end of a product to a counter in
+// memory, and one warp of each CTA waits for all of them and lets the CTA's others on.
 //
 // Roles.  Warp 0 copies A, warp 3 copies B, warp 1 issues the MMAs, warp 2 watches the counter; warps 4-11 finish the tiles.
 // Two accumulators alternate, so a tile is finished while the next one's MMAs run.  A finishing warp has 32 rows x up
@@ -28,6 +28,11 @@
 // one part ahead, and store the result from the same slot.
 // PAIR.  Two CTAs share a tile of 256 rows (cta_group::2): each stages its 128 rows of A and half of the columns of B.
 // Halves.  Where the last round of tiles would leave at least half of the CTAs without one, its tiles are cut in two.
+//
+// Bound by what SMs read from the second-level cache: a stage of 32 KB for 256 x 256 x 64 takes 628 cycles, one of
+// 24 KB for 256 x 128 x 64 518, or 47 to 52 bytes a cycle and SM, where the MMAs need 512 and 256.  4096 x 4096, five
+// steps: 1145 us by itself and 1320 us in a long run (power); 1.37 TFLOP are 827 us at the library's measured rate and 977 at its sustained one.  With 3, 4 and 5 stages 1541, 1424 and
+// 1385 us, without the cache hint 1431, a launch for each product 1376 (long runs).  1000 x 2309: 200 us, 15 products with few tiles for each SM.
 // Every wait on a barrier or the counter is bounded and ends in a status code; TMEM is always freed.  (Waits for tensor
 // memory and at a cluster's end: see gemm8.cuh.)
 #pragma once

@@ -104,6 +104,27 @@ def test_alternatives_where_values_are_equal_or_masked(rows, cols, kind):
         check(x, kind, 1.0, target, 3)
 
 
+@pytest.mark.parametrize("rows,cols,pad", [(1, 131072, 0), (2, 150001, 7), (20, 131079, 0), (60, 65539, 5), (76, 131100, 0), (140, 33000, 0)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_long_rows_that_ctas_share(rows, cols, pad, kind):
+    """By 8, 8, 8, 4, 2 and 2 CTAs; rows with one token, with none, of one value, and with their tokens in one CTA's part."""
+    rng = np.random.default_rng(cols)
+    x = logits(rng, rows, cols, kind)
+    target = rng.integers(0, cols, rows)
+    target[1::5] = -1
+    n = np.arange(cols)
+    special = [np.where(n == cols - 1, 2.0, -np.inf), np.full(cols, -np.inf), np.full(cols, 3.0), np.where(n < 40, n * 0.25, -np.inf),
+               np.where(n >= cols - 9, n - cols, float(torch.finfo(WIDE[kind][1]).min))]
+    check(x, kind, 0.75, target, 32, cols + pad)
+    for i, row in enumerate(special):
+        if rows > 2 and i < len(special) - 1:      # all at once
+            x[(i + 1) * rows // 6] = as_held(row[None], kind)[0]
+            continue
+        x[0] = as_held(row[None], kind)[0]
+        target[0] = (cols - 1, 3)[i % 2]
+        check(x, kind, 1.0, target, 20, cols + pad, i % 2 == 0)
+
+
 @pytest.mark.parametrize("rows,threads", [(300, 256), (900, 128)])
 def test_alternatives_of_long_rows_whose_large_values_lie_close_together(rows, threads):
     """More values above the bound than there is room for, in fewer threads than alternatives: the rows' large values lie at one
