@@ -25,7 +25,7 @@
 // (537 MB: 5.5 and 4.7 TB/s; the rereading and ranking at a row's end is hidden only by the other CTAs of the SM, of which
 // there are six).  301 x 49999 fp32: 15.6 us.  One row of 131072, eight CTAs: 5.0 us, with
 // 20 largest values 9.7, all latency (loads, three levels of joins, a second reading).
-// Backward: 2048 x 131072 bf16 170 us (1074 MB, 6.3 TB/s).  Packed both ways, 4096 x 32000 in 139 us: 23 instructions a value over a
+// Backward: 2048 x 131072 bf16 170 us (1074 MB, 6.3 TB/s).  Packed both ways, 4096 x 32000 in 143 us: 24 instructions a value over a
 // vector of 32 lanes (IPC 0.61), its 524 MB would take 80.
 #pragma once
 #include "fp8_util.cuh"
@@ -573,12 +573,18 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-// Gradients of a pair of logits.
+// Gradients of a pair of logits.  EXACT: what the power's rounding to 32 bits left of ln p, up to 2^-20 of p, goes to the other
+// factor.  In front of a rounding to 16 bits it would cost 174 -> 189 us at 2048 x 131072 for nothing; packed values, where it moves
+// roundings and blocks' powers of two, and 32-bit ones have it (4096 x 32000 packed 139 -> 143 us).
+template <bool EXACT>
 __device__ __forceinline__ F2 lp_grad2(F2 x, F2 scale, F2 minus_lse, F2 a, F2 d) {
   const float2 l = unf2(fma2(x, scale, minus_lse));
   const F2 lnp = f2(max_nan(l.x, kLpFar), max_nan(l.y, kLpFar));
-  const float2 e = unf2(mul2(lnp, f2(kLog2e)));
-  return mul2(f2(exp2_fast(e.x), exp2_fast(e.y)), fma2(d, lnp, a));
+  const F2 power = mul2(lnp, f2(kLog2e));
+  F2 w = fma2(d, lnp, a);
+  if (EXACT) w = fma2(w, fma2(power, f2(-kLn2), lnp), w);
+  const float2 e = unf2(power);
+  return mul2(f2(exp2_fast(e.x), exp2_fast(e.y)), w);
 }
 // The gradient at the target, from its logit: 1 - p as -(exp(ln p) - 1), which loses nothing where p is near 1 (the difference of
 // p from 1 would have p's error, 2^-22, instead of its own).
@@ -646,7 +652,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_bprop_kernel(const __gr
     F2 g[4];
     to_pairs<XT>(raw[i], g);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) g[k] = lp_grad2(g[k], scale, ml, a, d);
+    for (int k = 0; k < 4; ++k) g[k] = lp_grad2<XT == MAXDNN_F32>(g[k], scale, ml, a, d);
     store_pairs<XT, !SAME>(dx + c, g, n[i]);
   }
   if (own) dx[target] = from_float<XT>(lp_target_grad(args, w, r, own_x));
@@ -655,7 +661,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_bprop_kernel(const __gr
     const int64_t c = t < head ? t : t >= 32 && t - 32 < tail ? cols - tail + t - 32 : -1;
     if (c >= 0) {
       const float v = lp_one<XT>(x + c);
-      const float g = c != target ? unf2(lp_grad2(f2(v), scale, ml, a, d)).x : lp_target_grad(args, w, r, v);
+      const float g = c != target ? unf2(lp_grad2<XT == MAXDNN_F32>(f2(v), scale, ml, a, d)).x : lp_target_grad(args, w, r, v);
       dx[c] = from_float<XT>(g);
     }
   }
@@ -714,7 +720,7 @@ __global__ void __launch_bounds__(kLpPackThreads, 2) logprob_bprop_packed_kernel
       to_pairs<XT>(raw[k + h], v);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        v[i] = lp_grad2(v[i], scale, ml, a, d);
+        v[i] = lp_grad2<true>(v[i], scale, ml, a, d);
         if (EDGE) {
           const float2 u = unf2(v[i]);
           v[i] = f2(2 * i < have ? u.x : 0.f, 2 * i + 1 < have ? u.y : 0.f);
