@@ -96,18 +96,20 @@ __device__ __forceinline__ Raw8<DT> stage_raw8(const uint8_t* at, int n) {
 
 // A row that the group's threads have written into a stage as it will lie in memory (`shift` bytes into the units at `from`, all
 // of them behind a fence and a barrier): whole units by one bulk copy, which thread 0 has to wait for, and single values in
-// front and behind by the group's first threads.
+// front and behind (up to seven each) by the group's first threads.  A row without a whole unit, which may lie in two: up to 14
+// values, all of them single.
 template <class T>
 __device__ __forceinline__ void store_staged(T* row, const uint8_t* from, uint32_t shift, int cols, int t) {
   const uint32_t end = shift + (uint32_t)cols * (uint32_t)sizeof(T), u0 = (shift + 15u) & ~15u, u1 = end & ~15u;
   uint8_t* to = reinterpret_cast<uint8_t*>(row) - shift;
-  if (t == 0 && u1 > u0) {
+  const bool whole = u1 > u0;
+  if (t == 0 && whole) {
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to + u0), "r"(smem_u32(from) + u0), "r"(u1 - u0)
                  : "memory");
   }
-  const uint32_t front = (u1 > u0 ? u0 : end), back = u1 > u0 ? u1 : end;      // (a row inside one unit: all of it in front)
-  const uint32_t at = t < 8 ? shift + t * (uint32_t)sizeof(T) : back + (t - 8) * (uint32_t)sizeof(T);
-  if (t < 16 && at < (t < 8 ? front : end)) *reinterpret_cast<T*>(to + at) = *reinterpret_cast<const T*>(from + at);
+  const bool front = !whole || t < 8;
+  const uint32_t at = front ? shift + t * (uint32_t)sizeof(T) : u1 + (t - 8) * (uint32_t)sizeof(T);
+  if (t < 16 && at < (whole && front ? u0 : end)) *reinterpret_cast<T*>(to + at) = *reinterpret_cast<const T*>(from + at);
 }
 
 // Sum over the WR warps of a row's group.
