@@ -30,6 +30,7 @@ constexpr int kSmallImage = kSmallN * kSmallSlice * 2, kSmallSquare = kSmallN * 
 constexpr int kSmallPartial = kSmallN * kSmallPitch * 4;
 constexpr int kSmallTmem = 2 * kSmallSlice;      // columns: products, X
 constexpr int kSmallSmem = 1024 + kSmallImage + 2 * kSmallSquare + kSmallPartial;
+static_assert(2 * kSmallSquare + kSmallPartial >= 2 * kSmallImage, "a slice of X in 32 bits fits behind the image");
 
 struct OrthoSmallArgs {
   const void* x;
@@ -179,29 +180,24 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
     const double factor = norm_factor;
     const float narrow = (float)factor;
     const bool wide = !(narrow > 1e-30f && narrow < 1e30f);
-    // through shared memory to the threads that keep the entries: hi in the image, lo in `partial`, laid out as the image
-    uint8_t* rest = reinterpret_cast<uint8_t*>(partial);
+    // through shared memory to the threads that keep the entries: in 32 bits where A, B and the partial sums will be, the first and the
+    // last four of each eight laid out as the image.  (Not as two FP16 numbers: they end at 2^-35, where |G| is far below eps)
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
       float v[8];
       to_float8<XT>(raw[i], v);
-      uint32_t hi[4], lo[4];
+      uint32_t hi[4];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = wide ? (float)((double)v[k] * factor) : v[k] * narrow;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        float a = v[2 * k] * narrow, b = v[2 * k + 1] * narrow;
-        if (wide) {
-          a = (float)((double)v[2 * k] * factor);
-          b = (float)((double)v[2 * k + 1] * factor);
-        }
-        const __half2 h = __floats2half2_rn(a, b);
-        const float2 back = __half22float2(h);
-        const __half2 l = __floats2half2_rn((a - back.x) * kOrthoLo, (b - back.y) * kOrthoLo);
+        const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
         hi[k] = *reinterpret_cast<const uint32_t*>(&h);
-        lo[k] = *reinterpret_cast<const uint32_t*>(&l);
       }
       const uint32_t at = image_at(kRows, row_read(i), c_read / 8);
       *reinterpret_cast<uint4*>(image + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-      *reinterpret_cast<uint4*>(rest + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      *reinterpret_cast<float4*>(square_a + at) = make_float4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<float4*>(square_a + kSmallImage + at) = make_float4(v[4], v[5], v[6], v[7]);
     }
   }
   __syncthreads();
@@ -214,14 +210,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t at = image_at(kRows, row, chunk0 + 4 * u + i);
-      Raw8<MAXDNN_F16> hi, lo;
-      hi.a = *reinterpret_cast<const uint4*>(image + at);
-      lo.a = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(partial) + at);
-      float a[8], b[8];
-      to_float8<MAXDNN_F16>(hi, a);
-      to_float8<MAXDNN_F16>(lo, b);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[8 * i + k] = fmaf(b[k], 1.f / kOrthoLo, a[k]);
+      for (int k = 0; k < 2; ++k) {
+        const float4 f = *reinterpret_cast<const float4*>(square_a + k * kSmallImage + at);
+        v[8 * i + 4 * k] = f.x; v[8 * i + 4 * k + 1] = f.y; v[8 * i + 4 * k + 2] = f.z; v[8 * i + 4 * k + 3] = f.w;
+      }
     }
     tmem_st_32x32(t_x + 32u * u, v);
   }

@@ -1,0 +1,30 @@
+"""The orthogonalised update's special values and sizes of gradients through both of its kernels: matrices that a cluster keeps
+(shorter side up to 128, longer up to 4096), alone in a CTA and shared by 2 to 16, and those that go through memory.
+Tolerances: see test_orthogonalise_gpu.py."""
+import pytest
+import torch
+
+import paper_1501_06633_b200 as mx
+from test_orthogonalise_gpu import call, formula, gradients, near
+
+pytestmark = pytest.mark.gpu
+KEPT = [(16, 16), (64, 100), (128, 128), (400, 60), (90, 1000), (2000, 100), (100, 4000)]
+CHAIN = [(130, 260), (300, 140)]
+
+
+@pytest.mark.parametrize("rows,cols", KEPT + CHAIN)
+@pytest.mark.parametrize("size", [1e-35, 1e-30, 1e-20, 1e-18, 1e-17, 1e-16, 1e-14, 1e-10, 1e-8, 1e-7, 1e-6, 1e-4, 1e20, 1e35])
+def test_any_size_of_gradient(rows, cols, size):
+    """|G| far below eps, around it and far above, in few and many steps: as close to the formula everywhere."""
+    x = gradients(1, rows, cols, "f32", rows).double()
+    x = (x / x.norm() * size).float()
+    for steps in (5, 1, 6):
+        want = formula(x, steps)
+        near(call(x, "f32", steps), want)
+
+
+@pytest.mark.parametrize("rows,cols", KEPT + CHAIN)
+def test_steps_that_shrink(rows, cols):
+    """Coefficients below 1 make X smaller from step to step."""
+    x = gradients(1, rows, cols, "f32", 2)
+    near(call(x, "f32", 5, (0.1, -0.05, 0.0)), formula(x, 5, [(0.1, -0.05, 0.0)] * 5))
