@@ -144,7 +144,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
       to_pairs<XT>(raw[i], v);
       most = fmaxf(most, max8(v));
     }
-    const int up = most > 0.f && most < 3.0e38f ? 127 - (int)(__float_as_uint(most) >> 23) : 0;      // (subnormal: 127)
+    // (a subnormal one: by 2^127; from 2^127 on by 2^-126, the smallest unit; an infinity stays one)
+    const int up = most > 0.f && !isinf(most) ? max(127 - (int)(__float_as_uint(most) >> 23), -126) : 0;
     const F2 unit = f2(__uint_as_float((uint32_t)min(127 + up, 254) << 23));
     F2 squares = 0;
 #pragma unroll

@@ -28,3 +28,23 @@ def test_steps_that_shrink(rows, cols):
     """Coefficients below 1 make X smaller from step to step."""
     x = gradients(1, rows, cols, "f32", 2)
     near(call(x, "f32", 5, (0.1, -0.05, 0.0)), formula(x, 5, [(0.1, -0.05, 0.0)] * 5))
+
+
+@pytest.mark.parametrize("rows,cols", KEPT + CHAIN)
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [1.5e38, 2e38, 3.2e38, 3.38e38])
+def test_entries_near_the_largest_number(rows, cols, kind, top):
+    """Finite entries count, whatever their exponent: alone, next to ordinary ones, and throughout."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    for which in ("one", "some", "all"):
+        if which == "all":
+            x = torch.rand(1, rows, cols, device="cuda", generator=gen).sub_(0.5).sign_().mul_(top)
+            x[0, :, ::3] *= 0.9
+        else:
+            x = torch.randn(1, rows, cols, device="cuda", generator=gen)
+            x[0, rows // 2, cols // 2] = top
+            if which == "some":
+                x[0, 0, :] = -top
+                x[0, 1, ::2] = 0.25 * top
+        x = x.to(torch.float32 if kind == "f32" else torch.bfloat16)
+        near(call(x, kind), formula(x, 5))
