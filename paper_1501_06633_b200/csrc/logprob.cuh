@@ -573,18 +573,18 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-// Gradients of a pair of logits.  EXACT: what the power's rounding to 32 bits left of ln p, up to 2^-20 of p, goes to the other
-// factor.  In front of a rounding to 16 bits it would cost 174 -> 189 us at 2048 x 131072 for nothing; packed values, where it moves
-// roundings and blocks' powers of two, and 32-bit ones have it (4096 x 32000 packed 139 -> 143 us).
+// Gradients of a pair of logits.  EXACT: what the power's rounding to 32 bits left of ln p, up to 2^-20 of p, goes to p (not to the
+// other factor, which may be infinite).  In front of a rounding to 16 bits it would cost 174 -> 189 us at 2048 x 131072 for nothing;
+// packed values, where it moves roundings and blocks' powers of two, and 32-bit ones have it (4096 x 32000 packed 139 -> 143 us).
 template <bool EXACT>
 __device__ __forceinline__ F2 lp_grad2(F2 x, F2 scale, F2 minus_lse, F2 a, F2 d) {
   const float2 l = unf2(fma2(x, scale, minus_lse));
   const F2 lnp = f2(max_nan(l.x, kLpFar), max_nan(l.y, kLpFar));
   const F2 power = mul2(lnp, f2(kLog2e));
-  F2 w = fma2(d, lnp, a);
-  if (EXACT) w = fma2(w, fma2(power, f2(-kLn2), lnp), w);
   const float2 e = unf2(power);
-  return mul2(f2(exp2_fast(e.x), exp2_fast(e.y)), w);
+  F2 p = f2(exp2_fast(e.x), exp2_fast(e.y));
+  if (EXACT) p = fma2(p, fma2(power, f2(-kLn2), lnp), p);
+  return mul2(p, fma2(d, lnp, a));
 }
 // The gradient at the target, from its logit: 1 - p as -(exp(ln p) - 1), which loses nothing where p is near 1 (the difference of
 // p from 1 would have p's error, 2^-22, instead of its own).
