@@ -626,7 +626,9 @@ maxdnn_status maxdnn_rms_norm_bprop(const maxdnn_rms_norm_desc* desc, const void
  * both [rows][top]; a place for which no logit above -inf is left holds -inf and index -1.  A NaN counts as
  * larger than every number.  A row without any logit above -inf (all masked) has lse = -inf, logprob = -inf
  * (0 without a token), entropy = 0 and a gradient of zeros.  A row with a NaN or +inf has lse, logprob, entropy and
- * top_logprob NaN.  scale: positive and finite.  NOT_SUPPORTED: top above 32, more than 2^30 rows or columns.
+ * top_logprob NaN.  A logit that is further below the row's largest than the largest 32-bit number counts as one of -inf (but has
+ * its place among the `top`); a p below 2^-126 counts as 0.  scale: positive and finite.  NOT_SUPPORTED: scale above 2^127, top above
+ * 32, more than 2^30 rows or columns.
  */
 typedef enum maxdnn_index { MAXDNN_INDEX_I32 = 0, MAXDNN_INDEX_I64 = 1 } maxdnn_index;
 
@@ -644,7 +646,8 @@ maxdnn_status maxdnn_logprob_fprop(const maxdnn_logprob_desc* desc, const void* 
  *   dx_j = scale (dlogprob ([j = target] - p_j) - dentropy p_j (log p_j + entropy))
  * dlogprob (with target) or dentropy (with entropy), fp32 [rows], may be null.  Results, any of them: dx (x_type, pitch
  * ldd; may be x's own memory where ldd = ldx and nothing is packed in the same call), (q_row, s_row) and (q_col, s_col): dx
- * packed in row and column blocks (q_type, pitch ldq) from its 32-bit value, the operands of the two products behind it. */
+ * packed in row and column blocks (q_type, pitch ldq) from its 32-bit value, the operands of the two products behind it.
+ * An infinite dlogprob gives infinities where p is not 0 and NaN where it is, an infinite dentropy NaN, in its row alone. */
 maxdnn_status maxdnn_logprob_bprop(const maxdnn_logprob_desc* desc, const void* x, const void* target,
                                    const float* lse, const float* dlogprob, const float* entropy,
                                    const float* dentropy, void* dx, void* q_row, void* s_row, void* q_col,

@@ -7,7 +7,9 @@
 //
 // Forward.  A cluster of 1, 2, 4 or 8 CTAs has a row and reads it once: every thread keeps the running maximum of its
 // values and the two sums relative to it (in 32 bits), which are joined by warp, CTA and cluster at the end.
-// Differences to the maximum come first, so a term's error does not grow with the size of the logits.
+// Differences to the maximum come first, so a term's error does not grow with the size of the logits.  The exponential takes
+// numbers below 2^-126 for 0 (ex2.approx.ftz), forward and backward: one instruction for two, and such a term is below 2^-100 of a sum's
+// last place; a gradient below that is 0 where elementary operations would leave a subnormal number.
 //
 // The largest values come from the same reading.  Groups of threads have 64 maxima between them; the k-th largest of
 // those is a bound that at least k values reach, and hardly more than k do (a value above it is missed only by threads

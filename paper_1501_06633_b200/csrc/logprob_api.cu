@@ -12,6 +12,7 @@ maxdnn_status check_logprob(const maxdnn_logprob_desc* d) {
   if (!is_wide(d->x_type) || d->ldx < d->cols) return MAXDNN_INVALID_VALUE;
   if (d->target_type != MAXDNN_INDEX_I32 && d->target_type != MAXDNN_INDEX_I64) return MAXDNN_INVALID_VALUE;
   if (!(d->scale > 0.f) || std::isinf(d->scale)) return MAXDNN_INVALID_VALUE;
+  if (d->scale > 0x1p127f) return MAXDNN_NOT_SUPPORTED;      // (its multiple of log2 e, which differences are taken by, may be infinite)
   if (d->top > kLpMaxTop || d->cols > (1 << 30) || d->rows > (1 << 30)) return MAXDNN_NOT_SUPPORTED;      // (numbers of rows and columns are 32 bits)
   return MAXDNN_OK;
 }
