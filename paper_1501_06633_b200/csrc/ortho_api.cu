@@ -91,13 +91,43 @@ maxdnn_status chain_slots(const RuntimeDevice& dev, int (&slots)[2]) {
 
 constexpr int kNominalSlots[2] = {148, 74};      // (the workspace's layout does not depend on the device)
 
-// Matrices that a cluster has to itself.
-bool small_matrices(const maxdnn_ortho_desc& d) {
-  return std::min(d.rows, d.cols) <= kSmallN && std::max(d.rows, d.cols) <= kSmallSlice * kSmallMaxCluster;
+constexpr size_t small_smem() { return (size_t)std::max(kSmallSmem, cluster_smem_floor(kSmallTmem)); }
+
+// CTAs of the cluster that has a matrix to itself, where there is one; 0: it goes through memory.  A cluster of more than one CTA
+// needs as many SMs next to one another, which a device may not have (more than eight are no part of what every device offers).
+int small_cluster(const RuntimeDevice& dev, const maxdnn_ortho_desc& d) {
+  const int longer = std::max(d.rows, d.cols), parts = (longer + kSmallSlice - 1) / kSmallSlice;
+  if (std::min(d.rows, d.cols) > kSmallN || parts > std::min(kSmallMaxCluster, option(OPT_ORTHO_CLUSTER, kSmallMaxCluster))) return 0;
+  if (parts == 1) return 1;
+  static std::atomic<int> known[64][kSmallMaxCluster + 1];      // clusters that run at the same time + 1; 0: not asked for yet
+  int n = known[dev.index][parts].load(std::memory_order_acquire) - 1;
+  if (n < 0) {
+    // (any of the kernels: all have the same threads and memory)
+    auto kern = ortho_small_kernel<MAXDNN_BF16, false, false>;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)parts, 1, 1);
+    cfg.blockDim = dim3(kSmallThreads, 1, 1);
+    cfg.dynamicSmemBytes = small_smem();
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)parts;
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)small_smem()) != cudaSuccess ||
+        cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      n = 0;
+    }
+    known[dev.index][parts].store(n + 1, std::memory_order_release);
+  }
+  return n > 0 ? parts : 0;
 }
 
-maxdnn_status orthogonalise_small(const RuntimeDevice& dev, const maxdnn_ortho_desc& d, const void* x, const float* coefficients, void* out,
-                                  cudaStream_t stream) {
+maxdnn_status orthogonalise_small(const RuntimeDevice& dev, const maxdnn_ortho_desc& d, int parts, const void* x, const float* coefficients,
+                                  void* out, cudaStream_t stream) {
   OrthoSmallArgs a = {};
   a.x = x;
   a.out = static_cast<__nv_bfloat16*>(out);
@@ -113,8 +143,7 @@ maxdnn_status orthogonalise_small(const RuntimeDevice& dev, const maxdnn_ortho_d
     for (int k = 0; k < 3; ++k) a.coefficients[i][k] = coefficients ? coefficients[3 * i + k] : kOrthoCoefficients[k];
   a.test_missing_arrival = (uint32_t)option(OPT_TEST_MISSING_ARRIVAL);
   a.wc = runtime_wait_ctx(dev);
-  const int parts = (std::max(d.rows, d.cols) + kSmallSlice - 1) / kSmallSlice;
-  const size_t smem = (size_t)std::max(kSmallSmem, cluster_smem_floor(kSmallTmem));
+  const size_t smem = small_smem();
   const bool whole = d.cols % 8 == 0 && vec_ok(d.x_type, d.ldx) && (d.batch == 1 || vec_ok(d.x_type, d.stride_x));
   return by_wide(d.x_type, [&](auto xt) {
     return by_edge(whole, [&](auto edge) {
@@ -159,7 +188,7 @@ maxdnn_status orthogonalise(const maxdnn_ortho_desc* d, const void* x, const flo
   if (!workspace || !aligned16(workspace) || workspace_bytes < (size_t)p.bytes) return MAXDNN_INVALID_VALUE;
   RuntimeDevice dev;
   if ((st = runtime_device(&dev)) != MAXDNN_OK) return st;
-  if (small_matrices(*d)) return orthogonalise_small(dev, *d, x, coefficients, out, stream);
+  if (const int parts = small_cluster(dev, *d)) return orthogonalise_small(dev, *d, parts, x, coefficients, out, stream);
   int slots[2];
   if ((st = chain_slots(dev, slots)) != MAXDNN_OK) return st;
   if ((st = plan_ortho(*d, slots, &p)) != MAXDNN_OK) return st;

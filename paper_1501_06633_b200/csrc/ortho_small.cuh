@@ -15,6 +15,7 @@
 // With one launch and two cluster barriers a step instead of three products through memory with a wait for all CTAs after each
 // (about 4 us apiece), 16 x 512 x 128 takes 48 us instead of 84, 128 x 128 30 instead of 69, 128 x 4096 65.  What bounds it is the step's
 // chain of latencies: MMAs, reading tensor memory, the exchange of partial sums (4 us a step between two CTAs), two barriers.
+// Where a device cannot place a matrix's cluster, the matrix goes through memory (ortho_api.cu).
 // All waits on barriers in shared memory are bounded; a wait that runs out leaves the launch's results invalid and its status says so.
 #pragma once
 #include "ortho.cuh"

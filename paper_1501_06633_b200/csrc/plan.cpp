@@ -19,7 +19,7 @@ const char* const kOptionNames[OPT_COUNT] = {
     "UMMA_KC", "UMMA_PAIR", "UMMA_MERGE", "UMMA_STAGE_KB", "UMMA_COLS",
     "WGRAD_SPLITS", "WGRAD_PAIR", "SM_COUNT", "X3_CHUNK_ROWS", "DEBUG_STATUS",
     "KERNEL_CLOCK", "RAGGED_PADDED", "GEMM8_COLS", "GEMM8_SPLIT", "GEMM8_SWAP", "GEMM8_PAIR",
-    "TEST_MISSING_ARRIVAL"};
+    "ORTHO_CLUSTER", "TEST_MISSING_ARRIVAL"};
 struct OptionSlot {
   std::atomic<int32_t> value{0};
   std::atomic<bool> set{false};

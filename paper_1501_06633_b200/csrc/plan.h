@@ -21,7 +21,7 @@ enum OptionId : int {
   OPT_UMMA_KC, OPT_UMMA_PAIR, OPT_UMMA_MERGE, OPT_UMMA_STAGE_KB, OPT_UMMA_COLS,
   OPT_WGRAD_SPLITS, OPT_WGRAD_PAIR, OPT_SM_COUNT, OPT_X3_CHUNK_ROWS, OPT_DEBUG_STATUS,
   OPT_KERNEL_CLOCK, OPT_RAGGED_PADDED, OPT_GEMM8_COLS, OPT_GEMM8_SPLIT, OPT_GEMM8_SWAP, OPT_GEMM8_PAIR,
-  OPT_TEST_MISSING_ARRIVAL, OPT_COUNT
+  OPT_ORTHO_CLUSTER, OPT_TEST_MISSING_ARRIVAL, OPT_COUNT
 };
 bool option_is_set(OptionId id);
 int option(OptionId id, int unset_value = 0);          // the value, or unset_value
