@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
   typedef typename ElemOf<XT>::T T;
   constexpr int kRows = TALL ? kSmallSlice : kSmallN;        // of the image
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bar_mem;
+  __shared__ __align__(8) uint64_t bar_mem[2];      // a product's end; after a wait that ran out: the end of all of them
   __shared__ uint32_t tmem_mem;
   __shared__ double norm_part, norm_factor;
   __shared__ double warp_part[kSmallThreads / 32];
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
   uint8_t* square_b = square_a + kSmallSquare;
   float* partial = reinterpret_cast<float*>(square_b + kSmallSquare);
   const uint32_t u_image = base, u_a = base + kSmallImage, u_b = u_a + kSmallSquare, u_partial = u_b + kSmallSquare;
-  const uint32_t bar = smem_u32(&bar_mem);
+  const uint32_t bar = smem_u32(bar_mem);
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int q = warp & 3, group = warp >> 2;       // TMEM lanes; which quarter of the columns (TALL: tile of 128 rows and half)
   const int row = q * 32 + lane + (TALL ? 128 * (group >> 1) : 0);      // of the image
@@ -106,6 +106,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
   const int64_t matrix = blockIdx.x / parts;
   if (t == 0) {
     mbar_init(bar, 1 + (args.test_missing_arrival != 0 && blockIdx.x == 0 ? 1 : 0));      // (test hook)
+    mbar_init(bar + 8u, 1);
     fence_mbar_init();
     fence_proxy_async_smem();
   }
@@ -223,12 +224,14 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
   tmem_wait_st();
 
   // ---- products: one thread issues the MMAs when all have written what they read, and all wait for their end
+  // (a CTA whose wait ran out goes on with its cluster's barriers, but issues no more)
   uint32_t phase = 0;
+  bool ok = true;
   auto product = [&](auto issue) {
     tcgen05_fence_before();
     fence_proxy_async_smem();
     __syncthreads();
-    if (warp == 0) {
+    if (warp == 0 && __all_sync(0xFFFFFFFFu, ok)) {
       tcgen05_fence_after();
       if (elect_one()) {
         fence_proxy_async_smem();
@@ -237,7 +240,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
       }
       __syncwarp();
     }
-    mbar_wait(bar, phase, args.wc, kDevTimeoutAccum);
+    ok = ok && mbar_wait(bar, phase, args.wc, kDevTimeoutAccum);
     phase ^= 1u;
     tcgen05_fence_after();
   };
@@ -478,6 +481,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const __g
   cluster_arrive();      // no CTA leaves while another may still read its shared memory
   cluster_wait();
   if (warp == 0) {
+    if (!__all_sync(0xFFFFFFFFu, ok)) {      // every MMA issued so far has finished before TMEM is released
+      if (elect_one()) tcgen05_commit(bar + 8u);
+      __syncwarp();
+      mbar_wait_grace(bar + 8u, 0);
+    }
     tcgen05_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kSmallTmem) : "memory");
   }
