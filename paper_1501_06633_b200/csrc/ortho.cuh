@@ -282,6 +282,7 @@ ortho_chain_kernel(const __grid_constant__ OrthoMaps maps, const __grid_constant
         }
       }
     }
+    if (PAIR && ok) ok = wait_stages_free(empty_bar, stages, stage, phase, args.wc);
     if (!ok) {
       // leaving early: give copies already issued time to land (a pair's report to the leader)
       if constexpr (PAIR) {

@@ -228,6 +228,17 @@ __device__ __forceinline__ void tcgen05_commit_pair(uint32_t bar, uint16_t mask 
       : "memory");
 }
 
+// For the warp that fills a pair's ring, before its CTA leaves: the leader's commits arrive at the peer's "empty" barriers too, and
+// nothing orders one commit's arrival behind another's (the accumulator's, which comes later).  So the peer stays until the last
+// one of every stage is there; by then it has been for long.
+__device__ __forceinline__ bool wait_stages_free(uint32_t empty_bar, int stages, int stage, uint32_t phase, const WaitCtx& wc) {
+  for (int s = 0; s < stages; ++s) {
+    if (!mbar_wait(empty_bar + 8u * stage, phase ^ 1u, wc, kDevTimeoutEmpty)) return false;
+    if (++stage == stages) { stage = 0; phase ^= 1u; }
+  }
+  return true;
+}
+
 // Tiled bulk tensor loads whose completion barrier may live in the peer CTA of the pair
 // (the destination is always this CTA's shared memory; nothing is multicast).
 __device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap* m, uint32_t bar,
