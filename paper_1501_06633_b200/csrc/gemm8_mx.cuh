@@ -270,6 +270,7 @@ gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         if (++stage == stages) { stage = 0; phase ^= 1u; }
       }
     }
+    if (PAIR && ok) ok = wait_stages_free(empty_bar, stages, stage, phase, args.wc);
     if (!ok) {
       // leaving early: give copies already issued time to land (a pair's report to the leader)
       if constexpr (PAIR) {
@@ -329,6 +330,10 @@ gemm8_mx_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       }
       __syncwarp();
     }
+    // (as wait_stages_free: the commits that free scales arrive at both CTAs)
+    if (PAIR)
+      for (uint32_t g = groups > kMxScaleBufs ? groups - kMxScaleBufs : 0; g < groups && ok; ++g)
+        ok = mbar_wait(sfe_bar + 8u * (g % kMxScaleBufs), (g / kMxScaleBufs) & 1u, args.wc, kDevTimeoutEmpty);
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMAs (the leader's, for both CTAs)
     if (leader) {

@@ -393,6 +393,7 @@ umma_conv_kernel(const __grid_constant__ CUtensorMap map_filt,
         if (++stage == stages) { stage = 0; phase ^= 1u; }
       }
     }
+    if (PAIR && ok) ok = wait_stages_free(cx.empty_bar, stages, stage, phase, args.wc);
     if (!ok) {
       // Leaving early: give copies already issued time to land.
       if constexpr (PAIR) {

@@ -302,6 +302,7 @@ wgrad_umma_kernel(const __grid_constant__ CUtensorMap map_dout,
       if (++stage == stages) { stage = 0; phase ^= 1u; }
       pc.advance(g, n_units);
     }
+    if (PAIR && ok) ok = wait_stages_free(empty_bar, stages, stage, phase, args.wc);
     if (!ok) {
       // Leaving early: give copies already issued time to land.
       if constexpr (PAIR) {
