@@ -647,7 +647,8 @@ maxdnn_status maxdnn_logprob_fprop(const maxdnn_logprob_desc* desc, const void* 
  * dlogprob (with target) or dentropy (with entropy), fp32 [rows], may be null.  Results, any of them: dx (x_type, pitch
  * ldd; may be x's own memory where ldd = ldx and nothing is packed in the same call), (q_row, s_row) and (q_col, s_col): dx
  * packed in row and column blocks (q_type, pitch ldq) from its 32-bit value, the operands of the two products behind it.
- * An infinite dlogprob gives infinities where p is not 0 and NaN where it is, an infinite dentropy NaN, in its row alone. */
+ * An infinite dlogprob gives infinities where p is not 0 and NaN where it is, an infinite dentropy infinities or NaN: in
+ * its row alone. */
 maxdnn_status maxdnn_logprob_bprop(const maxdnn_logprob_desc* desc, const void* x, const void* target,
                                    const float* lse, const float* dlogprob, const float* entropy,
                                    const float* dentropy, void* dx, void* q_row, void* s_row, void* q_col,

@@ -64,3 +64,23 @@ def test_packed(kind, packed, rows, cols):
     np.testing.assert_array_equal(got[3], want[3])
     np.testing.assert_array_equal(got[1][:, others], want[1][:, others])
     assert np.all(ref.value_of(got[1][:, at]) == 1.0)           # no finite value: as a block of zeros
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_infinite_gradients_of_the_entropy_and_masked_logits(kind):
+    """An infinite dentropy gives infinities or NaN throughout its row, an infinite dlogprob NaN where p is 0; no other row is touched."""
+    rows, cols = 4, 300
+    x, target, dlp, lse = given(rows, cols, kind, 5)
+    x[:, 7], x[:, 250:] = -float("inf"), -float("inf")
+    target %= 7
+    lse = torch.logsumexp(x.double(), 1).float()
+    entropy = torch.distributions.Categorical(logits=x.float()).probs
+    entropy = -torch.special.xlogy(entropy, entropy).sum(1)
+    dh = torch.ones(rows, device="cuda")
+    dlp[1], dh[2] = float("inf"), -float("inf")
+    dx = torch.empty_like(x)
+    mx.logprob_bprop(mx.LogprobDesc.make(rows, cols, x_type=WIDE[kind][0]), x, target, lse, dlogprob=dlp, entropy=entropy, dentropy=dh, dx=dx)
+    got, masked = down(dx), np.isinf(down(x)[0])
+    assert np.isfinite(got[[0, 3]]).all() and np.all(got[[0, 3]][:, masked] == 0) and not np.isfinite(got[2]).any()
+    np.testing.assert_array_equal(np.isnan(got[1]), masked)
+    np.testing.assert_array_equal(got[1][~masked], np.where(np.arange(cols) == int(target[1]), 1, -1)[~masked] * np.inf)

@@ -48,3 +48,20 @@ def test_entries_near_the_largest_number(rows, cols, kind, top):
                 x[0, 1, ::2] = 0.25 * top
         x = x.to(torch.float32 if kind == "f32" else torch.bfloat16)
         near(call(x, kind), formula(x, 5))
+
+
+@pytest.mark.parametrize("rows,cols", KEPT + CHAIN)
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_zeros_and_values_that_are_not_finite(rows, cols, kind):
+    x = gradients(6, rows, cols, kind, 5)
+    x[1] = 0
+    x[2, 3, 5] = float("nan")
+    x[3, rows - 1, cols - 1] = float("inf")
+    x[4, 0, 0] = -float("inf")
+    d = mx.OrthoDesc.make(rows, cols, batch=6)
+    # a workspace that holds NaN before the call
+    ws = torch.full((mx.orthogonalise_workspace(d) // 2,), float("nan"), dtype=torch.float16, device="cuda").view(torch.uint8)
+    got = call(x, kind, ws=ws)
+    assert bool((got[1] == 0).all()) and all(bool(torch.isnan(got[i]).all()) for i in (2, 3, 4))
+    for i in (0, 5):
+        near(got[i:i + 1], formula(x[i:i + 1], 5))
