@@ -89,7 +89,7 @@ maxdnn_status by_warps(int wr, F f) {
 template <int XT>
 maxdnn_status launch_rms_fprop(const RuntimeDevice& dev, RmsNormArgs& a, bool whole, cudaStream_t stream) {
   const int wr = rms_group_warps(a.cols);
-  const int64_t stage = rms_stage_row(a.cols, elem_bytes(XT)) * (a.res ? 2 : 1);
+  const int64_t stage = rms_stage_row(a.cols, elem_bytes(XT), !whole) * (a.res ? 2 : 1);
   if (wr == kRmsLong) {
     const int64_t most = 2 * (int64_t)dev.sm_count;
     return launch_early(rms_norm_fprop_long_kernel<XT>, (unsigned)(a.rows < most ? a.rows : most), 1024, 0, 1, stream, a);
