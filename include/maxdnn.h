@@ -663,10 +663,11 @@ maxdnn_status maxdnn_logprob_bprop(const maxdnn_logprob_desc* desc, const void* 
  *
  * x: x_type F32, BF16 or F16, pitch ldx, matrices stride_x apart; out: BF16, pitch ldo, stride_o.  coefficients: HOST
  * memory, [steps][3] numbers a, b, c (read during the call); null: 3.4445, -4.7750, 2.0315 for every step.  The products
- * run on the tensor cores on operands rounded to FP16 with 32-bit sums; X itself is kept in 22 bits, the diagonals of A and
+ * run on the tensor cores on operands rounded to FP16 with 32-bit sums; X itself is kept in 22 bits or more, the diagonals of A and
  * of the polynomial in 32, so that the result is about 1e-3 (of its norm) from the formula's, whatever the spectrum: less
- * than its rounding to BF16, and whatever the size of G, also far below eps.  A matrix of zeros gives zeros (with eps > 0), one with a NaN or infinity gives NaN.  The coefficients
- * have to keep every singular value of X below 10 (the default ones: below 1.3).  workspace: 16-byte
+ * than its rounding to BF16, and whatever the size of G, also far below eps.  A matrix of zeros gives zeros (with eps > 0), one
+ * with a NaN or infinity gives NaN.  The coefficients have to keep every singular value of X below 10 (the default ones: below 1.3)
+ * and of b A + c A A below 60000, and not to shrink X: its entries are held to 2^-45.  workspace: 16-byte
  * aligned, its contents do not matter, for one call at a time.  The CTAs of a call may wait for one another (a cooperative
  * launch).  NOT_SUPPORTED: rows, cols or batch above 65536, steps above 32.
  */

@@ -25,10 +25,11 @@
 //
 // Bound by memory where there are rows for all SMs: 2048 x 131072 bf16 in 97 us without the largest values, 115 us with five
 // (537 MB: 5.5 and 4.7 TB/s; the rereading and ranking at a row's end is hidden only by the other CTAs of the SM, of which
-// there are six).  301 x 49999 fp32: 15.6 us.  One row of 131072, eight CTAs: 5.0 us, with
-// 20 largest values 9.7, all latency (loads, three levels of joins, a second reading).
-// Backward: 2048 x 131072 bf16 170 us (1074 MB, 6.3 TB/s).  Packed both ways, 4096 x 32000 in 143 us: 24 instructions a value over a
-// vector of 32 lanes (IPC 0.61), its 524 MB would take 80.
+// there are six).  301 x 49999 fp32, one largest value: 18.5 us from memory, 15.2 where the second-level cache has the logits.  One
+// row of 131072, eight CTAs: 5.0 us, with 20 largest values 9.7, all latency (loads, three levels of joins, a second reading).
+// Backward: 2048 x 131072 bf16 168 to 177 us (1074 MB, 6.1 to 6.4 TB/s).  Packed both ways, 4096 x 32000 in 143 us, its 524 MB would
+// take 80: latency (loads, barriers between the two packings) that half of an SM's warps do not hide, next to 24 instructions a
+// value (IPC 0.61).
 #pragma once
 #include "fp8_util.cuh"
 #include "umma_util.cuh"
@@ -698,7 +699,7 @@ __global__ void __launch_bounds__(kLpPackThreads, 2) logprob_bprop_packed_kernel
   if (t < kBlock8) {
     if (r0 + t < args.rows) {
       LpRow w = lp_row(args, r0 + t, &targets[t]);
-      // the target's gradient, where this tile has it (read before a thread writes to dx, which may be x)
+      // the target's gradient, where this tile has it
       if ((uint32_t)(targets[t] - cb * kBlock8) < (uint32_t)kBlock8)
         w.add = lp_target_grad(args, w, r0 + t, lp_one<XT>(x + (int64_t)(r0 + t) * args.ldx + targets[t]));
       rows[t] = w;

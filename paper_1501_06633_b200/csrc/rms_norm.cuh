@@ -44,7 +44,6 @@ struct RmsNormArgs {
 };
 
 constexpr int kRmsMaxDepth = 4;
-constexpr int kRmsRegCols = 16384;       // the longest row that a group's registers hold
 __host__ __device__ constexpr int rms_threads(int wr) { return wr > 8 ? 32 * wr : 256; }
 __host__ __device__ constexpr int rms_groups(int wr) { return wr > 8 ? 1 : 8 / wr; }
 // Bytes of a row in a stage: the 16-byte units that hold it; anywhere: wherever its first value lies in one.
